@@ -464,6 +464,159 @@ pp_status pp_net_run_host(pp_net* net, const float* x_host, float* y_host, void*
 
 void pp_net_destroy(pp_net* net);
 
+/* ------------------------------------------------------------------------
+ * Decoder operators behind a trunk.  A program that answers about frames turns
+ * a trunk's map into tokens on a (time, row, column) grid, and a decoder keeps
+ * their keys and values in a paged cache and attends to them.  The paper has no
+ * counterpart: these calls serve the networks that its trunks feed.
+ *
+ * Data types: PP_F32, PP_F16, PP_BF16; one type for the queries, keys, values,
+ * cache and outputs of a call.  Sums, norms and softmax statistics are held in
+ * fp32 and each output is rounded once.
+ * Token tensors are views [T][heads][D]: element (t, h, d) is at
+ * t * token_stride + h * head_stride + d (strides in elements, so q, k and v may
+ * be parts of one fused product).  Outputs are dense [T][heads][D].  Pointers
+ * need the alignment of one element; rows on 16-byte boundaries take wider loads.
+ * Index arrays (positions, slots, tables, lengths) are caller-owned device
+ * memory and cannot be checked on the host: an entry out of its range is never
+ * followed, and sets a bit of the cache's device status word.
+ * ------------------------------------------------------------------------ */
+#define PP_F32 0
+#define PP_F16 1
+#define PP_BF16 2
+
+typedef struct pp_rope pp_rope;
+
+/*
+ * A rotation plan for heads of D values.  The first 2 * pairs values of a head
+ * form `pairs` pairs: (j, pairs + j), or (2j, 2j + 1) with interleaved != 0.
+ * Pair j turns by the angle position[axis[j]] * freq[j] (radians); values from
+ * 2 * pairs on are not turned.  One axis is the plain rotary position; three
+ * (time, row, column) serve images and video.
+ *   axis   [pairs] host bytes, each below axes (NULL: all 0)
+ *   freq   [pairs] host doubles, finite
+ *   axes   number of position axes, 1..8
+ *   stream copies are enqueued on it; the call waits for them before returning
+ * The angle is taken modulo a turn in 64-bit fixed point, so it is as exact at
+ * position 2^31 - 1 as at 0.
+ * Errors: PP_ERR_INVALID_ARG (null pointer, axes, axis or freq out of range,
+ * pairs < 0 or 2 * pairs > D), PP_ERR_UNSUPPORTED (D odd or not in 2..256),
+ * PP_ERR_CUDA, PP_ERR_OOM.
+ */
+pp_status pp_rope_create(int D, int pairs, const uint8_t* axis, const double* freq, int axes, int interleaved,
+                         void* stream, pp_rope** out);
+void pp_rope_destroy(pp_rope* rope);
+
+/*
+ * Queries and keys of T tokens, normalised per head and rotated, in one pass:
+ *   y[t][h][d] = x[t][h][d] * w[d] / sqrt(mean_d x^2 + eps), then the rotation.
+ *   pos      [axes][T] device positions (any int32)
+ *   eps      added to the mean square; negative: no normalisation (and qw, kw NULL)
+ *   qw, kw   [D] device fp32 weights, or NULL for ones
+ *   q, k     views (token stride q_ts, head stride q_hs, ...); Hq or Hk may be 0
+ *   q_out    [T][Hq][D], k_out [T][Hk][D]; each may be its own input where that is dense
+ * Asynchronous on stream; T = 0 does nothing.  Errors: PP_ERR_INVALID_ARG (null
+ * pointer, negative size or stride, dtype, alignment), PP_ERR_CUDA.
+ */
+pp_status pp_qk_rotate(const pp_rope* rope, int dtype, int T, const int32_t* pos, float eps, const void* q, int64_t q_ts,
+                       int64_t q_hs, int Hq, const float* qw, void* q_out, const void* k, int64_t k_ts, int64_t k_hs,
+                       int Hk, const float* kw, void* k_out, void* stream);
+
+typedef struct pp_cache pp_cache;
+
+/*
+ * A paged key-value cache over caller-owned device memory (which must outlive
+ * the handle): k and v are [pages][H][page][D], 16-byte aligned.
+ *   page    tokens per page: 8, 16, 32, 64, 128 or 256
+ *   codes   [pages][H][2][D] int8 and scales [pages][H] fp32 device memory of the
+ *           page summaries (pp_cache_summarize), or both NULL: no page selection
+ * The handle owns a workspace for attention split over the cache's length, so
+ * its calls must be ordered with each other (one stream, or events); callers that
+ * attend on several streams at once make a handle for each over the same memory.
+ * Errors: PP_ERR_INVALID_ARG (null pointer, size, dtype, alignment),
+ * PP_ERR_UNSUPPORTED (page size; D not a multiple of 8 in 16..256; pages * H *
+ * page not below 2^31), PP_ERR_CUDA, PP_ERR_OOM.
+ */
+pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k, void* v, int8_t* codes, float* scales,
+                          pp_cache** out);
+void pp_cache_destroy(pp_cache* cache);
+
+/* Synchronous: bits of what the calls on this cache met since the last read (0:
+ * nothing); the word is cleared.  A call that sets a bit skips the entry. */
+#define PP_CACHE_BAD_PAGE 1    /* a page id outside 0..pages-1, or a selected index outside the table */
+#define PP_CACHE_BAD_LENGTH 2  /* a length below 0 or beyond the table, or token ranges that do not fit */
+#define PP_CACHE_BAD_SLOT 4    /* a slot outside -1..pages*page-1 */
+#define PP_CACHE_TIMEOUT 8     /* a bounded wait gave up: the call's output is invalid */
+pp_status pp_cache_device_status(const pp_cache* cache, int* device_error);
+
+/*
+ * pp_qk_rotate whose keys, and the values v as they are, go to the cache: token
+ * t to offset slots[t] % page of page slots[t] / page, -1 nowhere.  Slots of a
+ * call are distinct.  The dtype, H and D are the cache's; q may be NULL (Hq = 0).
+ * Errors: as pp_qk_rotate; also D of rope and cache not the same.
+ */
+pp_status pp_qkv_store(const pp_rope* rope, const pp_cache* cache, int T, const int32_t* pos, const int32_t* slots,
+                       float eps, const void* q, int64_t q_ts, int64_t q_hs, int Hq, const float* qw, void* q_out,
+                       const void* k, int64_t k_ts, int64_t k_hs, const float* kw, const void* v, int64_t v_ts,
+                       int64_t v_hs, void* stream);
+
+/*
+ * Summaries of n full pages (ids [n], device): per page and head, with mx[d] and
+ * mn[d] the largest and smallest key value, a = max_d max(|mx|, |mn|), r = 127 / a,
+ *   codes[0][d] = min(127, ceil(mx[d] * r)), codes[1][d] = max(-127, floor(mn[d] * r)),
+ *   scales = a * fl(1 / 127),
+ * each step one fp32 operation.  Where a is below 2^-100 the codes are 0; where a
+ * key is not finite they are 0 and the scale is NaN (the page ranks last).
+ * Call it when pages have been filled.  Errors: PP_ERR_INVALID_ARG (null pointer,
+ * n < 0, a cache without summaries), PP_ERR_CUDA.
+ */
+pp_status pp_cache_summarize(const pp_cache* cache, const int32_t* ids, int n, void* stream);
+
+/*
+ * Sequences of the two calls below.  B sequences, T query tokens:
+ *   q       [T][Hq][D] view; Hq a multiple of the cache's H: head h reads cache head h / (Hq / H)
+ *   starts  [B + 1] device: tokens starts[b] .. starts[b+1]-1 are sequence b's (0 = starts[0] <= ... <=
+ *           starts[B] = T), or NULL: one token per sequence (T = B)
+ *   table   [B][width] device page ids: keys p * page .. of sequence b are in page table[b][p]
+ *   lens    [B] device: keys of the sequence, the new tokens' own among them (0: none)
+ *   flags   PP_ATTN_CAUSAL: the i-th of n tokens sees keys 0 .. lens[b] - n + i; otherwise all lens[b]
+ */
+#define PP_ATTN_CAUSAL 1
+
+/*
+ * Pages worth reading, for every token and cache head: sel [T][H][keep], ascending
+ * indices into the token's row of the table, -1 after the last.  Of the P pages that
+ * hold the token's visible keys, the first `first` and the last `last` are always
+ * taken, and the best-scored others up to keep in all (ties: the lower index).
+ *   score = scale(page) * (sum_d p[d] codes[0][d] + m[d] codes[1][d]), where the queries of the
+ *   head's group are rounded to integers, c = rint(q * (Q / max |q|)), Q = min(127, floor(2^24 /
+ *   (127 D G))), G = Hq / H, and p[d], m[d] sum their positive and negative values.
+ * Up to rounding it bounds the sum over the group of the largest q.k of the page.  The sum is an
+ * exact integer and the score one fp32 product, so a selection depends on nothing but its inputs.
+ * A NaN score ranks lowest.  Queries that are all 0 or not finite count as 0.
+ * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, last < 1, first < 0, first + last >
+ * keep, a cache without summaries), PP_ERR_UNSUPPORTED (width > 32768, keep > 1024,
+ * Q < 1), PP_ERR_CUDA.
+ */
+pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
+                          const int32_t* starts, const int32_t* table, int width, const int32_t* lens, int flags,
+                          int first, int last, int keep, int32_t* sel, void* stream);
+
+/*
+ * Attention of the tokens over their visible keys, s = scale * q.k:
+ *   out[t][h] = sum_j softmax_j(s) v_j, and lse[t][h] = log sum_j exp(s_j) if lse is not NULL.
+ * A token that sees no key gets 0 and -infinity.
+ *   sel     [T][H][keep] as pp_cache_select writes it (any order, distinct; entries below 0 skipped):
+ *           only those pages are read; NULL (keep 0): all
+ * What the cache holds outside the visible keys is never used, NaN and infinities included.
+ * Asynchronous on stream, no allocation; the same inputs give the same bits.
+ * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, flags, scale not finite),
+ * PP_ERR_CUDA.
+ */
+pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
+                          const int32_t* starts, const int32_t* table, int width, const int32_t* lens, float scale,
+                          int flags, const int32_t* sel, int keep, void* out, float* lse, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,87 @@
+// Internal declarations of the decoder operators: element types, the rotation
+// plan and the paged cache.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "ppconv.h"
+
+struct pp_rope {
+  int D = 0, pairs = 0, axes = 0, interleaved = 0;
+  // per pair: the turn per position as a 64-bit fraction (2^64 = one turn), and its axis
+  const uint64_t* turn = nullptr;
+  const uint8_t* axis = nullptr;
+  void* dmem = nullptr;
+};
+
+struct pp_cache {
+  int dtype = 0, pages = 0, page = 0, H = 0, D = 0;
+  void* k = nullptr;
+  void* v = nullptr;
+  int8_t* codes = nullptr;
+  float* scales = nullptr;
+  void* dmem = nullptr;   // status word
+  int* status = nullptr;
+};
+
+namespace ppc {
+
+inline int dtype_size(int dtype) { return dtype == PP_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) { return dtype == PP_F32 || dtype == PP_F16 || dtype == PP_BF16; }
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <class T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// V consecutive elements moved as one (up to 16 bytes).
+template <class T, int V>
+struct alignas(sizeof(T) * V) Vec {
+  T v[V];
+};
+
+// A token of a call on the cache: its sequence and how many of that sequence's keys it sees.
+struct Seen {
+  int b, keys;
+};
+// starts null: token t is sequence t.  Lengths and ranges that do not fit are cut to what does, and recorded.
+__device__ __forceinline__ Seen seen_keys(int t, int T, int B, const int* __restrict__ starts,
+                                          const int* __restrict__ lens, int most, bool causal, int* status) {
+  int b = t, n = 1, i = 0;
+  if (starts) {
+    int lo = 0, hi = B;  // the last b with starts[b] <= t
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (starts[mid] <= t) lo = mid; else hi = mid;
+    }
+    b = lo;
+    const int s0 = starts[b], s1 = starts[b + 1];
+    n = s1 - s0;
+    i = t - s0;
+    if (i < 0 || i >= n) {  // no sequence has this token
+      atomicOr(status, PP_CACHE_BAD_LENGTH);
+      return {b, 0};
+    }
+  }
+  int len = lens[b];
+  if (len < 0 || len > most) {
+    atomicOr(status, PP_CACHE_BAD_LENGTH);
+    len = len < 0 ? 0 : most;
+  }
+  const int keys = causal ? len - n + i + 1 : len;
+  return {b, keys < 0 ? 0 : keys};
+}
+
+}  // namespace ppc

@@ -57,9 +57,21 @@ PP_ADD_SKIP = 1
 PP_RELU = 2
 PP_POOL2 = 4
 
+PP_F32 = 0
+PP_F16 = 1
+PP_BF16 = 2
+
+PP_ATTN_CAUSAL = 1
+
+PP_CACHE_BAD_PAGE = 1
+PP_CACHE_BAD_LENGTH = 2
+PP_CACHE_BAD_SLOT = 4
+PP_CACHE_TIMEOUT = 8
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _I64 = ctypes.c_int64
+_F = ctypes.c_float
 _PP = ctypes.POINTER(ctypes.c_void_p)
 
 _SIGS = {
@@ -102,6 +114,16 @@ _SIGS = {
     "pp_net_run": ([_P, _P, _P, _P], _I),
     "pp_net_run_host": ([_P, _P, _P, _P], _I),
     "pp_net_destroy": ([_P], None),
+    "pp_rope_create": ([_I, _I, _P, _P, _I, _I, _P, _PP], _I),
+    "pp_rope_destroy": ([_P], None),
+    "pp_qk_rotate": ([_P, _I, _I, _P, _F, _P, _I64, _I64, _I, _P, _P, _P, _I64, _I64, _I, _P, _P, _P], _I),
+    "pp_cache_create": ([_I, _I, _I, _I, _I, _P, _P, _P, _P, _PP], _I),
+    "pp_cache_destroy": ([_P], None),
+    "pp_cache_device_status": ([_P, _P], _I),
+    "pp_qkv_store": ([_P, _P, _I, _P, _P, _F, _P, _I64, _I64, _I, _P, _P, _P, _I64, _I64, _P, _P, _I64, _I64, _P], _I),
+    "pp_cache_summarize": ([_P, _P, _I, _P], _I),
+    "pp_cache_select": ([_P, _I, _P, _I64, _I64, _I, _I, _P, _P, _I, _P, _I, _I, _I, _I, _P, _P], _I),
+    "pp_attn_forward": ([_P, _I, _P, _I64, _I64, _I, _I, _P, _P, _I, _P, _F, _I, _P, _I, _P, _P, _P], _I),
 }
 for _name, (_args, _res) in _SIGS.items():
     _fn = getattr(lib, _name)
@@ -416,3 +438,152 @@ def pp_net_run_host(net, x_host, y_host, stream=None):
 
 def pp_net_destroy(net):
     lib.pp_net_destroy(net)
+
+
+# ------------------------------------------------------------------ decoder operators
+
+
+def _dtype(t) -> int:
+    """The library's type code of a tensor; PP_ERR_INVALID_ARG for types it does not take."""
+    name = str(t.dtype)
+    try:
+        return {"torch.float32": PP_F32, "torch.float16": PP_F16, "torch.bfloat16": PP_BF16}[name]
+    except KeyError:
+        raise PPError(PP_ERR_INVALID_ARG, f"dtype {name}") from None
+
+
+def _heads(t, dtype, T, D):
+    """(pointer, token stride, head stride, heads) of a view [T][heads][D]; None is no heads."""
+    if t is None:
+        return None, 0, 0, 0
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or (t.stride(2) != 1 and D > 1) or _dtype(t) != dtype:
+        raise PPError(PP_ERR_INVALID_ARG, "a token tensor is [T][heads][D] of the call's type, dense in D")
+    return t.data_ptr(), t.stride(0), t.stride(1), t.shape[1]
+
+
+def _dense(t, shape, dtype, where):
+    """Pointer of a dense tensor of this shape and torch type name."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or str(t.dtype) != dtype or not t.is_contiguous():
+        raise PPError(PP_ERR_INVALID_ARG, f"{where}: expected a dense {dtype} of {tuple(shape)}")
+    return t.data_ptr()
+
+
+class Rope(int):
+    """A rotation plan's handle with what the binding checks shapes by."""
+    D: int
+    axes: int
+
+
+class Cache(int):
+    """A cache's handle with what the binding checks shapes by; it keeps the pools alive."""
+    dtype: int
+    shape: tuple
+
+
+def pp_rope_create(D, axis, freq, axes=1, interleaved=False, stream=None) -> Rope:
+    """axis and freq [pairs]: pair j turns by position[axis[j]] * freq[j] (axis None: all 0)."""
+    f = _host(freq, np.float64)
+    a = _host(axis, np.uint8)
+    if f.ndim != 1 or (a is not None and a.shape != f.shape):
+        raise PPError(PP_ERR_INVALID_ARG, "pp_rope_create shapes")
+    out = ctypes.c_void_p()
+    _check(lib.pp_rope_create(D, len(f), _hp(a), _hp(f), axes, 1 if interleaved else 0, _stream(stream),
+                              ctypes.byref(out)), "pp_rope_create")
+    r = Rope(out.value)
+    r.D, r.axes = D, axes
+    return r
+
+
+def pp_rope_destroy(rope):
+    lib.pp_rope_destroy(rope)
+
+
+def pp_qk_rotate(rope, pos, eps, q, qw, q_out, k, kw, k_out, stream=None):
+    """q [T][Hq][D], k [T][Hk][D] (either may be None) normalised and rotated into q_out, k_out; pos [axes][T] int32."""
+    x = q if q is not None else k
+    T, D, dt = x.shape[0], rope.D, _dtype(x)
+    name = str(x.dtype)
+    qp, qt, qh, Hq = _heads(q, dt, T, D)
+    kp, kt, kh, Hk = _heads(k, dt, T, D)
+    _check(lib.pp_qk_rotate(rope, dt, T, _dense(pos, (rope.axes, T), "torch.int32", "pos"), eps, qp, qt, qh, Hq,
+                            _dense(qw, (D,), "torch.float32", "qw"), _dense(q_out, (T, Hq, D), name, "q_out"), kp, kt,
+                            kh, Hk, _dense(kw, (D,), "torch.float32", "kw"), _dense(k_out, (T, Hk, D), name, "k_out"),
+                            _stream(stream)), "pp_qk_rotate")
+
+
+def pp_cache_create(k, v, codes=None, scales=None) -> Cache:
+    """k, v: pools [pages][H][page][D]; codes [pages][H][2][D] int8 and scales [pages][H] fp32 of the page summaries."""
+    if k.dim() != 4:
+        raise PPError(PP_ERR_INVALID_ARG, "pp_cache_create shapes")
+    pages, H, page, D = k.shape
+    name = str(k.dtype)
+    out = ctypes.c_void_p()
+    _check(lib.pp_cache_create(_dtype(k), pages, page, H, D, _dense(k, k.shape, name, "k"),
+                               _dense(v, k.shape, name, "v"), _dense(codes, (pages, H, 2, D), "torch.int8", "codes"),
+                               _dense(scales, (pages, H), "torch.float32", "scales"), ctypes.byref(out)),
+           "pp_cache_create")
+    c = Cache(out.value)
+    c.dtype, c.shape, c.pools = _dtype(k), (pages, H, page, D), (k, v, codes, scales)
+    return c
+
+
+def pp_cache_destroy(cache):
+    lib.pp_cache_destroy(cache)
+
+
+def pp_cache_device_status(cache) -> int:
+    """Bits PP_CACHE_* of what the calls met since the last read (synchronous)."""
+    v = _I()
+    _check(lib.pp_cache_device_status(cache, ctypes.byref(v)), "pp_cache_device_status")
+    return v.value
+
+
+def pp_qkv_store(rope, cache, pos, slots, eps, q, qw, q_out, k, kw, v, stream=None):
+    """pp_qk_rotate with the keys, and the values as they are, stored to slots [T] (int32) of the cache."""
+    T, D, dt = k.shape[0], rope.D, cache.dtype
+    H = cache.shape[1]
+    qp, qt, qh, Hq = _heads(q, dt, T, D)
+    kp, kt, kh, Hk = _heads(k, dt, T, D)
+    vp, vt, vh, Hv = _heads(v, dt, T, D)
+    if Hk != H or Hv != H:
+        raise PPError(PP_ERR_INVALID_ARG, "pp_qkv_store: k and v have the cache's heads")
+    _check(lib.pp_qkv_store(rope, cache, T, _dense(pos, (rope.axes, T), "torch.int32", "pos"),
+                            _dense(slots, (T,), "torch.int32", "slots"), eps, qp, qt, qh, Hq,
+                            _dense(qw, (D,), "torch.float32", "qw"), _dense(q_out, (T, Hq, D), str(k.dtype), "q_out"),
+                            kp, kt, kh, _dense(kw, (D,), "torch.float32", "kw"), vp, vt, vh, _stream(stream)),
+           "pp_qkv_store")
+
+
+def pp_cache_summarize(cache, ids, stream=None):
+    """Summaries of the full pages ids [n] (int32) into the cache's codes and scales."""
+    _check(lib.pp_cache_summarize(cache, _dense(ids, (ids.numel(),), "torch.int32", "ids"), ids.numel(),
+                                  _stream(stream)), "pp_cache_summarize")
+
+
+def _sequences(q, cache, starts, table, lens):
+    """The arguments that pp_cache_select and pp_attn_forward share: tokens, queries, sequences."""
+    T = q.shape[0]
+    qp, qt, qh, Hq = _heads(q, cache.dtype, T, cache.shape[3])
+    B, width = table.shape
+    return (cache, T, qp, qt, qh, Hq, B, _dense(starts, (B + 1,), "torch.int32", "starts"),
+            _dense(table, (B, width), "torch.int32", "table"), width, _dense(lens, (B,), "torch.int32", "lens"))
+
+
+def pp_cache_select(cache, q, starts, table, lens, flags, first, last, sel, stream=None):
+    """The pages of each token and cache head worth reading, into sel [T][H][keep] (int32); see the header."""
+    keep = sel.shape[2]
+    _check(lib.pp_cache_select(*_sequences(q, cache, starts, table, lens), flags, first, last, keep,
+                               _dense(sel, (q.shape[0], cache.shape[1], keep), "torch.int32", "sel"), _stream(stream)),
+           "pp_cache_select")
+
+
+def pp_attn_forward(cache, q, starts, table, lens, scale, flags, sel, out, lse=None, stream=None):
+    """Attention of q [T][Hq][D] over the cache into out; sel None: every visible page.  lse [T][Hq] fp32 or None."""
+    T, Hq, D = q.shape
+    keep = 0 if sel is None else sel.shape[2]
+    _check(lib.pp_attn_forward(*_sequences(q, cache, starts, table, lens), scale, flags,
+                               _dense(sel, (T, cache.shape[1], keep), "torch.int32", "sel"), keep,
+                               _dense(out, (T, Hq, D), str(q.dtype), "out"),
+                               _dense(lse, (T, Hq), "torch.float32", "lse"), _stream(stream)), "pp_attn_forward")
