@@ -606,12 +606,13 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  * Attention of the tokens over their visible keys, s = scale * q.k:
  *   out[t][h] = sum_j softmax_j(s) v_j, and lse[t][h] = log sum_j exp(s_j) if lse is not NULL.
  * A token that sees no key gets 0 and -infinity.
- *   sel     [T][H][keep] as pp_cache_select writes it (any order, distinct; entries below 0 skipped):
- *           only those pages are read; NULL (keep 0): all
+ *   sel     [T][H][keep] as pp_cache_select writes it, only those pages are read: distinct, in any
+ *           order, the ones that the token sees before others (of a token that sees P pages the first
+ *           min(keep, P) entries count; those below 0 are skipped); NULL (keep 0): all pages
  * What the cache holds outside the visible keys is never used, NaN and infinities included.
  * Asynchronous on stream, no allocation; the same inputs give the same bits.
  * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, flags, scale not finite),
- * PP_ERR_CUDA.
+ * PP_ERR_UNSUPPORTED (width * page not below 2^31), PP_ERR_CUDA.
  */
 pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
                           const int32_t* starts, const int32_t* table, int width, const int32_t* lens, float scale,

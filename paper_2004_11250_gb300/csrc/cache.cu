@@ -170,6 +170,30 @@ __global__ void __launch_bounds__(256) select_kernel(const SelectParams p) {
 
 DeviceOnce g_select_once;
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// A pool as [pages * H * page][D]: boxes of 128 bytes by up to a tile of one page's rows, zeros beyond D.
+bool pool_map(CUtensorMap* m, const pp_cache& c, void* pool) {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+      q != cudaDriverEntryPointSuccess)
+    return false;
+  const int e = dtype_size(c.dtype);
+  const cuuint64_t dims[2] = {(cuuint64_t)c.D, (cuuint64_t)c.pages * c.H * c.page};
+  const cuuint64_t strides[1] = {(cuuint64_t)c.D * e};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / e), (cuuint32_t)std::min(c.page, tile_keys(c.dtype))};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType t = c.dtype == PP_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                : c.dtype == PP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                    : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return reinterpret_cast<EncodeTiledFn>(fn)(m, t, 2, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 extern "C" {
@@ -195,19 +219,28 @@ pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k,
   c->v = v;
   c->codes = codes;
   c->scales = scales;
-  cudaError_t e = cudaMalloc(&c->dmem, 256);
+  const int sms = device_sms();
+  if (sms <= 0 || attn_prepare() != cudaSuccess || !pool_map(&c->mk, *c, k) || !pool_map(&c->mv, *c, v)) {
+    delete c;
+    return PP_ERR_CUDA;
+  }
+  const AttnSpace space = attn_space(dtype, D, sms);
+  const size_t head = 256 + (space.counters + 255) / 256 * 256;
+  cudaError_t e = cudaMalloc(&c->dmem, head + space.partial);
   if (e != cudaSuccess) {
     cudaGetLastError();
     delete c;
     return e == cudaErrorMemoryAllocation ? PP_ERR_OOM : PP_ERR_CUDA;
   }
-  e = cudaMemset(c->dmem, 0, 256);
+  e = cudaMemset(c->dmem, 0, head);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
     pp_cache_destroy(c);
     return PP_ERR_CUDA;
   }
   c->status = static_cast<int*>(c->dmem);
+  c->counters = reinterpret_cast<int*>(static_cast<char*>(c->dmem) + 256);
+  c->partial = reinterpret_cast<float*>(static_cast<char*>(c->dmem) + head);
   *out = c;
   return PP_OK;
 }

@@ -25,11 +25,23 @@ struct pp_cache {
   void* v = nullptr;
   int8_t* codes = nullptr;
   float* scales = nullptr;
-  void* dmem = nullptr;   // status word
+  void* dmem = nullptr;   // status word, counters and partial results
   int* status = nullptr;
+  int* counters = nullptr;   // zero between calls
+  float* partial = nullptr;
+  CUtensorMap mk, mv;        // the pools as rows of D values; boxes of one 128-byte column of a page's rows
 };
 
 namespace ppc {
+
+// The row kernel's keys per tile (attn.cu): 64 rows of 16-bit values, 32 of fp32.
+inline int tile_keys(int dtype) { return dtype == PP_F32 ? 32 : 64; }
+// Device bytes that attention needs beside the status word: counters, then partial results.
+struct AttnSpace {
+  size_t counters, partial;
+};
+AttnSpace attn_space(int dtype, int D, int sms);
+cudaError_t attn_prepare();
 
 inline int dtype_size(int dtype) { return dtype == PP_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == PP_F32 || dtype == PP_F16 || dtype == PP_BF16; }

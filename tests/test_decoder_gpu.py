@@ -629,3 +629,36 @@ def test_refusals(pp):
             pp.pp_cache_destroy(c)
         for r in (rope, other):
             pp.pp_rope_destroy(r)
+
+
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("where", ["value", "key"])
+def test_what_a_later_token_sees_reaches_no_earlier_one(pp, dt, where):
+    """NaN and infinity at a key of the chunk's own tokens: those before it stay as they were, bit for bit finite."""
+    c = Case(pp, dt, 2, 1, 64, 16, [90], [40], seed=12)
+    try:
+        pool = c.v if where == "value" else c.k
+        for key, bad in ((70, math.nan), (81, math.inf)):
+            pool[int(c.table[0, key // 16]), 0, key % 16, 5] = bad
+        c.kd.copy_(c.k)
+        c.vd.copy_(c.v)
+        out, lse = c.attend()
+        want, wl, tol, tl = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.lens, 1 / 8.0, True)
+        clean = 70 - 50  # tokens 50 .. 89 are the chunk; the first 20 see neither
+        assert ref.worst(out[:clean], want[:clean], tol[:clean]) <= 1
+        assert ref.worst(lse[:clean], wl[:clean], tl[:clean]) <= 1
+        got = out[clean:].double().cpu()
+        assert torch.equal(torch.isfinite(got), torch.isfinite(want[clean:]))
+    finally:
+        c.close()
+
+
+def test_many_parts_of_one_unit(pp):
+    """One long sequence with one cache head: hundreds of parts, joined in two levels; and unequal neighbours."""
+    for dt, lens in ((BF16, [120_000]), (F32, [60_000]), (F16, [90_000, 0, 3, 70_000])):
+        c = Case(pp, dt, 4, 1, 64, 64, lens, seed=13)
+        try:
+            c.check()
+            assert c.status() == 0
+        finally:
+            c.close()
