@@ -62,8 +62,8 @@ struct Shape {
   static constexpr int QS = E == 4 ? kRows * (DP + 4) * 4 : 0;  // fp32 queries stay in shared memory
   static constexpr int AS = DP + 8;             // row stride of the joining buffer: rows 8 banks apart
   static constexpr int ACC = kRows * AS * 4;
-  // as many stages as fit: with 228 KB per SM, 1 KB of it taken and 3 KB static per CTA, 190 KB are in flight (16 bits)
-  static constexpr int STAGES = (233472 / CTAS - 1024 - 3072 - 1024 - ACC - QS) / (2 * TILE);
+  // as many stages as fit: with 228 KB per SM, 1 KB of it taken and 6 KB static per CTA, 190 KB are in flight (16 bits)
+  static constexpr int STAGES = (233472 / CTAS - 1024 - 6144 - 1024 - ACC - QS) / (2 * TILE);
   static constexpr int SMEM = STAGES * 2 * TILE + ACC + QS + 1024;
   static constexpr int PART = kRows * DP + 2 * kRows;  // floats of a partial result
 };
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
   __shared__ alignas(8) uint64_t full_bar[ST], empty_bar[ST];
   __shared__ Stage stage[ST];
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], rm[kRows], rl[kRows];
-  __shared__ float wts[kRows][kJoin];
+  __shared__ float wts[kRows][kJoin + 1], sums[kRows][kJoin + 1];
   __shared__ int64_t scan[kThreads / 32];
   __shared__ int64_t found_base;
   __shared__ int found_item, last_flag, dead;
@@ -661,14 +661,21 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
       };
       // n parts, step apart, into acc, rm and rl: in their order, whoever comes last
       auto join = [&](int part, int n, int step) {
+        for (int i = tid; i < n * kRows; i += kWarps * 32) {  // row i % 16 of part i / 16
+          const float* from = slot(part + i / kRows * step) + kRows * DP + i % kRows;
+          if (i % kRows < nrows) {
+            wts[i % kRows][i / kRows] = __ldcg(from);
+            sums[i % kRows][i / kRows] = __ldcg(from + kRows);
+          }
+        }
+        group_sync<kWarps * 32>();
         if (tid < nrows) {
           float mx = -INFINITY, sum = 0.f;
-          for (int i = 0; i < n; ++i) mx = fmaxf(mx, __ldcg(slot(part + i * step) + kRows * DP + tid));
+          for (int i = 0; i < n; ++i) mx = fmaxf(mx, wts[tid][i]);
           for (int i = 0; i < n; ++i) {
-            const float* from = slot(part + i * step) + kRows * DP + tid;
-            const float mi = __ldcg(from), c = mi == -INFINITY ? 0.f : ex2(mi - mx);
+            const float c = wts[tid][i] == -INFINITY ? 0.f : ex2(wts[tid][i] - mx);
             wts[tid][i] = c;
-            sum += c == 0.f ? 0.f : c * __ldcg(from + kRows);
+            sum += c == 0.f ? 0.f : c * sums[tid][i];
           }
           rm[tid] = mx;
           rl[tid] = sum;
