@@ -544,7 +544,8 @@ void pp_cache_destroy(pp_cache* cache);
 /* Synchronous: bits of what the calls on this cache met since the last read (0:
  * nothing); the word is cleared.  A call that sets a bit skips the entry. */
 #define PP_CACHE_BAD_PAGE 1    /* a page id outside 0..pages-1, or a selected index outside the table */
-#define PP_CACHE_BAD_LENGTH 2  /* a length below 0 or beyond the table, or token ranges that do not fit */
+#define PP_CACHE_BAD_LENGTH 2  /* a length below 0 or beyond the table (cut to it), or token ranges that do not fit
+                                * (their tokens get no output) */
 #define PP_CACHE_BAD_SLOT 4    /* a slot outside -1..pages*page-1 */
 #define PP_CACHE_TIMEOUT 8     /* a bounded wait gave up: the call's output is invalid */
 pp_status pp_cache_device_status(const pp_cache* cache, int* device_error);

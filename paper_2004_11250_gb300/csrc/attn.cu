@@ -4,7 +4,7 @@
 // maximum and sum.  With few query rows per key (single tokens, groups of heads
 // over one cache head) it is bound by reading K and V from device memory.
 //
-// A unit is 16 query rows (tokens x the heads of a group) of one sequence and
+// A unit is 8 or 16 query rows (tokens x the heads of a group) of one sequence and
 // cache head; its keys come in tiles (64 rows of 16-bit values, 32 of fp32).
 // All units' tiles in a row are cut into equal runs, one per CTA, whatever the
 // sequences' lengths: each CTA reads the same number of bytes, and only the host's
@@ -13,9 +13,11 @@
 //
 // A producer warp looks up pages and has TMA copy their rows, as 128-byte
 // swizzled columns, into a ring; four warps take a quarter of each tile's keys
-// each: scores by mma.sync m16n8k16 (fp32: three tf32 products), a softmax of
-// their own, then the product with V, and join at the end of a unit.  mma.sync
-// and not tcgen05: at most 16 rows meet a key, and the copies set the pace.
+// each: scores by mma.sync, a softmax of their own, then the product with V, and
+// join at the end of a unit.  mma.sync and not tcgen05: at most 16 rows meet a
+// key, and the copies set the pace.  With 16-bit values the products are
+// transposed (m16n8k16: keys x rows, then values x rows), so that groups of up to
+// 8 rows fill an instruction; fp32 takes three tf32 products (m16n8k8) per one.
 #include <algorithm>
 #include <cmath>
 
@@ -28,7 +30,7 @@ namespace {
 using namespace ppc;
 using namespace ppc_ptx;
 
-constexpr int kRows = 16;      // query rows of a unit
+constexpr int kRows = 16;      // query rows of a unit at most
 constexpr int kWarps = 4;      // that compute; one more copies
 constexpr int kThreads = kWarps * 32 + 32;
 constexpr int kGroup = 16;     // parts of a unit joined at once
@@ -47,21 +49,25 @@ struct AttnParams {
   int* counters;   // [CTAs][3], zero between calls
   float* partial;  // [CTAs][2] x (16 rows of DP sums, 16 maxima, 16 totals)
   float scale;
-  int T, B, H, G, D, page, pages, width, keep, causal;
+  int T, B, H, D, page, log_page, pages, width, keep, causal;
+  FastDiv G, by_head;  // by_head: by H
 };
 
-template <class T, int DP>
+template <class T, int DP, int RB>
 struct Shape {
   static constexpr int E = sizeof(T);
+  static constexpr int R = 8 * RB;              // query rows of a unit
   static constexpr int TK = E == 4 ? 32 : 64;   // keys per tile
+  static constexpr int LOG_TK = E == 4 ? 5 : 6;
   static constexpr int KW = TK / kWarps;        // keys per warp
   static constexpr int CH = 128 / E;            // values per 128-byte column
   static constexpr int NCH = DP / CH;
   static constexpr int TILE = TK * DP * E;      // bytes of a K or V tile
   static constexpr int CTAS = DP <= 128 ? 2 : 1;
-  static constexpr int QS = E == 4 ? kRows * (DP + 4) * 4 : 0;  // fp32 queries stay in shared memory
-  static constexpr int AS = DP + 8;             // row stride of the joining buffer: rows 8 banks apart
-  static constexpr int ACC = kRows * AS * 4;
+  static constexpr int QS = E == 4 ? R * (DP + 4) * 4 : 0;  // fp32 queries stay in shared memory
+  static constexpr int AS = DP + (E == 4 ? 8 : 4);          // row stride of the joining buffers, free of bank conflicts
+  static constexpr int NB = RB == 1 ? 2 : 1;                // joining buffers
+  static constexpr int ACC = NB * R * AS * 4;
   // as many stages as fit: with 228 KB per SM, 1 KB of it taken and 6 KB static per CTA, 190 KB are in flight (16 bits)
   static constexpr int STAGES = (233472 / CTAS - 1024 - 6144 - 1024 - ACC - QS) / (2 * TILE);
   static constexpr int SMEM = STAGES * 2 * TILE + ACC + QS + 1024;
@@ -135,6 +141,12 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// An 8 x 8 matrix of 16-bit values over the warp, two per lane, transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 template <class T>
 __device__ __forceinline__ uint32_t pack(float a, float b) {
   T v[2] = {from_f32<T>(a), from_f32<T>(b)};
@@ -143,14 +155,16 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   return r;
 }
 
-// Walks the units' tiles in their one order.  An item is a sequence, or a token where pages are selected for each
-// token; its units are (16 rows, head) pairs of kt tiles each.
+// Walks the units' tiles in their one order (whole: in runs that end with their unit).  An item is a sequence, or a token where pages are selected for each
+// token; its units are (R rows, head) pairs of kt tiles each.
 struct Walk {
-  int64_t base;  // its first tile in the order
-  int item, t0, n, len, rows, kt;
-  int64_t units;
+  int base;  // its first place in the order
+  int item, t0, n, len, rows, units;
+  int kt;    // tiles of a unit
+  int span;  // places of a unit in the order: its tiles, or whole runs of them
+  int places;
 };
-__device__ __forceinline__ void load_item(const AttnParams& p, int TK, int i, Walk& w) {
+__device__ __forceinline__ void load_item(const AttnParams& p, int TK, int R, int whole, int i, Walk& w) {
   w.item = i;
   int seen;
   if (p.sel) {
@@ -158,23 +172,25 @@ __device__ __forceinline__ void load_item(const AttnParams& p, int TK, int i, Wa
     w.t0 = i;
     w.n = 1;
     w.len = s.keys;
-    seen = min(p.keep, (s.keys + p.page - 1) / p.page) * p.page;
+    seen = min(p.keep, (s.keys + p.page - 1) >> p.log_page) << p.log_page;
   } else {
     w.t0 = p.starts ? p.starts[i] : i;
     w.n = p.starts ? p.starts[i + 1] - w.t0 : 1;
     int len = p.lens[i];
     const int most = p.width * p.page;
-    if (w.t0 < 0 || w.n < 0 || w.t0 + (int64_t)w.n > p.T || len < 0 || len > most) {
+    if (len < 0 || len > most) {
       atomicOr(p.status, PP_CACHE_BAD_LENGTH);
-      if (w.t0 < 0 || w.n < 0 || w.t0 + (int64_t)w.n > p.T) w.n = 0;
       len = min(max(len, 0), most);
     }
+    if (w.t0 < 0 || w.n < 0 || w.t0 > p.T - w.n) w.n = -1;  // ranges that do not fit: the call does nothing
     w.len = len;
     seen = len;
   }
-  w.rows = w.n * p.G;
-  w.units = (int64_t)((w.rows + kRows - 1) / kRows) * p.H;
+  w.rows = max(w.n, 0) * p.G.d;
+  w.units = (w.rows + R - 1) / R * p.H;
   w.kt = max(1, (seen + TK - 1) / TK);
+  w.span = whole ? (w.kt + whole - 1) / whole * whole : w.kt;
+  w.places = w.units * w.span;
 }
 
 // One row's attention over keys j0 .. j1 - 1 of a sequence by one warp, one key after the other.
@@ -186,9 +202,9 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) o[i] = 0.f;
   for (int j = j0; j < j1; ++j) {
-    const int id = row[j / p.page];
+    const int id = row[j >> p.log_page];
     if (id < 0 || id >= p.pages) continue;
-    const int64_t at = (((int64_t)id * p.H + h) * p.page + j % p.page) * p.D;
+    const int64_t at = (((int64_t)id * p.H + h) * p.page + (j & (p.page - 1))) * p.D;
     float x = 0.f;
     for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
 #pragma unroll
@@ -209,141 +225,194 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
   }
 }
 
-template <class T, int DP>
-__global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
+template <class T, int DP, int RB>
+__global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv) {
-  using S = Shape<T, DP>;
-  constexpr int TK = S::TK, KW = S::KW, ST = S::STAGES;
+  using S = Shape<T, DP, RB>;
+  constexpr int TK = S::TK, KW = S::KW, ST = S::STAGES, R = S::R;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* acc = reinterpret_cast<float*>(smem + ST * 2 * S::TILE);
-  [[maybe_unused]] float* qs = acc + kRows * S::AS;
+  [[maybe_unused]] float* qs = acc + S::NB * R * S::AS;
   __shared__ alignas(8) uint64_t full_bar[ST], empty_bar[ST];
   __shared__ Stage stage[ST];
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], rm[kRows], rl[kRows];
   __shared__ float wts[kRows][kJoin + 1], sums[kRows][kJoin + 1];
-  __shared__ int64_t scan[kThreads / 32];
-  __shared__ int64_t found_base;
-  __shared__ int found_item, last_flag, dead;
+  __shared__ int scan[4][kThreads / 32], last_flag, dead;
+  __shared__ Walk found;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int NI = p.sel ? p.T : p.B;
 
   if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
     dead = 0;
-    found_item = -1;
     for (int i = 0; i < ST; ++i) {
       mbar_init(su32(&full_bar[i]), 1);
       mbar_init(su32(&empty_bar[i]), kWarps);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // every thread sums a run of items; a scan of the sums places them in the one order
+  // every thread looks after a run of items
   const int per = (NI + kThreads - 1) / kThreads;
   const int i0 = min(NI, tid * per), i1 = min(NI, i0 + per);
-  int64_t mine = 0;
+  int tiles = 0, units = 0;
+  bool bad_range = false;
   Walk w;
   for (int i = i0; i < i1; ++i) {
-    load_item(p, TK, i, w);
-    mine += w.units * w.kt;
+    load_item(p, TK, R, 0, i, w);
+    tiles += w.places;
+    units += w.units;
+    bad_range = bad_range || w.n < 0;
   }
-  int64_t before = mine;
+  const int grid = gridDim.x;
+  // block-wide sums of N numbers
+  auto sums_of = [&](auto& v) {
+    constexpr int N = sizeof(v) / sizeof(int);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = __reduce_add_sync(~0u, v[i]);
+      if (lane == 0) scan[i][warp] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0;
+#pragma unroll
+      for (int j = 0; j < kThreads / 32; ++j) v[i] += scan[i][j];
+    }
+    __syncthreads();
+  };
+  int all[3] = {tiles, units, bad_range};
+  sums_of(all);
+  if (all[2]) {
+    if (tid == 0) atomicOr(p.status, PP_CACHE_BAD_LENGTH);
+    return;
+  }
+  // Equal runs; one of a single tile would spend more on joining than on its keys.  Where every unit can have CTAs of its
+  // own with runs not much longer (up to 1.4 times, which the copies of the other CTAs make up for), runs end with
+  // their unit: a CTA that changes units waits some 3 us for queries, joining and stores.
+  int run = max((all[0] + grid - 1) / grid, 2), whole = 0;
+  if (all[1] <= grid) {
+    const int longer[4] = {run, run + run / 10 + 1, run + run / 4 + 1, run + run * 2 / 5 + 2};
+    int ctas[4] = {};
+    for (int i = i0; i < i1; ++i) {
+      if (per > 1) load_item(p, TK, R, 0, i, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ctas[j] += w.units * ((w.kt + longer[j] - 1) / longer[j]);
+    }
+    sums_of(ctas);
+#pragma unroll
+    for (int j = 3; j >= 0; --j)
+      if (ctas[j] <= grid) whole = longer[j];
+    if (whole) run = whole;
+  }
+  // a scan places the items in the one order
+  int mine = 0;
+  for (int i = i0; i < i1; ++i) {
+    if (per > 1 || whole) load_item(p, TK, R, whole, i, w);
+    mine += w.places;
+  }
+  int before = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t o = __shfl_up_sync(~0u, before, d);
-    if (lane >= d) before += o;
+    const int up = __shfl_up_sync(~0u, before, d);
+    if (lane >= d) before += up;
   }
-  if (lane == 31) scan[warp] = before;
+  if (lane == 31) scan[0][warp] = before;
   __syncthreads();
-  int64_t total = 0;
+  int total = 0;
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) {
-    if (i < warp) before += scan[i];
-    total += scan[i];
+    if (i < warp) before += scan[0][i];
+    total += scan[0][i];
   }
   before -= mine;
-  // equal runs; one of a single tile would spend more on joining than on its keys
-  const int64_t run = max((total + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)2);
-  const int64_t x0 = (int64_t)blockIdx.x * run, x1 = min(total, x0 + run);
-  if (x0 >= total) return;
+  if ((int64_t)blockIdx.x * run >= total) return;
+  const int x0 = blockIdx.x * run, x1 = min(total, x0 + run);
   if (x0 >= before && x0 < before + mine) {
     for (int i = i0;; ++i) {
-      load_item(p, TK, i, w);
-      const int64_t c = w.units * w.kt;
-      if (x0 < before + c) {
-        found_item = i;
-        found_base = before;
-        break;
-      }
-      before += c;
+      if (per > 1) load_item(p, TK, R, whole, i, w);
+      if (x0 < before + w.places) break;
+      before += w.places;
     }
+    w.base = before;
+    found = w;
   }
   __syncthreads();
-  load_item(p, TK, found_item, w);
-  w.base = found_base;
-  const int BR = min(p.page, TK), pieces = TK / BR;
+  w = found;
+  const int log_br = min(p.log_page, S::LOG_TK), BR = 1 << log_br, pieces = TK >> log_br;
   const float sl = p.scale * 1.44269504f;  // softmax in powers of two
 
   // the unit at x: its rows, head and tiles up to this CTA's end
-  auto settle = [&](int64_t x) {
-    while (x - w.base >= w.units * w.kt) {
-      const int64_t b = w.base + w.units * w.kt;
-      load_item(p, TK, w.item + 1, w);
+  auto settle = [&](int x) {
+    while (x - w.base >= w.places) {
+      const int b = w.base + w.places;
+      load_item(p, TK, R, whole, w.item + 1, w);
       w.base = b;
     }
   };
 
   if (warp == kWarps) {
-    // ---- producer: lane j < pieces looks after piece j of each tile
+    // ---- producer.  Pages are looked up 32 pieces at a time, a lane each, so that the latency of the lists and tables
+    // is paid once in 32 / pieces tiles
     int s = 0;
     uint32_t ph = 1;  // an empty ring
-    for (int64_t x = x0; x < x1;) {
+    const int log_pc = S::LOG_TK - log_br;
+    for (int x = x0; x < x1;) {
       settle(x);
-      const int64_t u = (x - w.base) / w.kt;
-      const int h = (int)(u % p.H), k0 = (int)((x - w.base) % w.kt), k1 = (int)min((int64_t)w.kt, k0 + x1 - x);
+      const int u = (x - w.base) / w.span, h = p.by_head.mod(u);
+      const int k0 = x - w.base - u * w.span, next = x + min(w.span - k0, x1 - x), k1 = min(w.kt, k0 + next - x);
       const int b = p.sel ? seen_keys(w.t0, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status).b : w.item;
       const int* row = p.table + (int64_t)b * p.width;
       const int* list = p.sel ? p.sel + ((int64_t)w.t0 * p.H + h) * p.keep : nullptr;
+      int have32 = 0, y32 = 0;
       for (int k = k0; k < k1; ++k) {
-        int have = 0;
-        int64_t y = 0;
-        if (lane < pieces) {
-          const int key = k * TK + lane * BR, off = key % p.page;  // key of the sequence, or of the list's pages in a row
-          int at = key / p.page;
-          bool ok = true;
-          if (list) {
-            ok = at < p.keep;
-            at = ok ? list[at] : -1;
-            if (at >= p.width) atomicOr(p.status, PP_CACHE_BAD_PAGE);
-            ok = at >= 0 && at < p.width;
-          }
-          have = ok ? min(BR, w.len - at * p.page - off) : 0;
-          if (have > 0) {
-            const int id = row[at];
-            if (id < 0 || id >= p.pages) {
-              atomicOr(p.status, PP_CACHE_BAD_PAGE);
-              have = 0;
+        const int in32 = (k - k0) << log_pc & 31;  // the tile's first piece among the 32
+        if (in32 == 0) {
+          have32 = 0;
+          // key of the sequence, or of the list's pages in a row
+          const int64_t key = (int64_t)k * TK + lane * BR;
+          if (key < (int64_t)k1 * TK) {
+            const int off = (int)key & (p.page - 1);
+            int at = (int)(key >> p.log_page);
+            bool ok = true;
+            if (list) {
+              ok = at < p.keep;
+              at = ok ? list[at] : -1;
+              if (at >= p.width) atomicOr(p.status, PP_CACHE_BAD_PAGE);
+              ok = at >= 0 && at < p.width;
             }
-            y = ((int64_t)id * p.H + h) * p.page + off;
+            have32 = ok ? max(0, min(BR, w.len - at * p.page - off)) : 0;
+            if (have32 > 0) {
+              const int id = row[at];
+              if (id < 0 || id >= p.pages) {
+                atomicOr(p.status, PP_CACHE_BAD_PAGE);
+                have32 = 0;
+              }
+              y32 = (int)(((int64_t)id * p.H + h) * p.page) + off;
+            }
           }
-          have = max(have, 0);
         }
-        const unsigned live = __ballot_sync(~0u, have > 0), whole = __ballot_sync(~0u, have == BR);
+        const int have = __shfl_sync(~0u, have32, in32 + (lane & pieces - 1));
+        const int y = __shfl_sync(~0u, y32, in32 + (lane & pieces - 1));
+        const unsigned live = __ballot_sync(~0u, lane < pieces && have > 0);
+        const bool whole = __all_sync(~0u, have == BR);
         if (!*(volatile int*)&dead && !wait(su32(&empty_bar[s]), ph)) dead = 1;
         __syncwarp();
         const bool go = !*(volatile int*)&dead;
         if (lane < pieces) stage[s].have[lane] = have;
-        if (lane == 0) stage[s].full = __popc(whole) == pieces;
+        if (lane == 0) stage[s].full = whole;
         __syncwarp();
         if (lane == 0) mbar_arrive_expect_tx(su32(&full_bar[s]), go ? __popc(live) * 2 * BR * DP * S::E : 0);
         __syncwarp();
         const uint32_t dst = su32(smem + s * 2 * S::TILE);
-        const int boxes = pieces * S::NCH * 2;  // box i: piece i % pieces, column and pool i / pieces
-        for (int i = lane; i - lane < boxes; i += 32) {
-          const int j = i % pieces, c = i / pieces % S::NCH, v = i / pieces / S::NCH;
-          const int yy = __shfl_sync(~0u, (int)y, j);
-          if (go && i < boxes && (live >> j & 1))
-            copy_box(dst + v * S::TILE + c * TK * 128 + j * BR * 128, v ? &mv : &mk, c * S::CH, yy, su32(&full_bar[s]));
+        const int boxes = pieces * S::NCH * 2, j = lane & pieces - 1;  // box i: piece i % pieces, column and pool i / pieces
+        for (int i = lane; i < boxes; i += 32) {
+          const int c = (i >> log_pc) % S::NCH, v = (i >> log_pc) / S::NCH;
+          if (go && (live >> j & 1))
+            copy_box(dst + v * S::TILE + c * TK * 128 + j * BR * 128, v ? &mv : &mk, c * S::CH, y, su32(&full_bar[s]));
         }
         __syncwarp();
         if (++s == ST) {
@@ -351,90 +420,123 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
           ph ^= 1;
         }
       }
-      x += k1 - k0;
+      x = next;
     }
     return;
   }
 
   // ---- consumers
-  constexpr int NT = KW / 8, ND = DP / 8;
+  // A lane's sums: 16 bits, values i * 16 + g, + 8 of rows 8 rb + 2t, + 1 (o[rb][i]); fp32, rows g, g + 8 of values
+  // i * 8 + 2t, + 1 (o[0][i]).
+  constexpr int NO = S::E == 2 ? DP / 16 : DP / 8, OB = S::E == 2 ? RB : 1, NR = 2 * (S::E == 2 ? RB : 1);
   const int g = lane / 4, t = lane % 4;
+  // the r-th of the lane's NR rows
+  auto row_of = [&](int r) { return S::E == 2 ? (r >> 1) * 8 + 2 * t + (r & 1) : g + 8 * r; };
   const T* q = static_cast<const T*>(p.q);
-  const bool even = ((reinterpret_cast<uintptr_t>(q) & 3) | (p.q_ts & 1) | (p.q_hs & 1)) == 0;
+  [[maybe_unused]] const bool q16 = ((reinterpret_cast<uintptr_t>(q) & 15) | (p.q_ts & 7) | (p.q_hs & 7)) == 0;
   int s = 0;
   uint32_t ph = 0;
   bool timed_out = false;
-  for (int64_t x = x0; x < x1;) {
+  for (int x = x0; x < x1;) {
     settle(x);
-    const int64_t u = (x - w.base) / w.kt;
-    const int h = (int)(u % p.H), r0 = (int)(u / p.H) * kRows;
-    const int k0 = (int)((x - w.base) % w.kt), k1 = (int)min((int64_t)w.kt, k0 + x1 - x);
-    const int nrows = min(kRows, w.rows - r0);
+    const int u = (x - w.base) / w.span, h = p.by_head.mod(u), r0 = p.by_head.div(u) * R;
+    const int k0 = x - w.base - u * w.span, next = x + min(w.span - k0, x1 - x), k1 = min(w.kt, k0 + next - x);
+    const int nrows = min(R, w.rows - r0);
     const bool listed = p.sel != nullptr;
     // keys that a row of the unit may see
     auto limit = [&](int r) {
-      return p.causal && !listed ? min(w.len, max(0, w.len - w.n + (r0 + r) / p.G + 1)) : w.len;
+      return p.causal && !listed ? min(w.len, max(0, w.len - w.n + p.G.div(r0 + r) + 1)) : w.len;
     };
-    const int lim[2] = {limit(min(g, nrows - 1)), limit(min(g + 8, nrows - 1))};
+    int lim[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) lim[r] = limit(min(row_of(r), nrows - 1));
     const int lim_min = limit(0), lim_max = limit(nrows - 1);
     // the row's queries: token r / G of the unit's, head r % G of the group's
     auto qrow = [&](int r) {
-      return q + (w.t0 + (r0 + r) / p.G) * p.q_ts + (int64_t)(h * p.G + (r0 + r) % p.G) * p.q_hs;
+      return q + (w.t0 + p.G.div(r0 + r)) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r0 + r)) * p.q_hs;
     };
-    [[maybe_unused]] uint32_t qf[S::E == 2 ? DP / 16 : 1][4];
+    [[maybe_unused]] uint32_t qf[S::E == 2 ? RB : 1][S::E == 2 ? DP / 16 : 1][2];
     if constexpr (S::E == 2) {
+      // through the joining buffer, free here, so that each value is read once and 16 bytes at a time where they lie so
+      T* stage_q = reinterpret_cast<T*>(acc);
+      for (int i = tid; i < R * (DP / 8); i += kWarps * 32) {
+        const int r = i / (DP / 8), d = i % (DP / 8) * 8;
+        Vec<T, 8> v = {};
+        if (r < nrows && d < p.D) {
+          const T* from = qrow(r) + d;
+          if (q16) {
+            v = *reinterpret_cast<const Vec<T, 8>*>(from);
+          } else {
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int r = g + 8 * half;
-        const T* x = qrow(min(r, nrows - 1));
-#pragma unroll
-        for (int kk = 0; kk < DP / 16; ++kk)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int d = kk * 16 + e * 8 + 2 * t;
-            uint32_t v = 0;
-            if (r < nrows && d < p.D) {
-              if (even) {
-                v = *reinterpret_cast<const uint32_t*>(x + d);
-              } else {
-                T two[2] = {x[d], x[d + 1]};
-                memcpy(&v, two, 4);
-              }
-            }
-            qf[kk][half + 2 * e] = v;
+            for (int e = 0; e < 8; ++e) v.v[e] = from[e];
           }
+        }
+        *reinterpret_cast<Vec<T, 8>*>(stage_q + r * (DP + 8) + d) = v;
       }
+      group_sync<kWarps * 32>();
+      // matrices of 8 rows x 8 values, four at a time: b0, b1 of two steps
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const uint32_t at = su32(stage_q + (rb * 8 + lane % 8) * (DP + 8) + lane / 8 * 8);
+#pragma unroll
+        for (int kk = 0; kk < DP / 16; kk += 2) {
+          uint32_t f[4];
+          ldsm4(at + kk * 32, f);
+          qf[rb][kk][0] = f[0];
+          qf[rb][kk][1] = f[1];
+          qf[rb][kk + 1][0] = f[2];
+          qf[rb][kk + 1][1] = f[3];
+        }
+      }
+      group_sync<kWarps * 32>();
     } else {
       group_sync<kWarps * 32>();  // the last unit's are read
-      for (int i = tid; i < kRows * DP; i += kWarps * 32) {
+      for (int i = tid; i < R * DP; i += kWarps * 32) {
         const int r = i / DP, d = i % DP;
         qs[r * (DP + 4) + d] = r < nrows && d < p.D ? to_f32(qrow(r)[d]) : 0.f;
       }
       group_sync<kWarps * 32>();
     }
-    float o[ND][4];
+    float o[OB][NO][4];
 #pragma unroll
-    for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int rb = 0; rb < OB; ++rb)
+#pragma unroll
+      for (int i = 0; i < NO; ++i) o[rb][i][0] = o[rb][i][1] = o[rb][i][2] = o[rb][i][3] = 0.f;
+    float m[NR], l[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      m[r] = -INFINITY;
+      l[r] = 0.f;
+    }
 
     for (int k = k0; k < k1; ++k) {
       if (!*(volatile int*)&dead && !wait(su32(&full_bar[s]), ph)) dead = 1;
       __syncwarp();
       timed_out = timed_out || *(volatile int*)&dead;
       const uint32_t kt = su32(smem + s * 2 * S::TILE), vt = kt + S::TILE;
-      // ---- scores of this warp's keys
-      float sc[NT][4];
+      const Stage& sg = stage[s];
+      const bool clean = sg.full && (listed || (k + 1) * TK <= lim_min);
+      // ---- scores of this warp's keys.  16 bits: sc[rb] is keys g (0, 1) and g + 8 (2, 3) by the lane's two rows;
+      // fp32: rows g (0, 1) and g + 8 (2, 3) by keys 2t, 2t + 1
+      float sc[OB][4];
 #pragma unroll
-      for (int i = 0; i < NT; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+      for (int rb = 0; rb < OB; ++rb) sc[rb][0] = sc[rb][1] = sc[rb][2] = sc[rb][3] = 0.f;
       if constexpr (S::E == 2) {
-        const int key = warp * KW + (lane / 16) * 8 + lane % 8;
+        float odd[OB][4];  // every other step apart: two chains of products instead of one
+#pragma unroll
+        for (int rb = 0; rb < OB; ++rb) odd[rb][0] = odd[rb][1] = odd[rb][2] = odd[rb][3] = 0.f;
+        const int key = warp * KW + lane % 16;
 #pragma unroll
         for (int kk = 0; kk < DP / 16; ++kk) {
-          uint32_t b[4];
-          ldsm4(kt + kk / 4 * TK * 128 + key * 128 + ((((kk % 4) * 2 + (lane / 8 & 1)) ^ (key & 7)) << 4), b);
-          mma16<T>(sc[0], qf[kk], b[0], b[1]);
-          mma16<T>(sc[1], qf[kk], b[2], b[3]);
+          uint32_t a[4];
+          ldsm4(kt + kk / 4 * TK * 128 + key * 128 + ((((kk % 4) * 2 + lane / 16) ^ (key & 7)) << 4), a);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) mma16<T>(kk % 2 ? odd[rb] : sc[rb], a, qf[rb][kk][0], qf[rb][kk][1]);
         }
+#pragma unroll
+        for (int rb = 0; rb < OB; ++rb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[rb][e] += odd[rb][e];
       } else {
         const int key = warp * KW + g;
         const float* kp = reinterpret_cast<const float*>(smem + s * 2 * S::TILE);
@@ -450,23 +552,24 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
           mma8x3(sc[0], ah, al, row[((c ^ (key & 7)) << 2) + t], row[(((c + 1) ^ (key & 7)) << 2) + t]);
         }
       }
-      const Stage& sg = stage[s];
-      const bool clean = sg.full && (listed || (k + 1) * TK <= lim_min);
+      // entry e of sc[rb]: its row among the lane's, its key in the tile
+      auto row_in = [&](int rb, int e) { return S::E == 2 ? 2 * rb + (e & 1) : e >> 1; };
+      auto key_in = [&](int e) { return warp * KW + (S::E == 2 ? g + 8 * (e >> 1) : 2 * t + (e & 1)); };
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
+      for (int rb = 0; rb < OB; ++rb)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          sc[i][e] *= sl;
+          sc[rb][e] *= sl;
           if (!clean) {
-            const int j = warp * KW + i * 8 + 2 * t + (e & 1);
-            if (j % BR >= sg.have[j / BR] || (!listed && k * TK + j >= lim[e >> 1])) sc[i][e] = -INFINITY;
+            const int j = key_in(e);
+            if ((j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim[row_in(rb, e)])) sc[rb][e] = -INFINITY;
           }
         }
       if (!clean) {  // values that no row sees: 0 x them has to be 0
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
           const int j = warp * KW + i;
-          if (j % BR >= sg.have[j / BR] || (!listed && k * TK + j >= lim_max))
+          if ((j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim_max))
             for (int c = lane; c < S::NCH * 8; c += 32)
               *reinterpret_cast<uint4*>(smem + s * 2 * S::TILE + S::TILE + c / 8 * TK * 128 + j * 128 + c % 8 * 16) =
                   make_uint4(0, 0, 0, 0);
@@ -474,56 +577,65 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
         __syncwarp();
       }
       // ---- softmax over what this warp has seen
-      float f[2];
+      float f[NR];
+      bool moved = false;
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        float mx = fmaxf(sc[0][2 * r], sc[0][2 * r + 1]);
-        if (NT == 2) mx = fmaxf(mx, fmaxf(sc[NT - 1][2 * r], sc[NT - 1][2 * r + 1]));
-        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
-        mx = fmaxf(m[r], fmaxf(mx, __shfl_xor_sync(~0u, mx, 2)));
+      for (int r = 0; r < NR; ++r) {
+        // the row's entries of this lane, and the lanes that hold its others
+        float& s0 = S::E == 2 ? sc[r >> 1][r & 1] : sc[0][2 * r];
+        float& s1 = S::E == 2 ? sc[r >> 1][2 + (r & 1)] : sc[0][2 * r + 1];
+        float mx = fmaxf(s0, s1);
+        if constexpr (S::E == 2) {
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+        } else {
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
+        }
+        mx = fmaxf(m[r], mx);
         const float at = mx == -INFINITY ? 0.f : mx;
         f[r] = ex2(m[r] - at);
+        moved = moved || m[r] != mx;
         m[r] = mx;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          sc[i][2 * r] = ex2(sc[i][2 * r] - at);
-          sc[i][2 * r + 1] = ex2(sc[i][2 * r + 1] - at);
-          sum += sc[i][2 * r] + sc[i][2 * r + 1];
-        }
-        l[r] = l[r] * f[r] + sum;
+        s0 = ex2(s0 - at);
+        s1 = ex2(s1 - at);
+        l[r] = l[r] * f[r] + (s0 + s1);
       }
-      if (__any_sync(~0u, f[0] != 1.f || f[1] != 1.f)) {
+      if (__any_sync(~0u, moved)) {
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-          o[i][0] *= f[0];
-          o[i][1] *= f[0];
-          o[i][2] *= f[1];
-          o[i][3] *= f[1];
-        }
+        for (int rb = 0; rb < OB; ++rb)
+#pragma unroll
+          for (int i = 0; i < NO; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[rb][i][e] *= f[row_in(rb, e)];
       }
       // ---- their product with V
       if constexpr (S::E == 2) {
         // the weights as two halves of the inputs' type, so that they keep 16 bits and more (22 in f16): bound by the
         // copies, the kernel has the time, and the output's own rounding stays the largest error
-        uint32_t ph4[4], pl4[4];
+        uint32_t bh[RB][2], bl[RB][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float a = sc[i / 2][i % 2 * 2], b = sc[i / 2][i % 2 * 2 + 1];
-          ph4[i] = pack<T>(a, b);
-          T two[2];
-          memcpy(two, &ph4[i], 4);
-          pl4[i] = pack<T>(a - to_f32(two[0]), b - to_f32(two[1]));
-        }
-        const int key = warp * KW + (lane / 8 & 1) * 8 + lane % 8;
+        for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int i = 0; i < ND; i += 2) {
-          uint32_t b[4];
-          ldsm4t(vt + i / 8 * TK * 128 + key * 128 + (((i % 8 + lane / 16) ^ (key & 7)) << 4), b);
-          mma16<T>(o[i], ph4, b[0], b[1]);
-          mma16<T>(o[i + 1], ph4, b[2], b[3]);
-          mma16<T>(o[i], pl4, b[0], b[1]);
-          mma16<T>(o[i + 1], pl4, b[2], b[3]);
+          for (int i = 0; i < 2; ++i) {
+            const float a = sc[rb][2 * i], b = sc[rb][2 * i + 1];
+            const uint32_t hi = pack<T>(a, b);
+            T two[2];
+            memcpy(two, &hi, 4);
+            bh[rb][i] = transpose8(hi);  // keys x rows to rows x keys
+            bl[rb][i] = transpose8(pack<T>(a - to_f32(two[0]), b - to_f32(two[1])));
+          }
+        const int key = warp * KW + (lane / 16) * 8 + lane % 8;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) {
+          uint32_t a[4];
+          ldsm4t(vt + i / 4 * TK * 128 + key * 128 + (((i % 4 * 2 + (lane / 8 & 1)) ^ (key & 7)) << 4), a);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            mma16<T>(o[rb][i], a, bl[rb][0], bl[rb][1]);
+            mma16<T>(o[rb][i], a, bh[rb][0], bh[rb][1]);
+          }
         }
       } else {
         // columns t and t + 4 of the product's left side are keys 2t and 2t + 1: the sum does not mind
@@ -535,10 +647,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
         const float* vp = reinterpret_cast<const float*>(smem + s * 2 * S::TILE + S::TILE);
         const int key = warp * KW + 2 * t;
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
+        for (int i = 0; i < NO; ++i) {
           const float* row = vp + i / 4 * TK * 32 + key * 32;
           const int c = i % 4 * 2 + g / 4;
-          mma8x3(o[i], ah, al, row[((c ^ (key & 7)) << 2) + g % 4], row[32 + ((c ^ (key + 1 & 7)) << 2) + g % 4]);
+          mma8x3(o[0][i], ah, al, row[((c ^ (key & 7)) << 2) + g % 4], row[32 + ((c ^ (key + 1 & 7)) << 2) + g % 4]);
         }
       }
       if (!clean) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the zeros before the next copy
@@ -552,46 +664,71 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
 
     // ---- the four warps' parts into one
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      l[r] += __shfl_xor_sync(~0u, l[r], 1);
-      l[r] += __shfl_xor_sync(~0u, l[r], 2);
-      if (t == 0) {
-        wm[warp][g + 8 * r] = m[r];
-        wl[warp][g + 8 * r] = l[r];
+    for (int r = 0; r < NR; ++r) {
+      if constexpr (S::E == 2) {
+        l[r] += __shfl_xor_sync(~0u, l[r], 4);
+        l[r] += __shfl_xor_sync(~0u, l[r], 8);
+        l[r] += __shfl_xor_sync(~0u, l[r], 16);
+      } else {
+        l[r] += __shfl_xor_sync(~0u, l[r], 1);
+        l[r] += __shfl_xor_sync(~0u, l[r], 2);
+      }
+      if (S::E == 2 ? g == 0 : t == 0) {
+        wm[warp][row_of(r)] = m[r];
+        wl[warp][row_of(r)] = l[r];
       }
     }
     group_sync<kWarps * 32>();
-    float f[2];
+    float f[NR];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int row = g + 8 * r;
+    for (int r = 0; r < NR; ++r) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, wm[i][row]);
+      for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, wm[i][row_of(r)]);
       f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - mx);
-      if (warp == 0 && t == 0) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) sum += wm[i][row] == -INFINITY ? 0.f : wl[i][row] * ex2(wm[i][row] - mx);
-        rm[row] = mx;
-        rl[row] = sum;
-      }
     }
-#pragma unroll 1
-    for (int i = 0; i < kWarps; ++i) {
-      if (warp == i) {
+    if (tid < R) {
+      float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          if (g + 8 * r >= nrows) continue;
-          float* row = acc + (g + 8 * r) * S::AS + 2 * t;
+      for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, wm[i][tid]);
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            float2 v = i == 0 ? make_float2(0.f, 0.f) : *reinterpret_cast<float2*>(row + d * 8);
-            v.x += o[d][2 * r] * f[r];
-            v.y += o[d][2 * r + 1] * f[r];
-            *reinterpret_cast<float2*>(row + d * 8) = v;
+      for (int i = 0; i < kWarps; ++i) sum += wm[i][tid] == -INFINITY ? 0.f : wl[i][tid] * ex2(wm[i][tid] - mx);
+      rm[tid] = mx;
+      rl[tid] = sum;
+    }
+    // warp i adds to buffer i % NB in round i / NB
+#pragma unroll
+    for (int round = 0; round < kWarps / S::NB; ++round) {
+      if (warp / S::NB == round) {
+        float* buf = acc + warp % S::NB * R * S::AS;
+#pragma unroll
+        for (int rb = 0; rb < OB; ++rb) {
+          constexpr int C = 8;  // read together, then written: not one after the other
+#pragma unroll
+          for (int i0 = 0; i0 < NO; i0 += C) {
+            float v[C][4];
+            auto place = [&](int i, int e) {
+              return S::E == 2 ? buf + row_of(2 * rb + (e & 1)) * S::AS + i * 16 + g + 8 * (e >> 1)
+                               : buf + row_of(e >> 1) * S::AS + i * 8 + 2 * t + (e & 1);
+            };
+#pragma unroll
+            for (int i = 0; i < C && i0 + i < NO; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[i][e] = round == 0 ? 0.f : *place(i0 + i, e);
+#pragma unroll
+            for (int i = 0; i < C && i0 + i < NO; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) *place(i0 + i, e) = v[i][e] + o[rb][i0 + i][e] * f[S::E == 2 ? 2 * rb + (e & 1) : e >> 1];
           }
         }
+      }
+      group_sync<kWarps * 32>();
+    }
+    if constexpr (S::NB == 2) {
+      for (int i = tid; i < nrows * (DP / 4); i += kWarps * 32) {
+        float4* a = reinterpret_cast<float4*>(acc + i / (DP / 4) * S::AS + i % (DP / 4) * 4);
+        const float4 b = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a) + R * S::AS);
+        *a = make_float4(a->x + b.x, a->y + b.y, a->z + b.z, a->w + b.w);
       }
       group_sync<kWarps * 32>();
     }
@@ -616,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
         const float n = rl[r] > 0.f || rl[r] != rl[r] ? 1.f / rl[r] : 0.f;
         Vec<T, 4> y = {from_f32<T>(v.x * n), from_f32<T>(v.y * n), from_f32<T>(v.z * n), from_f32<T>(v.w * n)};
         T* dst = static_cast<T*>(p.out) +
-                 ((int64_t)(w.t0 + (r0 + r) / p.G) * p.H * p.G + h * p.G + (r0 + r) % p.G) * p.D + d;
+                 ((int64_t)(w.t0 + p.G.div(r0 + r)) * p.H * p.G.d + h * p.G.d + p.G.mod(r0 + r)) * p.D + d;
         if (wide) {
           *reinterpret_cast<Vec<T, 4>*>(dst) = y;
         } else {
@@ -625,11 +762,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
         }
       }
       if (p.lse && tid < nrows)
-        p.lse[(int64_t)(w.t0 + (r0 + tid) / p.G) * p.H * p.G + h * p.G + (r0 + tid) % p.G] =
+        p.lse[(int64_t)(w.t0 + p.G.div(r0 + tid)) * p.H * p.G.d + h * p.G.d + p.G.mod(r0 + tid)] =
             rl[tid] == 0.f ? -INFINITY : rm[tid] * 0.693147181f + logf(rl[tid]);
     };
-    const int64_t first = w.base + u * w.kt;  // the unit's first tile
-    const int c0 = (int)(first / run), parts = (int)((first + w.kt - 1) / run) - c0 + 1;
+    const int first = w.base + u * w.span;  // the unit's first place
+    const int c0 = first / run, parts = (first + w.span - 1) / run - c0 + 1;
     if (parts == 1) {
       rows_out();
     } else {
@@ -714,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
       }
     }
     group_sync<kWarps * 32>();  // acc is free
-    x += k1 - k0;
+    x = next;
   }
   if (timed_out) {
     if (lane == 0) atomicOr(p.status, PP_CACHE_TIMEOUT);
@@ -723,30 +860,39 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP>::CTAS)
   }
 }
 
-template <class T, int DP>
+template <class T, int DP, int RB>
 cudaError_t prepare_one() {
-  return cudaFuncSetAttribute(attn_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<T, DP>::SMEM);
+  return cudaFuncSetAttribute(attn_kernel<T, DP, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<T, DP, RB>::SMEM);
 }
 
-template <class T, int DP>
+template <class T, int DP, int RB>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
-  const int grid = std::min(sms * Shape<T, DP>::CTAS, kMaxCtas);
-  attn_kernel<T, DP><<<grid, kThreads, Shape<T, DP>::SMEM, stream>>>(p, c.mk, c.mv);
+  const int grid = std::min(sms * Shape<T, DP, RB>::CTAS, kMaxCtas);
+  attn_kernel<T, DP, RB><<<grid, kThreads, Shape<T, DP, RB>::SMEM, stream>>>(p, c.mk, c.mv);
   return cudaGetLastError();
+}
+
+// Units of 8 rows where a sequence (or, with selected pages, a token) has no more, else of 16: fp32 always of 16.
+template <class T, int DP>
+cudaError_t by_rows(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
+  if constexpr (sizeof(T) == 2) {
+    if (p.G.d <= 8 && (p.sel || !p.starts || (int64_t)p.T * p.G.d <= (int64_t)p.B * 8)) return launch<T, DP, 1>(p, c, sms, stream);
+  }
+  return launch<T, DP, 2>(p, c, sms, stream);
 }
 
 template <class T>
 cudaError_t by_head(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
-  return p.D <= 64    ? launch<T, 64>(p, c, sms, stream)
-         : p.D <= 128 ? launch<T, 128>(p, c, sms, stream)
-                      : launch<T, 256>(p, c, sms, stream);
+  return p.D <= 64    ? by_rows<T, 64>(p, c, sms, stream)
+         : p.D <= 128 ? by_rows<T, 128>(p, c, sms, stream)
+                      : by_rows<T, 256>(p, c, sms, stream);
 }
 
-template <class T>
+template <class T, int RB>
 cudaError_t prepare_type() {
-  cudaError_t e = prepare_one<T, 64>();
-  if (e == cudaSuccess) e = prepare_one<T, 128>();
-  if (e == cudaSuccess) e = prepare_one<T, 256>();
+  cudaError_t e = prepare_one<T, 64, RB>();
+  if (e == cudaSuccess) e = prepare_one<T, 128, RB>();
+  if (e == cudaSuccess) e = prepare_one<T, 256, RB>();
   return e;
 }
 
@@ -764,9 +910,11 @@ AttnSpace attn_space(int, int D, int sms) {
 
 cudaError_t attn_prepare() {
   return g_attn_once.run([](int) {
-    cudaError_t e = prepare_type<float>();
-    if (e == cudaSuccess) e = prepare_type<__half>();
-    if (e == cudaSuccess) e = prepare_type<__nv_bfloat16>();
+    cudaError_t e = prepare_type<float, 2>();
+    if (e == cudaSuccess) e = prepare_type<__half, 1>();
+    if (e == cudaSuccess) e = prepare_type<__half, 2>();
+    if (e == cudaSuccess) e = prepare_type<__nv_bfloat16, 1>();
+    if (e == cudaSuccess) e = prepare_type<__nv_bfloat16, 2>();
     return e;
   });
 }
@@ -789,8 +937,14 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
   const int sms = device_sms();
   if (sms <= 0) return PP_ERR_CUDA;
   const pp_cache& c = *cache;
-  AttnParams p = {q, q_ts, q_hs, c.k, c.v, starts, table, lens, sel, out, lse, c.status, c.counters, c.partial, scale, T, B, c.H,
-                  Hq / c.H, c.D, c.page, c.pages, width, keep, flags & PP_ATTN_CAUSAL};
+  const int G = Hq / c.H;
+  // all tiles, at most: they are counted in 32 bits
+  const int64_t units = sel ? (int64_t)T * ((G + 7) / 8) : ((int64_t)T * G + (int64_t)B * 7) / 8;
+  const int64_t deep = std::max<int64_t>(1, ((int64_t)(sel ? std::min(width, keep) : width) * c.page + tile_keys(c.dtype) - 1) / tile_keys(c.dtype));
+  if (units * c.H >= INT32_MAX / deep || (int64_t)T * G >= INT32_MAX) return PP_ERR_UNSUPPORTED;
+  AttnParams p = {q,     q_ts,   q_hs,        c.k,        c.v,     starts, table, lens, sel,  out, lse, c.status, c.counters,
+                  c.partial, scale, T, B, c.H, c.D, c.page, log2_of(c.page), c.pages, width, keep, flags & PP_ATTN_CAUSAL,
+                  FastDiv(G), FastDiv(c.H)};
   const cudaStream_t s = (cudaStream_t)stream;
   const cudaError_t e = c.dtype == PP_F32   ? by_head<float>(p, c, sms, s)
                         : c.dtype == PP_F16 ? by_head<__half>(p, c, sms, s)

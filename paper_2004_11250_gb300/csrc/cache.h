@@ -58,6 +58,24 @@ __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2hal
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Division of numbers below 2^31 by a number known on the host: n / d = (n m / 2^32 + n) / 2^shift with the round-up
+// multiplier m of Granlund and Montgomery.  A general division is tens of dependent instructions.
+struct FastDiv {
+  uint32_t m;
+  int shift, d;
+  explicit FastDiv(int by = 1) : m(0), shift(0), d(by) {
+    while ((int64_t(1) << shift) < by) ++shift;
+    m = (uint32_t)((((uint64_t(1) << shift) - (uint64_t)by) << 32) / (uint64_t)by + 1);
+  }
+  __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> shift); }
+  __device__ __forceinline__ int mod(int n) const { return n - div(n) * d; }
+};
+inline int log2_of(int n) {
+  int s = 0;
+  while ((1 << s) < n) ++s;
+  return s;
+}
+
 // V consecutive elements moved as one (up to 16 bytes).
 template <class T, int V>
 struct alignas(sizeof(T) * V) Vec {
