@@ -21,14 +21,14 @@
 #include <algorithm>
 #include <cmath>
 
-#include "cache.h"
+#include "attn.cuh"
 #include "internal.h"
-#include "tc_ptx.cuh"
 
 namespace {
 
 using namespace ppc;
 using namespace ppc_ptx;
+using namespace ppc_attn;
 
 constexpr int kRows = 16;      // query rows of a unit at most
 constexpr int kWarps = 4;      // that compute; one more copies
@@ -36,22 +36,6 @@ constexpr int kThreads = kWarps * 32 + 32;
 constexpr int kGroup = 16;     // parts of a unit joined at once
 constexpr int kMaxCtas = 512;  // kGroup^2 parts and more
 constexpr int kJoin = kMaxCtas / kGroup;
-constexpr int kPieces = 8;     // boxes down a tile at most (pages of 8)
-
-struct AttnParams {
-  const void* q;
-  int64_t q_ts, q_hs;
-  const void *k, *v;
-  const int *starts, *table, *lens, *sel;
-  void* out;
-  float* lse;
-  int* status;
-  int* counters;   // [CTAs][3], zero between calls
-  float* partial;  // [CTAs][2] x (16 rows of DP sums, 16 maxima, 16 totals)
-  float scale;
-  int T, B, H, D, page, log_page, pages, width, keep, causal;
-  FastDiv G, by_head;  // by_head: by H
-};
 
 template <class T, int DP, int RB>
 struct Shape {
@@ -64,7 +48,8 @@ struct Shape {
   static constexpr int NCH = DP / CH;
   static constexpr int TILE = TK * DP * E;      // bytes of a K or V tile
   static constexpr int CTAS = DP <= 128 ? 2 : 1;
-  static constexpr int QS = E == 4 ? R * (DP + 4) * 4 : 0;  // fp32 queries stay in shared memory
+  static constexpr int QW = DP + 4;             // row stride of fp32 queries, which stay in shared memory as two tf32 parts
+  static constexpr int QS = E == 4 ? R * QW * 8 : 0;
   static constexpr int AS = DP + (E == 4 ? 8 : 4);          // row stride of the joining buffers, free of bank conflicts
   static constexpr int NB = RB == 1 ? 2 : 1;                // joining buffers
   static constexpr int ACC = NB * R * AS * 4;
@@ -78,19 +63,6 @@ struct Stage {          // what the producer says of a tile
   int have[kPieces];    // keys of each piece that the call may use
   int full;             // all of them
 };
-
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
-  for (long i = 0; i < PP_WAIT_POLLS; ++i)
-    if (mbar_try(bar, parity)) return true;
-  return false;
-}
-
-__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(m), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
 
 __device__ __forceinline__ void ldsm4(uint32_t a, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -121,25 +93,22 @@ __device__ __forceinline__ void mma8(float (&c)[4], const uint32_t (&a)[4], uint
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// v = hi + lo with hi exact in tf32; the dropped part of lo is below 2^-21 |v|
+// v = hi + lo in tf32, both rounded to nearest: what is left is below 2^-23 |v| and of either sign (cut off instead, all
+// products would be too small, and sums of them off by five times as much)
 __device__ __forceinline__ void split_tf32(float v, uint32_t& hi, uint32_t& lo) {
-  const float h = tf32_hi(v);
-  hi = __float_as_uint(h);
-  lo = __float_as_uint(v - h);
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(v));
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(v - __uint_as_float(hi)));
 }
-// c += a b with fp32 operands as three tf32 products (lo lo, below 2^-22, is left out)
+// a b with fp32 operands as three tf32 products (lo lo, below 2^-22, is left out).  They start from 0 and are added to a
+// running sum outside: a tensor-core sum is cut off at each product, always towards 0, and over many of them that shows.
 __device__ __forceinline__ void mma8x3(float (&c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], float b0, float b1) {
   uint32_t h0, l0, h1, l1;
   split_tf32(b0, h0, l0);
   split_tf32(b1, h1, l1);
+  c[0] = c[1] = c[2] = c[3] = 0.f;
   mma8(c, al, h0, h1);
   mma8(c, ah, l0, l1);
   mma8(c, ah, h0, h1);
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 // An 8 x 8 matrix of 16-bit values over the warp, two per lane, transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
@@ -147,14 +116,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-template <class T>
-__device__ __forceinline__ uint32_t pack(float a, float b) {
-  T v[2] = {from_f32<T>(a), from_f32<T>(b)};
-  uint32_t r;
-  memcpy(&r, v, 4);
-  return r;
-}
-
 // Walks the units' tiles in their one order (whole: in runs that end with their unit).  An item is a sequence, or a token where pages are selected for each
 // token; its units are (R rows, head) pairs of kt tiles each.
 struct Walk {
@@ -234,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* acc = reinterpret_cast<float*>(smem + ST * 2 * S::TILE);
-  [[maybe_unused]] float* qs = acc + S::NB * R * S::AS;
+  [[maybe_unused]] uint2* qs = reinterpret_cast<uint2*>(acc + S::NB * R * S::AS);
   __shared__ alignas(8) uint64_t full_bar[ST], empty_bar[ST];
   __shared__ Stage stage[ST];
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], rm[kRows], rl[kRows];
@@ -493,7 +454,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       group_sync<kWarps * 32>();  // the last unit's are read
       for (int i = tid; i < R * DP; i += kWarps * 32) {
         const int r = i / DP, d = i % DP;
-        qs[r * (DP + 4) + d] = r < nrows && d < p.D ? to_f32(qrow(r)[d]) : 0.f;
+        uint2 v;
+        split_tf32(r < nrows && d < p.D ? to_f32(qrow(r)[d]) : 0.f, v.x, v.y);
+        qs[r * S::QW + d] = v;
       }
       group_sync<kWarps * 32>();
     }
@@ -544,12 +507,18 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
         for (int kk = 0; kk < DP / 8; ++kk) {
           const float* row = kp + kk / 4 * TK * 32 + key * 32;
           const int c = kk % 4 * 2;
-          uint32_t ah[4], al[4];
-          split_tf32(qs[g * (DP + 4) + kk * 8 + t], ah[0], al[0]);
-          split_tf32(qs[(g + 8) * (DP + 4) + kk * 8 + t], ah[1], al[1]);
-          split_tf32(qs[g * (DP + 4) + kk * 8 + t + 4], ah[2], al[2]);
-          split_tf32(qs[(g + 8) * (DP + 4) + kk * 8 + t + 4], ah[3], al[3]);
-          mma8x3(sc[0], ah, al, row[((c ^ (key & 7)) << 2) + t], row[(((c + 1) ^ (key & 7)) << 2) + t]);
+          const uint2* qa = qs + g * S::QW + kk * 8 + t;
+          const uint2 q0 = qa[0], q2 = qa[4];
+          uint2 q1 = make_uint2(0, 0), q3 = q1;
+          if (nrows > 8) {
+            q1 = qa[8 * S::QW];
+            q3 = qa[8 * S::QW + 4];
+          }
+          const uint32_t ah[4] = {q0.x, q1.x, q2.x, q3.x}, al[4] = {q0.y, q1.y, q2.y, q3.y};
+          float part[4];
+          mma8x3(part, ah, al, row[((c ^ (key & 7)) << 2) + t], row[(((c + 1) ^ (key & 7)) << 2) + t]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[0][e] += part[e];
         }
       }
       // entry e of sc[rb]: its row among the lane's, its key in the tile
@@ -650,7 +619,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
         for (int i = 0; i < NO; ++i) {
           const float* row = vp + i / 4 * TK * 32 + key * 32;
           const int c = i % 4 * 2 + g / 4;
-          mma8x3(o[0][i], ah, al, row[((c ^ (key & 7)) << 2) + g % 4], row[32 + ((c ^ (key + 1 & 7)) << 2) + g % 4]);
+          float part[4];
+          mma8x3(part, ah, al, row[((c ^ (key & 7)) << 2) + g % 4], row[32 + ((c ^ (key + 1 & 7)) << 2) + g % 4]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[0][i][e] += part[e];
         }
       }
       if (!clean) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the zeros before the next copy
@@ -910,7 +882,8 @@ AttnSpace attn_space(int, int D, int sms) {
 
 cudaError_t attn_prepare() {
   return g_attn_once.run([](int) {
-    cudaError_t e = prepare_type<float, 2>();
+    cudaError_t e = tile_prepare();
+    if (e == cudaSuccess) e = prepare_type<float, 2>();
     if (e == cudaSuccess) e = prepare_type<__half, 1>();
     if (e == cudaSuccess) e = prepare_type<__half, 2>();
     if (e == cudaSuccess) e = prepare_type<__nv_bfloat16, 1>();
@@ -946,7 +919,8 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
                   c.partial, scale, T, B, c.H, c.D, c.page, log2_of(c.page), c.pages, width, keep, flags & PP_ATTN_CAUSAL,
                   FastDiv(G), FastDiv(c.H)};
   const cudaStream_t s = (cudaStream_t)stream;
-  const cudaError_t e = c.dtype == PP_F32   ? by_head<float>(p, c, sms, s)
+  const cudaError_t e = tile_applicable(p, c.dtype, sms) ? tile_launch(p, c, s)
+                        : c.dtype == PP_F32 ? by_head<float>(p, c, sms, s)
                         : c.dtype == PP_F16 ? by_head<__half>(p, c, sms, s)
                                             : by_head<__nv_bfloat16>(p, c, sms, s);
   return e == cudaSuccess ? PP_OK : PP_ERR_CUDA;

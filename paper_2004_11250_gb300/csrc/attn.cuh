@@ -1,0 +1,62 @@
+// What the two attention kernels share: a call's parameters, bounded waits, box copies.
+#pragma once
+
+#include <cmath>
+
+#include "cache.h"
+#include "tc_ptx.cuh"
+
+namespace ppc_attn {
+
+using namespace ppc;
+using namespace ppc_ptx;
+
+constexpr int kPieces = 8;  // boxes down a tile at most (pages of 8)
+
+struct AttnParams {
+  const void* q;
+  int64_t q_ts, q_hs;
+  const void *k, *v;
+  const int *starts, *table, *lens, *sel;
+  void* out;
+  float* lse;
+  int* status;
+  int* counters;   // [CTAs][3], zero between calls
+  float* partial;  // [CTAs][2] x (16 rows of DP sums, 16 maxima, 16 totals)
+  float scale;
+  int T, B, H, D, page, log_page, pages, width, keep, causal;
+  FastDiv G, by_head;  // by_head: by H
+};
+
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+  for (long i = 0; i < PP_WAIT_POLLS; ++i)
+    if (mbar_try(bar, parity)) return true;
+  return false;
+}
+
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(m), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <class T>
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+  T v[2] = {from_f32<T>(a), from_f32<T>(b)};
+  uint32_t r;
+  memcpy(&r, v, 4);
+  return r;
+}
+
+// attn_tile.cu: tiles of 128 query rows on the tensor cores, for 16-bit types and heads of up to 128.
+bool tile_applicable(const AttnParams& p, int dtype, int sms);
+cudaError_t tile_prepare();
+cudaError_t tile_launch(const AttnParams& p, const pp_cache& c, cudaStream_t stream);
+
+}  // namespace ppc_attn

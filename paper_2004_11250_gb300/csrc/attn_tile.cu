@@ -1,0 +1,603 @@
+// Attention for many query tokens: tiles of 128 query rows on the tensor cores
+// (tcgen05), for 16-bit types and heads of up to 128 values.
+//
+// A CTA has the rows of one cache head: the heads of its group for as many
+// consecutive tokens as give up to 128 rows, one row per TMEM lane.  Keys come in
+// blocks of 64 (whole pages, or pieces of one).  Per block
+//   S = Q K^T       128 x 64, operands in shared memory, sums in TMEM
+//   P = 2^(S - m)   a thread per row: no exchange between lanes
+//   O += P V        P from TMEM (over S's own columns), V from shared memory
+// The score product of a block runs while the softmax of the one before it does
+// (two S buffers), and two CTAs share an SM, so one's softmax hides behind the
+// other's products.  m is only raised, and O rescaled in TMEM, when a row's
+// maximum has grown by more than 2^8: the weights then stay below 2^8, and their
+// sums are what they would be, since both are divided in the end.
+//
+// Where pages are selected for each token, the tile reads the union of its tokens'
+// pages once, and a bit per (page, token) says which rows use it: neighbouring
+// tokens select mostly the same pages, and a gather per token would read each of
+// them through L2 again (2048 tokens over 512 pages: 17 GB).
+#include <algorithm>
+#include <type_traits>
+
+#include "attn.cuh"
+#include "internal.h"
+
+namespace {
+
+using namespace ppc_attn;
+
+constexpr int kRowsT = 128;            // query rows of a tile
+constexpr int kSoft = 128;             // threads of the softmax; then a copying and a multiplying warp
+constexpr int kThreadsT = kSoft + 64;
+constexpr int kKeys = 64;              // keys per block
+constexpr int kStages = 2;             // of K and of V
+constexpr int kMaskWords = 2048;       // token bits of the pages in one window
+constexpr float kGrow = 8.f;           // log2 of how far a row's scores may pass its m
+
+template <int DP>
+struct TileShape {
+  static constexpr int Q = kRowsT * DP * 2, KV = kKeys * DP * 2;
+  static constexpr int SMEM = Q + 2 * kStages * KV + kMaskWords * 4 + kMaskWords * 2 + 1024;
+  static constexpr int COLS = 256;     // TMEM: O at 0 .. DP - 1, S at 128 and 192
+};
+
+struct Block {          // what the copying warp says of a block
+  int have[kPieces];
+  int full;
+};
+
+// Shared-memory descriptors of 128-byte swizzled operands.  K-major (Q, K): rows of 128 bytes, groups of 8 rows 1024
+// bytes apart.  MN-major (V): 128 bytes of values per key, groups of 8 keys 1024 bytes apart, the next 64 values `lbo`
+// bytes on.
+__device__ __forceinline__ uint64_t desc_128(uint32_t addr, uint32_t lbo) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+template <class T>
+__host__ __device__ constexpr uint32_t idesc(int m, int n, bool b_mn) {
+  const uint32_t f = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  return (1u << 4) | (f << 7) | (f << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+// the left operand in TMEM
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a),
+      "l"(b), "r"(id), "r"(acc));
+}
+__device__ __forceinline__ void tm_ld32(uint32_t a, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(a));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tm_st32(uint32_t a, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+      "r"(r[31]), "r"(a)
+      : "memory");
+}
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// One row's attention by one warp, a key after the other: of a row whose product met a value that is not finite at a key
+// that another row of the tile sees and it does not.
+template <class T, int DP>
+__device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int* table, const int* list, int h, int keys,
+                                      float sl, T* out, float* lse) {
+  const int lane = threadIdx.x % 32, P = (keys + p.page - 1) >> p.log_page;
+  float o[DP / 32], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) o[i] = 0.f;
+  for (int e = 0; e < (list ? min(p.keep, P) : P); ++e) {
+    const int w = list ? list[e] : e;
+    if (w < 0 || w >= P) continue;
+    const int id = table[w];
+    if (id < 0 || id >= p.pages) continue;
+    for (int j = 0; j < min(p.page, keys - w * p.page); ++j) {
+      const int64_t at = (((int64_t)id * p.H + h) * p.page + j) * p.D;
+      float x = 0.f;
+      for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+      x *= sl;
+      const float mx = fmaxf(m, x), ref = mx == -INFINITY ? 0.f : mx, f = ex2(m - ref), c = ex2(x - ref);
+      m = mx;
+      l = l * f + c;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+        if (lane + 32 * i < p.D) o[i] = o[i] * f + c * to_f32(static_cast<const T*>(p.v)[at + lane + 32 * i]);
+    }
+  }
+  const float n = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+    if (lane + 32 * i < p.D) out[lane + 32 * i] = from_f32<T>(o[i] * n);
+  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
+}
+
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreadsT, 2)
+    attn_tile_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
+                     const __grid_constant__ CUtensorMap mv) {
+  using S = TileShape<DP>;
+  constexpr int CHUNK_Q = kRowsT * 128, CHUNK_KV = kKeys * 128;  // bytes of 64 values of every row
+  extern __shared__ unsigned char raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* kbuf = smem + S::Q;
+  unsigned char* vbuf = kbuf + kStages * S::KV;
+  uint32_t* masks = reinterpret_cast<uint32_t*>(vbuf + kStages * S::KV);
+  uint16_t* list = reinterpret_cast<uint16_t*>(masks + kMaskWords);
+  __shared__ alignas(8) uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], s_full[2],
+      p_full[2], pv_done;
+  __shared__ Block info[kStages];
+  __shared__ uint32_t tmem_s;
+  __shared__ int scan[kThreadsT / 32], tile_of[4], found_n, dead;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+
+  // ---- which tile: those of a sequence's last tokens, which see the most keys, come first
+  const int TT = kRowsT / p.G.d;  // tokens per tile
+  const int h = blockIdx.x % p.H, order = blockIdx.x / p.H;
+  if (tid == 0) {
+    found_n = 0;
+    dead = 0;
+    tile_of[0] = -1;
+  }
+  __syncthreads();
+  const int per = (p.B + kThreadsT - 1) / kThreadsT, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+  int mine = 0;
+  bool bad = false;
+  for (int b = b0; b < b1; ++b) {
+    const int s0 = p.starts ? p.starts[b] : b, n = p.starts ? p.starts[b + 1] - s0 : 1;
+    bad = bad || s0 < 0 || n < 0 || s0 > p.T - n;
+    mine += (max(n, 0) + TT - 1) / TT;
+  }
+  int before = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int up = __shfl_up_sync(~0u, before, d);
+    if (lane >= d) before += up;
+  }
+  if (lane == 31) scan[warp] = before;
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) atomicOr(p.status, PP_CACHE_BAD_LENGTH);
+    return;
+  }
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < kThreadsT / 32; ++i) {
+    if (i < warp) before += scan[i];
+    total += scan[i];
+  }
+  before -= mine;
+  if (order >= total) return;
+  const int want = total - 1 - order;
+  if (want >= before && want < before + mine) {
+    for (int b = b0;; ++b) {
+      const int s0 = p.starts ? p.starts[b] : b, n = p.starts ? p.starts[b + 1] - s0 : 1, c = (n + TT - 1) / TT;
+      if (want < before + c) {
+        tile_of[0] = b;
+        tile_of[1] = s0;
+        tile_of[2] = n;
+        tile_of[3] = (want - before) * TT;
+        break;
+      }
+      before += c;
+    }
+  }
+  __syncthreads();
+  const int b = tile_of[0], t0 = tile_of[1] + tile_of[3], nt = min(TT, tile_of[2] - tile_of[3]), rows = nt * p.G.d;
+  int len = p.lens[b];
+  const int most = p.width * p.page;
+  if (len < 0 || len > most) {
+    if (tid == 0) atomicOr(p.status, PP_CACHE_BAD_LENGTH);
+    len = min(max(len, 0), most);
+  }
+  // keys that token i of the tile sees
+  auto limit = [&](int i) { return p.causal ? min(len, max(0, len - tile_of[2] + tile_of[3] + i + 1)) : len; };
+  const int lim_max = limit(nt - 1), P = (lim_max + p.page - 1) >> p.log_page;
+  const int* table = p.table + (int64_t)b * p.width;
+  const int log_br = min(p.log_page, 6), BR = 1 << log_br, log_pc = 6 - log_br, pieces = 1 << log_pc;
+  const int log_pp = p.log_page - log_br;  // pieces per page
+  const float sl = p.scale * 1.44269504f;
+
+  // ---- set up
+  if (warp == 5) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&tmem_s)), "n"(S::COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
+    mbar_init(su32(&q_full), kSoft);
+    mbar_init(su32(&pv_done), 1);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(su32(&k_full[i]), 1);
+      mbar_init(su32(&k_empty[i]), 1);
+      mbar_init(su32(&v_full[i]), 1);
+      mbar_init(su32(&v_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(su32(&s_full[i]), 1);
+      mbar_init(su32(&p_full[i]), kSoft);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tm_fence_before();
+  __syncthreads();
+  tm_fence_after();
+  const uint32_t tmem = tmem_s;
+  // a bounded wait; after one gave up none waits any more
+  auto hold = [&](uint64_t* bar, uint32_t parity) {
+    if (!*(volatile int*)&dead && !wait(su32(bar), parity)) *(volatile int*)&dead = 1;
+  };
+
+  const T* q = static_cast<const T*>(p.q);
+  if (warp < 4) {  // the queries, swizzled as a copy would
+    const bool q16 = ((reinterpret_cast<uintptr_t>(q) & 15) | (p.q_ts & 7) | (p.q_hs & 7)) == 0;
+    for (int i = tid; i < kRowsT * (DP / 8); i += kSoft) {
+      const int r = i / (DP / 8), c = i % (DP / 8);
+      Vec<T, 8> v = {};
+      if (r < rows && c * 8 < p.D) {
+        const T* from = q + (t0 + p.G.div(r)) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs + c * 8;
+        if (q16) {
+          v = *reinterpret_cast<const Vec<T, 8>*>(from);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v.v[e] = from[e];
+        }
+      }
+      *reinterpret_cast<Vec<T, 8>*>(smem + c / 8 * CHUNK_Q + r * 128 + ((c % 8 ^ (r & 7)) << 4)) = v;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    mbar_arrive(su32(&q_full));
+  }
+
+  // softmax state of the thread's row
+  const int tok = min(p.G.div(tid), nt - 1);
+  const bool live_row = tid < rows;
+  const int lim = warp < 4 ? limit(tok) : 0;
+  float m = -INFINITY, l = 0.f;
+  const uint32_t row_tm = tmem + ((uint32_t)(warp * 32) << 16);
+
+  const int words = (TT + 31) / 32, window = p.sel ? kMaskWords / words : INT32_MAX;
+  int done = 0;  // blocks before this window
+  for (int w0 = 0; w0 < P; w0 = p.sel ? w0 + window : P) {
+    int npieces = (lim_max + BR - 1) >> log_br;  // of the window: all, or those of the listed pages
+    if (p.sel) {
+      const int wn = min(window, P - w0);
+      __syncthreads();
+      for (int i = tid; i < wn * words; i += kThreadsT) masks[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < nt * p.keep; i += kThreadsT) {
+        const int tk = i / p.keep, e = i - tk * p.keep, Pt = (limit(tk) + p.page - 1) >> p.log_page;
+        if (e >= Pt) continue;
+        const int w = p.sel[((int64_t)(t0 + tk) * p.H + h) * p.keep + e];
+        if (w >= p.width) atomicOr(p.status, PP_CACHE_BAD_PAGE);
+        if (w >= w0 && w < w0 + wn && w < Pt) atomicOr(&masks[(w - w0) * words + tk / 32], 1u << (tk % 32));
+      }
+      __syncthreads();
+      // the pages that some token uses, in order
+      const int each = (wn + kThreadsT - 1) / kThreadsT, a0 = min(wn, tid * each), a1 = min(wn, a0 + each);
+      int used = 0;
+      auto any = [&](int w) {
+        uint32_t v = 0;
+        for (int i = 0; i < words; ++i) v |= masks[w * words + i];
+        return v != 0;
+      };
+      for (int w = a0; w < a1; ++w) used += any(w);
+      int at = used;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(~0u, at, d);
+        if (lane >= d) at += up;
+      }
+      if (lane == 31) scan[warp] = at;
+      __syncthreads();
+      int sum = 0;
+#pragma unroll
+      for (int i = 0; i < kThreadsT / 32; ++i) {
+        if (i < warp) at += scan[i];
+        sum += scan[i];
+      }
+      at -= used;
+      for (int w = a0; w < a1; ++w)
+        if (any(w)) list[at++] = (uint16_t)w;
+      __syncthreads();
+      npieces = sum << log_pp;
+    }
+    const int n = (npieces + pieces - 1) >> log_pc;  // blocks of the window
+    // piece i: its first key, -1 beyond the last
+    auto key_of = [&](int i) {
+      if (i >= npieces) return -1;
+      return p.sel ? ((w0 + list[i >> log_pp]) << p.log_page) + ((i & (1 << log_pp) - 1) << log_br) : i << log_br;
+    };
+
+    if (warp == 4) {
+      // ---- copies.  Pages are looked up 32 pieces at a time, a lane each
+      int have32 = 0, y32 = 0;
+      for (int k = 0; k < n; ++k) {
+        const int g = done + k, st = g % kStages;
+        const uint32_t ph = (g / kStages + 1) & 1;
+        const int in32 = k << log_pc & 31;
+        if (in32 == 0) {
+          const int key = key_of((k << log_pc) + lane);
+          have32 = key < 0 ? 0 : max(0, min(BR, lim_max - key));
+          if (have32 > 0) {
+            const int id = table[key >> p.log_page];
+            if (id < 0 || id >= p.pages) {
+              atomicOr(p.status, PP_CACHE_BAD_PAGE);
+              have32 = 0;
+            }
+            y32 = (int)(((int64_t)id * p.H + h) * p.page) + (key & (p.page - 1));
+          }
+        }
+        const int j = lane & pieces - 1, have = __shfl_sync(~0u, have32, in32 + j), y = __shfl_sync(~0u, y32, in32 + j);
+        const unsigned live = __ballot_sync(~0u, lane < pieces && have > 0);
+        const bool whole = __all_sync(~0u, have == BR);
+        const int bytes = __popc(live) * BR * DP * 2, boxes = pieces * (DP / 64), c = lane >> log_pc;
+        hold(&k_empty[st], ph);
+        __syncwarp();
+        bool go = !*(volatile int*)&dead;
+        if (lane == 0) mbar_arrive_expect_tx(su32(&k_full[st]), go ? bytes : 0);
+        __syncwarp();
+        if (go && lane < boxes && (live >> j & 1))
+          copy_box(su32(kbuf + st * S::KV) + c * CHUNK_KV + j * BR * 128, &mk, c * 64, y, su32(&k_full[st]));
+        hold(&v_empty[st], ph);
+        __syncwarp();
+        go = !*(volatile int*)&dead;
+        if (lane < pieces) info[st].have[lane] = have;
+        if (lane == 0) info[st].full = whole;
+        __syncwarp();
+        if (lane == 0) mbar_arrive_expect_tx(su32(&v_full[st]), go ? bytes : 0);
+        __syncwarp();
+        if (go && lane < boxes && (live >> j & 1))
+          copy_box(su32(vbuf + st * S::KV) + c * CHUNK_KV + j * BR * 128, &mv, c * 64, y, su32(&v_full[st]));
+      }
+    } else if (warp == 5) {
+      // ---- products
+      if (lane == 0) {
+        auto scores = [&](int k) {
+          const int g = done + k, st = g % kStages;
+          hold(&k_full[st], g / kStages & 1);
+          tm_fence_after();
+          const uint32_t a = su32(smem), kb = su32(kbuf + st * S::KV);
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk)
+            mma_f16(tmem + 128 + (g & 1) * 64, desc_128(a + kk / 4 * CHUNK_Q + kk % 4 * 32, 16),
+                    desc_128(kb + kk / 4 * CHUNK_KV + kk % 4 * 32, 16), idesc<T>(kRowsT, kKeys, false), kk > 0);
+          mma_commit(su32(&k_empty[st]));
+          mma_commit(su32(&s_full[g & 1]));
+        };
+        if (n > 0) {
+          if (done == 0) hold(&q_full, 0);
+          scores(0);
+        }
+        for (int k = 0; k < n; ++k) {
+          const int g = done + k, st = g % kStages;
+          if (k + 1 < n) scores(k + 1);
+          hold(&p_full[g & 1], g >> 1 & 1);
+          hold(&v_full[st], g / kStages & 1);
+          tm_fence_after();
+          const uint32_t vb = su32(vbuf + st * S::KV);
+#pragma unroll
+          for (int kk = 0; kk < kKeys / 16; ++kk)
+            mma_f16_ts(tmem, tmem + 128 + (g & 1) * 64 + kk * 8, desc_128(vb + kk * 2048, CHUNK_KV), idesc<T>(kRowsT, DP, true),
+                       g > 0 || kk > 0);
+          mma_commit(su32(&v_empty[st]));
+          mma_commit(su32(&pv_done));
+        }
+      }
+      __syncwarp();
+    } else {
+      // ---- softmax, a thread per row
+      for (int k = 0; k < n; ++k) {
+        const int g = done + k, st = g % kStages;
+        hold(&v_full[st], g / kStages & 1);  // what the copying warp says, too
+        hold(&s_full[g & 1], g >> 1 & 1);
+        __syncwarp();
+        tm_fence_after();
+        const uint32_t tm = row_tm + 128 + (g & 1) * 64;
+        // which of the block's keys the row sees, a bit each
+        uint64_t see = 0;
+        const Block& bl = info[st];
+#pragma unroll 1
+        for (int j = 0; j < pieces; ++j) {
+          const int i = (k << log_pc) + j, key = key_of(i);
+          bool on = live_row && key >= 0;
+          if (on && p.sel) on = masks[(i >> log_pp < (npieces >> log_pp) ? list[i >> log_pp] : 0) * words + tok / 32] >> (tok % 32) & 1;
+          const int c = on ? min(bl.have[j], lim - key) : 0;
+          if (c > 0) see |= (c >= 64 ? ~0ull : (1ull << c) - 1) << (j << log_br);
+        }
+        const bool all = __all_sync(~0u, see == ~0ull), none = __all_sync(~0u, see == 0);
+        uint32_t w[32];
+        bool waited = false;
+        if (none) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) w[i] = 0;
+        } else {
+          float x[64];
+          tm_ld32(tm, reinterpret_cast<float(&)[32]>(x[0]));
+          tm_ld32(tm + 32, reinterpret_cast<float(&)[32]>(x[32]));
+          tm_wait_ld();
+          // where every key is seen the scale goes into the exponent's product, else in first, before what is not seen
+          float mul = sl;
+          if (!all || sl <= 0.f) {
+            mul = 1.f;
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              x[i] = (i < 32 ? (uint32_t)see : (uint32_t)(see >> 32)) >> (i & 31) & 1 ? x[i] * sl : -INFINITY;
+          }
+          float mx = x[0];
+#pragma unroll
+          for (int i = 1; i < 64; ++i) mx = fmaxf(mx, x[i]);
+          mx *= mul;
+          const bool grow = mx > m + kGrow;  // from -infinity, too
+          if (__any_sync(~0u, grow)) {
+            const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
+            m = to;
+            l *= f;
+            if (g > 0) {  // the sums so far, in TMEM
+              hold(&pv_done, (g - 1) & 1);
+              waited = true;
+              __syncwarp();
+              tm_fence_after();
+#pragma unroll
+              for (int c = 0; c < DP; c += 32) {
+                float o[32];
+                tm_ld32(row_tm + c, o);
+                tm_wait_ld();
+                uint32_t r[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * f);
+                tm_st32(row_tm + c, r);
+              }
+              tm_wait_st();
+            }
+          }
+          const float at = m == -INFINITY ? 0.f : m;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float a = ex2(fmaf(x[2 * i], mul, -at)), c = ex2(fmaf(x[2 * i + 1], mul, -at));
+            sum += a + c;
+            w[i] = pack<T>(a, c);
+          }
+          l += sum;
+        }
+        tm_st32(tm, w);
+        if (!bl.full) {  // values that no row sees: 0 x them has to be 0
+          for (int i = tid; i < kKeys * (DP / 8); i += kSoft) {
+            const int key = i / (DP / 8), c = i % (DP / 8);
+            if ((key & BR - 1) >= bl.have[key >> log_br])
+              *reinterpret_cast<uint4*>(vbuf + st * S::KV + c / 8 * CHUNK_KV + key * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        tm_wait_st();
+        // each block's products with V are waited for, and in order, so that a parity names one of two phases; those of the
+        // block before are done by now
+        if (g > 0 && !waited) hold(&pv_done, (g - 1) & 1);
+        tm_fence_before();
+        mbar_arrive(su32(&p_full[g & 1]));
+      }
+    }
+    done += n;
+  }
+
+  // ---- out
+  if (warp < 4) {
+    if (done > 0) hold(&pv_done, (done - 1) & 1);
+    __syncwarp();
+    tm_fence_after();
+    const int64_t cell = (int64_t)(t0 + p.G.div(live_row ? tid : 0)) * p.H * p.G.d + h * p.G.d + p.G.mod(live_row ? tid : 0);
+    T* dst = static_cast<T*>(p.out) + cell * p.D;
+    const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 15) == 0;
+    const float scale = l == 0.f ? 0.f : 1.f / l;
+    bool odd = false;
+#pragma unroll
+    for (int c = 0; c < DP; c += 32) {
+      float o[32];
+      if (done > 0) {
+        tm_ld32(row_tm + c, o);
+        tm_wait_ld();
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        if (c + i >= p.D || !live_row) continue;
+        Vec<T, 8> y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          odd = odd || !isfinite(o[i + e]);
+          y.v[e] = from_f32<T>(o[i + e] * scale);
+        }
+        if (wide) {
+          *reinterpret_cast<Vec<T, 8>*>(dst + c + i) = y;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dst[c + i + e] = y.v[e];
+        }
+      }
+    }
+    if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
+    unsigned again = __ballot_sync(~0u, odd && live_row && (p.sel || p.causal));
+    while (again) {
+      const int r = warp * 32 + __ffs(again) - 1, tk = p.G.div(r);
+      again &= again - 1;
+      const int64_t at = (int64_t)(t0 + tk) * p.H * p.G.d + h * p.G.d + p.G.mod(r);
+      redo_row<T, DP>(p, q + (t0 + tk) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs, table,
+                      p.sel ? p.sel + ((int64_t)(t0 + tk) * p.H + h) * p.keep : nullptr, h, limit(tk), sl,
+                      static_cast<T*>(p.out) + at * p.D, p.lse ? p.lse + at : nullptr);
+    }
+    tm_fence_before();
+  }
+  __syncthreads();
+  if (dead && tid == 0) {
+    atomicOr(p.status, PP_CACHE_TIMEOUT);
+    // copies and products still in flight end before the CTA does
+    for (int i = 0; i < kStages; ++i)
+      for (uint32_t ph = 0; ph < 2; ++ph) wait(su32(&k_full[i]), ph), wait(su32(&v_full[i]), ph);
+    for (uint32_t ph = 0; ph < 2; ++ph) wait(su32(&pv_done), ph);
+  }
+  if (warp == 5) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS));
+  }
+}
+
+template <class T, int DP>
+cudaError_t prepare_one() {
+  return cudaFuncSetAttribute(attn_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
+}
+
+template <class T>
+cudaError_t launch(const AttnParams& p, const pp_cache& c, int64_t grid, cudaStream_t stream) {
+  if (p.D <= 64)
+    attn_tile_kernel<T, 64><<<(unsigned)grid, kThreadsT, TileShape<64>::SMEM, stream>>>(p, c.mk, c.mv);
+  else
+    attn_tile_kernel<T, 128><<<(unsigned)grid, kThreadsT, TileShape<128>::SMEM, stream>>>(p, c.mk, c.mv);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+namespace ppc_attn {
+
+bool tile_applicable(const AttnParams& p, int dtype, int sms) {
+  if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
+  // Rows of units (attn.cu) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where
+  // pages are selected) at about 1 us per 64 keys and CTA; a tile meets it with 128 in about half of that.
+  const int64_t tiles = ((int64_t)p.T * p.G.d + kRowsT - 1) / kRowsT * p.H, units = ((int64_t)p.T * p.G.d + 15) / 16 * p.H;
+  return (tiles + 2 * sms - 1) / (2 * sms) * sms < units;
+}
+
+cudaError_t tile_prepare() {
+  cudaError_t e = prepare_one<__half, 64>();
+  if (e == cudaSuccess) e = prepare_one<__half, 128>();
+  if (e == cudaSuccess) e = prepare_one<__nv_bfloat16, 64>();
+  if (e == cudaSuccess) e = prepare_one<__nv_bfloat16, 128>();
+  return e;
+}
+
+cudaError_t tile_launch(const AttnParams& p, const pp_cache& c, cudaStream_t stream) {
+  // each sequence adds at most one tile that is not full; CTAs beyond the last tile leave
+  const int TT = kRowsT / p.G.d;
+  const int64_t grid = ((int64_t)p.T / TT + std::min(p.T, p.B)) * p.H;
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  return c.dtype == PP_F16 ? launch<__half>(p, c, grid, stream) : launch<__nv_bfloat16>(p, c, grid, stream);
+}
+
+}  // namespace ppc_attn

@@ -117,12 +117,14 @@ def attend(q, k, v, table, starts, lens, scale, causal, sel=None):
     for t, (b, n) in enumerate(seen_keys(T, starts, lens, causal)):
         P = -(-n // page)
         for h in range(H):
-            some = range(P) if sel is None else [w for w in sel[t, h].tolist() if 0 <= w < P]
-            cells = [(int(table[b, w]), i) for w in some for i in range(min(page, n - w * page)) if 0 <= int(table[b, w]) < pages]
-            if not cells:
+            some = torch.arange(P) if sel is None else sel[t, h][(sel[t, h] >= 0) & (sel[t, h] < P)].long()
+            key = (some[:, None] * page + torch.arange(page)).flatten()
+            key = key[key < n]
+            ip, io = table[b, key // page].long(), key % page
+            good = (ip >= 0) & (ip < pages)
+            ip, io = ip[good], io[good]
+            if not len(ip):
                 continue
-            ip = torch.tensor([c[0] for c in cells])
-            io = torch.tensor([c[1] for c in cells])
             kk, vv = k[ip, h, io].double(), v[ip, h, io].double()
             x = q[t, h * G: (h + 1) * G].double()
             s = scale * (x @ kk.T)
@@ -130,10 +132,10 @@ def attend(q, k, v, table, starts, lens, scale, causal, sel=None):
             p = torch.softmax(s, -1)
             o = p @ vv
             hs = slice(h * G, (h + 1) * G)
-            rel = 2 * d + 2.0 ** -19 + len(cells) * 2.0 ** -24 + (2.0 ** -20 if wide else UNIT[dt])
+            rel = 2 * d + 2.0 ** -19 + len(ip) * 2.0 ** -24 + (2.0 ** -20 if wide else UNIT[dt])
             out[t, hs], lse[t, hs] = o, torch.logsumexp(s, -1)
             tol[t, hs] += rel * (p @ vv.abs()) + UNIT[dt] * o.abs() * 1.01
-            tl[t, hs] = d[:, 0] + 2.0 ** -19 + len(cells) * 2.0 ** -24 + 2.0 ** -22 * lse[t, hs].abs()
+            tl[t, hs] = d[:, 0] + 2.0 ** -19 + len(ip) * 2.0 ** -24 + 2.0 ** -22 * lse[t, hs].abs()
     return out, lse, tol, tl
 
 

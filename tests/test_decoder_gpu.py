@@ -1,8 +1,9 @@
 """The decoder operators on the GPU, through the binding, against their definitions in 64 bits (tests/decoder_ref.py):
 rotations into tensors and into the cache, page summaries, selections, attention over all and over selected pages."""
 import math
+import re
+import warnings
 
-import numpy as np
 import pytest
 import torch
 
@@ -662,3 +663,150 @@ def test_many_parts_of_one_unit(pp):
             assert c.status() == 0
         finally:
             c.close()
+
+
+# ------------------------------------------------------------------ many tokens: tiles of 128 rows
+
+TILES = [
+    # dtype, G, H, D, page, lens, tokens: enough rows that the tile kernel takes them
+    (BF16, 8, 1, 128, 64, [400], [330]),
+    (F16, 8, 1, 128, 64, [331, 0, 70], [331, 0, 5]),
+    (BF16, 2, 2, 64, 16, [900], [700]),
+    (F16, 3, 2, 80, 32, [520, 77], [500, 40]),     # 42 tokens to a tile, heads that end inside a column
+    (BF16, 1, 2, 128, 128, [1350], [1300]),
+    (F16, 1, 2, 64, 8, [1300, 20], [1300, 1]),
+    (BF16, 64, 1, 16, 8, [90], [50]),
+    (F16, 4, 4, 96, 256, [300], [170]),
+    (BF16, 5, 1, 24, 64, [640], [600]),
+]
+
+
+def tile_kernel_runs(c, tmp_path, sel=None):
+    """Whether this call launches the tile kernel, from a captured graph's dump."""
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    g.enable_debug_mode()
+    with torch.cuda.graph(g):
+        c.attend(sel=sel, stream=torch.cuda.current_stream())
+    dot = tmp_path / "graph.dot"
+    with warnings.catch_warnings():
+        warnings.simplefilter("ignore")
+        g.debug_dump(str(dot))
+    names = re.findall(r"attn_\w*kernel", dot.read_text())
+    assert names
+    return any("tile" in n for n in names)
+
+
+@pytest.mark.parametrize("dt,G,H,D,page,lens,tokens", TILES)
+def test_tiles(pp, tmp_path, dt, G, H, D, page, lens, tokens):
+    c = Case(pp, dt, G, H, D, page, lens, tokens, seed=D + G)
+    try:
+        assert tile_kernel_runs(c, tmp_path)
+        c.check()
+        c.check(causal=False)
+        c.check(scale=-0.3)
+        c.check(scale=0.0)
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt,G,H,D,page,lens,tokens", TILES)
+@pytest.mark.parametrize("keep", [1, 7])
+def test_tiles_selected(pp, tmp_path, dt, G, H, D, page, lens, tokens, keep):
+    """Neighbours that select different pages, tokens without any, entries of no page."""
+    c = Case(pp, dt, G, H, D, page, lens, tokens, seed=D + G + keep)
+    try:
+        g = torch.Generator().manual_seed(2)
+        sel = torch.full((c.T, H, keep), -1, dtype=torch.int32)
+        for t, (b, n) in enumerate(ref.seen_keys(c.T, c.starts, lens, True)):
+            P = -(-n // page)
+            for h in range(H):
+                some = torch.randperm(P, generator=g)[:keep]
+                sel[t, h, : len(some)] = some.to(torch.int32)
+        sel[3] = -1
+        sel[5, 0, 0] = -7
+        assert tile_kernel_runs(c, tmp_path, sel.cuda())
+        c.check(sel=sel)
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+def test_tiles_large_logits(pp, dt):
+    """Maxima that grow by hundreds from block to block, so that the sums are rescaled, and ones that never do."""
+    c = Case(pp, dt, 4, 2, 64, 64, [700], [400], seed=21)
+    try:
+        for w in range(c.table.shape[1] - 1):  # later pages hold larger keys
+            i = int(c.table[0, w])
+            c.k[i] = (c.k[i].float() * (0.1 + 0.4 * w)).to(dt)
+        c.kd.copy_(c.k)
+        for scale in (0.125, 2.0, 20.0):
+            c.check(scale=scale)
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("selected", [False, True])
+@pytest.mark.parametrize("where", ["value", "key"])
+def test_tiles_keep_tokens_apart(pp, where, selected):
+    """NaN and infinity at a key that some of a tile's tokens see: the others stay as they were."""
+    c = Case(pp, BF16, 4, 2, 64, 16, [500], [400], seed=12)
+    try:
+        pool = c.v if where == "value" else c.k
+        for key, bad in ((170, math.nan), (230, math.inf)):
+            pool[int(c.table[0, key // 16]), 0, key % 16, 5] = bad
+        c.kd.copy_(c.k)
+        c.vd.copy_(c.v)
+        sel = None
+        if selected:
+            g = torch.Generator().manual_seed(4)
+            sel = torch.stack([torch.randperm(100 // 16, generator=g)[:3] for _ in range(c.T * 2)]).view(c.T, 2, 3).to(torch.int32)
+            sel[::3, :, 1] = 170 // 16
+        out, lse = c.attend(sel=None if sel is None else sel.cuda())
+        want, wl, tol, tl = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.lens, 1 / 8.0, True, sel)
+        fine = torch.isfinite(want)
+        got = out.double().cpu()
+        assert torch.equal(torch.isfinite(got), fine)
+        assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
+    finally:
+        c.close()
+
+
+def test_tiles_bad_pages(pp):
+    c = Case(pp, F16, 4, 2, 64, 16, [500, 40], [300, 40], seed=4)
+    try:
+        for bad in (-1, c.k.shape[0], 2 ** 30):
+            c.table[0, 2] = bad
+            c.td.copy_(c.table)
+            c.check()
+            assert c.status() == pp.PP_CACHE_BAD_PAGE
+        c.sd.copy_(torch.tensor([0, 400, 340]))  # token ranges that do not fit
+        c.attend()
+        assert c.status() & pp.PP_CACHE_BAD_LENGTH
+    finally:
+        c.close()
+
+
+def test_tiles_over_windows_of_pages(pp, tmp_path):
+    """More pages than the masks of one window hold."""
+    c = Case(pp, BF16, 1, 2, 64, 8, [9000], [1300], seed=4)
+    try:
+        g = torch.Generator().manual_seed(2)
+        sel = torch.stack([torch.randperm(7700 // 8, generator=g)[:5] for _ in range(c.T * 2)]).view(c.T, 2, 5).to(torch.int32)
+        assert tile_kernel_runs(c, tmp_path, sel.cuda())
+        c.check(sel=sel)
+    finally:
+        c.close()
+
+
+def test_tiles_same_bits(pp):
+    c = Case(pp, BF16, 4, 2, 128, 64, [3000, 500], [500, 100], seed=6)
+    try:
+        first, l1 = c.attend()
+        for _ in range(4):
+            again, l2 = c.attend()
+            assert torch.equal(first, again) and torch.equal(l1, l2)
+        c.check()
+    finally:
+        c.close()
