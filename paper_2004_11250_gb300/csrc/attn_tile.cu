@@ -209,7 +209,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   const int* table = p.table + (int64_t)b * p.width;
   const int log_br = min(p.log_page, 6), BR = 1 << log_br, log_pc = 6 - log_br, pieces = 1 << log_pc;
   const int log_pp = p.log_page - log_br;  // pieces per page
-  const float sl = p.scale * 1.44269504f;
+  // a negative scale goes into the queries, and so does 0 (with no queries, any scale): sl > 0
+  const float sl = p.scale == 0.f ? 1.f : fabsf(p.scale) * 1.44269504f;
 
   // ---- set up
   if (warp == 5) {
@@ -255,6 +256,10 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v.v[e] = from[e];
+        }
+        if (p.scale <= 0.f) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v.v[e] = from_f32<T>(p.scale < 0.f ? -to_f32(v.v[e]) : 0.f);
         }
       }
       *reinterpret_cast<Vec<T, 8>*>(smem + c / 8 * CHUNK_Q + r * 128 + ((c % 8 ^ (r & 7)) << 4)) = v;
@@ -403,23 +408,32 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       // ---- softmax, a thread per row
       for (int k = 0; k < n; ++k) {
         const int g = done + k, st = g % kStages;
-        hold(&v_full[st], g / kStages & 1);  // what the copying warp says, too
+        // which of the block's keys the row sees, a bit each
+        uint64_t see = 0;
+        const Block& bl = info[st];
+        if (log_pc == 0) {  // a page, or a piece of one
+          const int key = key_of(k);
+          bool on = live_row && key >= 0;
+          if (on && p.sel) on = masks[list[k >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
+          hold(&v_full[st], g / kStages & 1);  // what the copying warp says, too
+          const int c = on ? min(bl.have[0], lim - key) : 0;
+          see = c >= 64 ? ~0ull : c > 0 ? (1ull << c) - 1 : 0;
+        } else {
+          hold(&v_full[st], g / kStages & 1);
+#pragma unroll 1
+          for (int j = 0; j < pieces; ++j) {
+            const int i = (k << log_pc) + j, key = key_of(i);
+            bool on = live_row && key >= 0;
+            if (on && p.sel) on = masks[list[i >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
+            const int c = on ? min(bl.have[j], lim - key) : 0;
+            if (c > 0) see |= ((1ull << c) - 1) << (j << log_br);
+          }
+        }
+        const bool part = __any_sync(~0u, see != 0 && see != ~0ull), none = __all_sync(~0u, see == 0);
         hold(&s_full[g & 1], g >> 1 & 1);
         __syncwarp();
         tm_fence_after();
         const uint32_t tm = row_tm + 128 + (g & 1) * 64;
-        // which of the block's keys the row sees, a bit each
-        uint64_t see = 0;
-        const Block& bl = info[st];
-#pragma unroll 1
-        for (int j = 0; j < pieces; ++j) {
-          const int i = (k << log_pc) + j, key = key_of(i);
-          bool on = live_row && key >= 0;
-          if (on && p.sel) on = masks[(i >> log_pp < (npieces >> log_pp) ? list[i >> log_pp] : 0) * words + tok / 32] >> (tok % 32) & 1;
-          const int c = on ? min(bl.have[j], lim - key) : 0;
-          if (c > 0) see |= (c >= 64 ? ~0ull : (1ull << c) - 1) << (j << log_br);
-        }
-        const bool all = __all_sync(~0u, see == ~0ull), none = __all_sync(~0u, see == 0);
         uint32_t w[32];
         bool waited = false;
         if (none) {
@@ -430,18 +444,20 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           tm_ld32(tm, reinterpret_cast<float(&)[32]>(x[0]));
           tm_ld32(tm + 32, reinterpret_cast<float(&)[32]>(x[32]));
           tm_wait_ld();
-          // where every key is seen the scale goes into the exponent's product, else in first, before what is not seen
-          float mul = sl;
-          if (!all || sl <= 0.f) {
-            mul = 1.f;
+          // rows that see all or nothing need no mask: the latter's exponents are taken from infinity below
+          if (part) {
 #pragma unroll
             for (int i = 0; i < 64; ++i)
-              x[i] = (i < 32 ? (uint32_t)see : (uint32_t)(see >> 32)) >> (i & 31) & 1 ? x[i] * sl : -INFINITY;
+              if (!((i < 32 ? (uint32_t)see : (uint32_t)(see >> 32)) >> (i & 31) & 1)) x[i] = -INFINITY;
           }
-          float mx = x[0];
+          float top[4];
 #pragma unroll
-          for (int i = 1; i < 64; ++i) mx = fmaxf(mx, x[i]);
-          mx *= mul;
+          for (int c = 0; c < 4; ++c) {
+            top[c] = fmaxf(x[c], x[c + 4]);
+#pragma unroll
+            for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
+          }
+          const float mx = see ? fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl : -INFINITY;
           const bool grow = mx > m + kGrow;  // from -infinity, too
           if (__any_sync(~0u, grow)) {
             const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
@@ -465,15 +481,21 @@ __global__ void __launch_bounds__(kThreadsT, 2)
               tm_wait_st();
             }
           }
-          const float at = m == -INFINITY ? 0.f : m;
-          float sum = 0.f;
+          const float at = see ? (m == -INFINITY ? 0.f : m) : INFINITY;
+          const uint64_t sl2 = pack2(sl, sl), at2 = pack2(-at, -at);
+          uint64_t sum[4] = {};
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            const float a = ex2(fmaf(x[2 * i], mul, -at)), c = ex2(fmaf(x[2 * i + 1], mul, -at));
-            sum += a + c;
+            float a, c;
+            unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), sl2, at2), a, c);
+            a = ex2(a);
+            c = ex2(c);
+            sum[i & 3] = add2(sum[i & 3], pack2(a, c));
             w[i] = pack<T>(a, c);
           }
-          l += sum;
+          float a, c;
+          unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, c);
+          l += a + c;
         }
         tm_st32(tm, w);
         if (!bl.full) {  // values that no row sees: 0 x them has to be 0

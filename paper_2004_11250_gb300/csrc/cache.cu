@@ -1,19 +1,15 @@
-// The paged cache: its handle, page summaries and page selection
-// (pp_cache_create, pp_cache_summarize, pp_cache_select).
+// The paged cache: its handle and page summaries (pp_cache_create,
+// pp_cache_summarize).
 #include <algorithm>
 #include <cmath>
 #include <new>
 
 #include "cache.h"
 #include "internal.h"
-#include "tc_ptx.cuh"
 
 namespace {
 
 using namespace ppc;
-using namespace ppc_ptx;
-
-constexpr float kTiny = 0x1p-100f;  // largest value below which a page or query counts as 0: 127 / a stays finite
 
 constexpr int kThreads = 256;
 
@@ -86,210 +82,6 @@ __global__ void __launch_bounds__(kThreads) summarize_kernel(const T* __restrict
   if (tid == 0) scales[cell] = odd ? nanf("") : __fmul_rn(a, 1.f / 127.f);
 }
 
-// ---- selection
-
-struct SelectParams {
-  const void* q;
-  int64_t q_ts, q_hs;
-  const int *starts, *table, *lens;
-  const int8_t* codes;
-  const float* scales;
-  int* sel;
-  int* status;
-  int T, B, H, G, D, page, pages, width, first, last, keep, Q, causal;
-};
-
-// A score as an integer of the same order; NaN as the lowest.
-__device__ __forceinline__ uint32_t ordered(float v) {
-  if (v != v) v = -INFINITY;
-  const uint32_t u = __float_as_uint(v + 0.f);  // one zero
-  return u >> 31 ? ~u : u | 0x80000000u;
-}
-
-// A group's queries as sums of integers: value d of up [D] and down [D] for token t and head h, by nthr threads of which
-// this is thread i.  big: the largest |q| of the group (infinity if one is not finite).
-template <class T>
-__device__ __forceinline__ float largest_query(const SelectParams& p, int t, int h, int i, int nthr) {
-  const T* q = static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)h * p.G * p.q_hs;
-  float m = 0.f;
-  for (int j = i; j < p.G * p.D; j += nthr) {
-    const float v = fabsf(to_f32(q[j / p.D * p.q_hs + j % p.D]));
-    m = v <= 3.402823466e38f ? fmaxf(m, v) : INFINITY;  // a NaN too
-  }
-  return m;
-}
-template <class T>
-__device__ __forceinline__ void query_codes(const SelectParams& p, int t, int h, float big, int d, int& up, int& down) {
-  const T* q = static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)h * p.G * p.q_hs + d;
-  up = down = 0;
-  if (!(big >= kTiny) || big == INFINITY) return;
-  const float r = __fdiv_rn((float)p.Q, big);
-  for (int g = 0; g < p.G; ++g) {
-    const int c = (int)rintf(__fmul_rn(to_f32(q[g * p.q_hs]), r));
-    up += max(c, 0);
-    down += min(c, 0);
-  }
-}
-
-__device__ __forceinline__ int dot2_lo(int a, int b, int c) {  // c + a's two 16-bit halves times b's bytes 0 and 1
-  int d;
-  asm("dp2a.lo.s32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ int dot2_hi(int a, int b, int c) {
-  int d;
-  asm("dp2a.hi.s32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-
-// Single tokens: a cluster per (token, head), its CTAs sharing the pages.  Bound by reading the codes, 2 D bytes a page:
-// a lane keeps 16 of the query's integers and meets 16 codes of every page with two-way integer products.  The first
-// CTA has all scores in shared memory and finds the keep-th largest digit by digit (8 bits each).
-template <class T>
-__global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) {
-  extern __shared__ uint32_t key[];
-  __shared__ __align__(16) short code[512];
-  __shared__ float big[kThreads / 32];
-  __shared__ int hist[256], warp_sum[kThreads / 32], digit_of, left_of;
-  const int rank = cluster_rank(), ranks = cluster_size();
-  const int t = blockIdx.x / ranks, h = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-  const Seen s = seen_keys(t, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
-  const int P = (s.keys + p.page - 1) / p.page;
-  int* out = p.sel + ((int64_t)t * p.H + h) * p.keep;
-  if (P <= p.keep) {  // the whole cluster
-    if (rank == 0)
-      for (int i = tid; i < p.keep; i += kThreads) out[i] = i < P ? i : -1;
-    return;
-  }
-  float m = largest_query<T>(p, t, h, tid, kThreads);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-  if (lane == 0) big[warp] = m;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, big[i]);
-  if (tid < p.D) {
-    int up, down;
-    query_codes<T>(p, t, h, m, tid, up, down);
-    code[tid] = (short)up;
-    code[p.D + tid] = (short)down;
-  }
-  __syncthreads();
-  // candidates: pages first .. P - last - 1; 2 D / 16 lanes a page, in a power of two
-  const int N = P - p.first - p.last, chunks = p.D / 8;
-  int span = 2;
-  while (span < chunks) span *= 2;
-  const int at = lane % span, per = 32 / span;  // pages per warp at a time
-  int mine[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) mine[i] = at < chunks ? reinterpret_cast<const int*>(code)[at * 8 + i] : 0;
-  const int* row = p.table + (int64_t)s.b * p.width + p.first;
-  const uint32_t keys0 = map_rank((uint32_t)__cvta_generic_to_shared(key), 0);
-  const int step = (kThreads / 32) * per;
-  constexpr int U = 4;
-  for (int w0 = (rank * U * (kThreads / 32) + warp * U) * per; w0 < N; w0 += ranks * U * step) {
-    int4 c[U];
-    float sc[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int w = w0 + u * per + lane / span;
-      c[u] = make_int4(0, 0, 0, 0);
-      sc[u] = nanf("");
-      if (w < N) {
-        const int id = row[w];
-        if (id < 0 || id >= p.pages) {
-          if (at == 0) atomicOr(p.status, PP_CACHE_BAD_PAGE);
-        } else {
-          const int64_t cell = (int64_t)id * p.H + h;
-          if (at < chunks) c[u] = *reinterpret_cast<const int4*>(p.codes + cell * 2 * p.D + at * 16);
-          sc[u] = p.scales[cell];
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      int sum = dot2_hi(mine[1], c[u].x, dot2_lo(mine[0], c[u].x, 0));
-      sum = dot2_hi(mine[3], c[u].y, dot2_lo(mine[2], c[u].y, sum));
-      sum = dot2_hi(mine[5], c[u].z, dot2_lo(mine[4], c[u].z, sum));
-      sum = dot2_hi(mine[7], c[u].w, dot2_lo(mine[6], c[u].w, sum));
-      for (int d = span / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-      const int w = w0 + u * per + lane / span;
-      if (at == 0 && w < N)
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys0 + 4 * w), "r"(ordered(__fmul_rn((float)sum, sc[u]))) : "memory");
-    }
-  }
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  if (rank != 0) return;
-  // the need-th largest key: thr, with `need` of those equal to it (under the mask of the digits found)
-  int need = p.keep - p.first - p.last;
-  uint32_t thr = 0, mask = 0;
-  for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-    hist[tid] = 0;
-    __syncthreads();
-    for (int w = tid; w < N; w += kThreads)
-      if ((key[w] & mask) == thr) atomicAdd(&hist[key[w] >> shift & 255], 1);
-    __syncthreads();
-    const int have = hist[255 - tid];  // digits from the largest down
-    int sum = have;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(~0u, sum, d);
-      if (lane >= d) sum += o;
-    }
-    if (lane == 31) warp_sum[warp] = sum;
-    __syncthreads();
-    for (int i = 0; i < warp; ++i) sum += warp_sum[i];
-    if (sum >= need && sum - have < need) {
-      digit_of = 255 - tid;
-      left_of = need - (sum - have);
-    }
-    __syncthreads();
-    thr |= (uint32_t)digit_of << shift;
-    mask |= 255u << shift;
-    need = left_of;
-    if (hist[digit_of] == need) break;  // all that start like this
-    __syncthreads();
-  }
-  __syncthreads();
-  // each thread a run of pages, in order: those above thr, and the first `need` equal to it
-  const int len = (N + kThreads - 1) / kThreads, w0 = min(N, tid * len), w1 = min(N, w0 + len);
-  int above = 0, equal = 0;
-  if (p.keep > p.first + p.last)
-    for (int w = w0; w < w1; ++w) {
-      const uint32_t v = key[w] & mask;
-      above += v > thr;
-      equal += v == thr;
-    }
-  int sum = above | equal << 16;  // above < 2^11, equal <= 2^15
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int o = __shfl_up_sync(~0u, sum, d);
-    if (lane >= d) sum += o;
-  }
-  if (lane == 31) warp_sum[warp] = sum;
-  __syncthreads();
-  for (int i = 0; i < warp; ++i) sum += warp_sum[i];
-  sum -= above | equal << 16;
-  int a = sum & 0xFFFF, e = (uint32_t)sum >> 16;
-  if (p.keep > p.first + p.last)
-    for (int w = w0; w < w1; ++w) {
-      const uint32_t v = key[w] & mask;
-      if (v > thr || (v == thr && e < need)) out[p.first + a + min(e, need)] = p.first + w;
-      a += v > thr;
-      e += v == thr;
-    }
-  for (int i = tid; i < p.first; i += kThreads) out[i] = i;
-  for (int i = tid; i < p.last; i += kThreads) out[p.keep - p.last + i] = P - p.last + i;
-}
-
-DeviceOnce g_select_once;
-
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -340,7 +132,7 @@ pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k,
   c->codes = codes;
   c->scales = scales;
   const int sms = device_sms();
-  if (sms <= 0 || attn_prepare() != cudaSuccess || !pool_map(&c->mk, *c, k) || !pool_map(&c->mv, *c, v)) {
+  if (sms <= 0 || attn_prepare() != cudaSuccess || select_prepare() != cudaSuccess || !pool_map(&c->mk, *c, k) || !pool_map(&c->mv, *c, v)) {
     delete c;
     return PP_ERR_CUDA;
   }
@@ -398,52 +190,6 @@ pp_status pp_cache_summarize(const pp_cache* cache, const int32_t* ids, int n, v
   else
     run(static_cast<const __nv_bfloat16*>(c.k));
   return cudaGetLastError() == cudaSuccess ? PP_OK : PP_ERR_CUDA;
-}
-
-pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
-                          const int32_t* starts, const int32_t* table, int width, const int32_t* lens, int flags,
-                          int first, int last, int keep, int32_t* sel, void* stream) {
-  if (!cache || !cache->codes || T < 0 || B < 0 || Hq < 1 || Hq % cache->H || width < 1 || q_ts < 0 || q_hs < 0 ||
-      first < 0 || last < 1 || keep < 1 || (int64_t)first + last > keep || (flags & ~PP_ATTN_CAUSAL))
-    return PP_ERR_INVALID_ARG;
-  if (T > 0 && (!q || !table || !lens || !sel || B < 1 || (!starts && T != B) ||
-                (reinterpret_cast<uintptr_t>(q) & (dtype_size(cache->dtype) - 1))))
-    return PP_ERR_INVALID_ARG;
-  const int G = Hq / cache->H;
-  const int64_t Q = std::min<int64_t>(127, (1 << 24) / ((int64_t)127 * cache->D * G));
-  if (width > 32768 || keep > 1024 || Q < 1) return PP_ERR_UNSUPPORTED;
-  if (T == 0) return PP_OK;
-  const int sms = device_sms();
-  if (sms <= 0) return PP_ERR_CUDA;
-  const cudaError_t e = g_select_once.run([](int) {
-    cudaError_t r = cudaFuncSetAttribute(select_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 131072);
-    if (r == cudaSuccess)
-      r = cudaFuncSetAttribute(select_kernel<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, 131072);
-    if (r == cudaSuccess)
-      r = cudaFuncSetAttribute(select_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 131072);
-    return r;
-  });
-  if (e != cudaSuccess) return PP_ERR_CUDA;
-  SelectParams p = {q, q_ts, q_hs, starts, table, lens, cache->codes, cache->scales, sel, cache->status, T, B, cache->H, G,
-                    cache->D, cache->page, cache->pages, width, first, last, keep, (int)Q, flags & PP_ATTN_CAUSAL};
-  // CTAs per (token, head): more where there are few, so that long tables are read by enough of them
-  int ranks = 1;
-  while (ranks < 8 && (int64_t)T * cache->H * ranks * 2 <= sms * 2 && width >= ranks * 2 * 128) ranks *= 2;
-  if ((int64_t)T * ranks > INT32_MAX) return PP_ERR_UNSUPPORTED;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(T * ranks, cache->H);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)width * 4;
-  cfg.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)ranks, 1, 1};
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  const cudaError_t r = cache->dtype == PP_F32   ? cudaLaunchKernelEx(&cfg, select_kernel<float>, p)
-                        : cache->dtype == PP_F16 ? cudaLaunchKernelEx(&cfg, select_kernel<__half>, p)
-                                                 : cudaLaunchKernelEx(&cfg, select_kernel<__nv_bfloat16>, p);
-  return r == cudaSuccess ? PP_OK : PP_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -42,6 +42,7 @@ struct AttnSpace {
 };
 AttnSpace attn_space(int dtype, int D, int sms);
 cudaError_t attn_prepare();
+cudaError_t select_prepare();
 
 inline int dtype_size(int dtype) { return dtype == PP_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == PP_F32 || dtype == PP_F16 || dtype == PP_BF16; }
@@ -75,6 +76,8 @@ inline int log2_of(int n) {
   while ((1 << s) < n) ++s;
   return s;
 }
+
+constexpr float kTiny = 0x1p-100f;  // a page's or query's largest value below which it counts as 0: 127 / a stays finite
 
 // V consecutive elements moved as one (up to 16 bytes).
 template <class T, int V>
