@@ -32,6 +32,7 @@ constexpr int kSoft = 128;             // threads of the softmax; then a copying
 constexpr int kThreadsT = kSoft + 64;
 constexpr int kKeys = 64;              // keys per block
 constexpr int kStages = 2;             // of K and of V
+constexpr int kInfo = 4;               // blocks that the copying warp may be ahead of the softmax, and one
 constexpr int kMaskWords = 2048;       // token bits of the pages in one window
 constexpr float kGrow = 8.f;           // log2 of how far a row's scores may pass its m
 
@@ -50,20 +51,41 @@ struct Block {          // what the copying warp says of a block
 // Shared-memory descriptors of 128-byte swizzled operands.  K-major (Q, K): rows of 128 bytes, groups of 8 rows 1024
 // bytes apart.  MN-major (V): 128 bytes of values per key, groups of 8 keys 1024 bytes apart, the next 64 values `lbo`
 // bytes on.
-__device__ __forceinline__ uint64_t desc_128(uint32_t addr, uint32_t lbo) {
-  return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+constexpr uint32_t kDescHi = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr >> 4) & 0x3FFF) | (lbo >> 4) << 16; }
 template <class T>
 __host__ __device__ constexpr uint32_t idesc(int m, int n, bool b_mn) {
   const uint32_t f = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
   return (1u << 4) | (f << 7) | (f << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-// the left operand in TMEM
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+// Products and commits of a whole warp, issued by its leader.  The warp stays together, so that the operands are in
+// uniform registers, as the instructions want them: behind a branch of one lane each is moved there first, and an issue
+// took some 100 cycles.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t acc, uint32_t leader) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a),
-      "l"(b), "r"(id), "r"(acc));
+      "{ .reg .pred p, q; .reg .b64 x, y; setp.ne.b32 p, %5, 0; setp.ne.b32 q, %6, 0; mov.b64 x, {%1, %4}; mov.b64 y, {%2, %4};"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(id), "r"(kDescHi), "r"(acc), "r"(leader)
+      : "memory");
+}
+// the left operand in TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t acc, uint32_t leader) {
+  asm volatile(
+      "{ .reg .pred p, q; .reg .b64 y; setp.ne.b32 p, %5, 0; setp.ne.b32 q, %6, 0; mov.b64 y, {%2, %4};"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(id), "r"(kDescHi), "r"(acc), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar, uint32_t leader) {
+  asm volatile(
+      "{ .reg .pred q; setp.ne.b32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar),
+      "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+  return r;
 }
 __device__ __forceinline__ void tm_ld32(uint32_t a, float (&v)[32]) {
   uint32_t r[32];
@@ -140,7 +162,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   uint16_t* list = reinterpret_cast<uint16_t*>(masks + kMaskWords);
   __shared__ alignas(8) uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], s_full[2],
       p_full[2], pv_done;
-  __shared__ Block info[kStages];
+  __shared__ Block info[kInfo];
+  __shared__ alignas(8) uint64_t info_full[kInfo];
   __shared__ uint32_t tmem_s;
   __shared__ int scan[kThreadsT / 32], tile_of[4], found_n, dead;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -228,6 +251,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       mbar_init(su32(&v_full[i]), 1);
       mbar_init(su32(&v_empty[i]), 1);
     }
+    for (int i = 0; i < kInfo; ++i) mbar_init(su32(&info_full[i]), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(su32(&s_full[i]), 1);
       mbar_init(su32(&p_full[i]), kSoft);
@@ -352,18 +376,21 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         const bool whole = __all_sync(~0u, have == BR);
         const int bytes = __popc(live) * BR * DP * 2, boxes = pieces * (DP / 64), c = lane >> log_pc;
         hold(&k_empty[st], ph);
+        // the softmax is done with what was said of block g - 4: the scores of g - 2, just found done, were asked for after it
+        if (lane < pieces) info[g % kInfo].have[lane] = have;
+        if (lane == 0) info[g % kInfo].full = whole;
         __syncwarp();
         bool go = !*(volatile int*)&dead;
-        if (lane == 0) mbar_arrive_expect_tx(su32(&k_full[st]), go ? bytes : 0);
+        if (lane == 0) {
+          mbar_arrive(su32(&info_full[g % kInfo]));
+          mbar_arrive_expect_tx(su32(&k_full[st]), go ? bytes : 0);
+        }
         __syncwarp();
         if (go && lane < boxes && (live >> j & 1))
           copy_box(su32(kbuf + st * S::KV) + c * CHUNK_KV + j * BR * 128, &mk, c * 64, y, su32(&k_full[st]));
         hold(&v_empty[st], ph);
         __syncwarp();
         go = !*(volatile int*)&dead;
-        if (lane < pieces) info[st].have[lane] = have;
-        if (lane == 0) info[st].full = whole;
-        __syncwarp();
         if (lane == 0) mbar_arrive_expect_tx(su32(&v_full[st]), go ? bytes : 0);
         __syncwarp();
         if (go && lane < boxes && (live >> j & 1))
@@ -371,55 +398,53 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       }
     } else if (warp == 5) {
       // ---- products
-      if (lane == 0) {
-        auto scores = [&](int k) {
-          const int g = done + k, st = g % kStages;
-          hold(&k_full[st], g / kStages & 1);
-          tm_fence_after();
-          const uint32_t a = su32(smem), kb = su32(kbuf + st * S::KV);
+      const uint32_t leader = elect();
+      const uint32_t qa = desc_lo(su32(smem), 16), kb = desc_lo(su32(kbuf), 16), vb = desc_lo(su32(vbuf), CHUNK_KV);
+      auto scores = [&](int k) {
+        const int g = done + k, st = g % kStages;
+        hold(&k_full[st], g / kStages & 1);
+        tm_fence_after();
+        const uint32_t kd = kb + st * (S::KV >> 4), to = tmem + 128 + (g & 1) * 64;
 #pragma unroll
-          for (int kk = 0; kk < DP / 16; ++kk)
-            mma_f16(tmem + 128 + (g & 1) * 64, desc_128(a + kk / 4 * CHUNK_Q + kk % 4 * 32, 16),
-                    desc_128(kb + kk / 4 * CHUNK_KV + kk % 4 * 32, 16), idesc<T>(kRowsT, kKeys, false), kk > 0);
-          mma_commit(su32(&k_empty[st]));
-          mma_commit(su32(&s_full[g & 1]));
-        };
-        if (n > 0) {
-          if (done == 0) hold(&q_full, 0);
-          scores(0);
-        }
-        for (int k = 0; k < n; ++k) {
-          const int g = done + k, st = g % kStages;
-          if (k + 1 < n) scores(k + 1);
-          hold(&p_full[g & 1], g >> 1 & 1);
-          hold(&v_full[st], g / kStages & 1);
-          tm_fence_after();
-          const uint32_t vb = su32(vbuf + st * S::KV);
-#pragma unroll
-          for (int kk = 0; kk < kKeys / 16; ++kk)
-            mma_f16_ts(tmem, tmem + 128 + (g & 1) * 64 + kk * 8, desc_128(vb + kk * 2048, CHUNK_KV), idesc<T>(kRowsT, DP, true),
-                       g > 0 || kk > 0);
-          mma_commit(su32(&v_empty[st]));
-          mma_commit(su32(&pv_done));
-        }
+        for (int kk = 0; kk < DP / 16; ++kk)
+          mma_ss(to, qa + (kk / 4 * CHUNK_Q + kk % 4 * 32 >> 4), kd + (kk / 4 * CHUNK_KV + kk % 4 * 32 >> 4),
+                 idesc<T>(kRowsT, kKeys, false), kk > 0, leader);
+        commit(su32(&k_empty[st]), leader);
+        commit(su32(&s_full[g & 1]), leader);
+      };
+      if (n > 0) {
+        if (done == 0) hold(&q_full, 0);
+        scores(0);
       }
-      __syncwarp();
+      for (int k = 0; k < n; ++k) {
+        const int g = done + k, st = g % kStages;
+        if (k + 1 < n) scores(k + 1);
+        hold(&v_full[st], g / kStages & 1);
+        hold(&p_full[g & 1], g >> 1 & 1);
+        tm_fence_after();
+        const uint32_t vd = vb + st * (S::KV >> 4), pt = tmem + 128 + (g & 1) * 64;
+#pragma unroll
+        for (int kk = 0; kk < kKeys / 16; ++kk)
+          mma_ts(tmem, pt + kk * 8, vd + (kk * 2048 >> 4), idesc<T>(kRowsT, DP, true), g > 0 || kk > 0, leader);
+        commit(su32(&v_empty[st]), leader);
+        commit(su32(&pv_done), leader);
+      }
     } else {
       // ---- softmax, a thread per row
       for (int k = 0; k < n; ++k) {
         const int g = done + k, st = g % kStages;
         // which of the block's keys the row sees, a bit each
         uint64_t see = 0;
-        const Block& bl = info[st];
+        const Block& bl = info[g % kInfo];
         if (log_pc == 0) {  // a page, or a piece of one
           const int key = key_of(k);
           bool on = live_row && key >= 0;
           if (on && p.sel) on = masks[list[k >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
-          hold(&v_full[st], g / kStages & 1);  // what the copying warp says, too
+          hold(&info_full[g % kInfo], g / kInfo & 1);
           const int c = on ? min(bl.have[0], lim - key) : 0;
           see = c >= 64 ? ~0ull : c > 0 ? (1ull << c) - 1 : 0;
         } else {
-          hold(&v_full[st], g / kStages & 1);
+          hold(&info_full[g % kInfo], g / kInfo & 1);
 #pragma unroll 1
           for (int j = 0; j < pieces; ++j) {
             const int i = (k << log_pc) + j, key = key_of(i);
@@ -499,6 +524,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         }
         tm_st32(tm, w);
         if (!bl.full) {  // values that no row sees: 0 x them has to be 0
+          hold(&v_full[st], g / kStages & 1);
           for (int i = tid; i < kKeys * (DP / 8); i += kSoft) {
             const int key = i / (DP / 8), c = i % (DP / 8);
             if ((key & BR - 1) >= bl.have[key >> log_br])
