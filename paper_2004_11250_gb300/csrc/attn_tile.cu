@@ -58,7 +58,7 @@ __host__ __device__ constexpr uint32_t idesc(int m, int n, bool b_mn) {
   const uint32_t f = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
   return (1u << 4) | (f << 7) | (f << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-// Products and commits of a whole warp, issued by its leader.  The warp stays together, so that the operands are in
+// Copies, products and commits of a whole warp, issued by its leader.  The warp stays together, so that the operands are in
 // uniform registers, as the instructions want them: behind a branch of one lane each is moved there first, and an issue
 // took some 100 cycles.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t acc, uint32_t leader) {
@@ -79,6 +79,19 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint3
 __device__ __forceinline__ void commit(uint32_t bar, uint32_t leader) {
   asm volatile(
       "{ .reg .pred q; setp.ne.b32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar),
+      "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar, uint32_t leader) {
+  asm volatile(
+      "{ .reg .pred q; setp.ne.b32 q, %5, 0;"
+      " @q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4]; }" ::"r"(dst),
+      "l"(m), "r"(x), "r"(y), "r"(bar), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void expect(uint32_t bar, int bytes, uint32_t leader) {
+  asm volatile(
+      "{ .reg .pred q; setp.ne.b32 q, %2, 0; @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1; }" ::"r"(bar), "r"(bytes),
       "r"(leader)
       : "memory");
 }
@@ -148,6 +161,11 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
   if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
 }
 
+// what a wait comes to that does not find its phase complete at once
+__device__ __noinline__ void hold_on(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (!*dead && !wait(bar, parity)) *dead = 1;
+}
+
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreadsT, 2)
     attn_tile_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
@@ -164,15 +182,15 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       p_full[2], pv_done;
   __shared__ Block info[kInfo];
   __shared__ alignas(8) uint64_t info_full[kInfo];
+  __shared__ int2 found[32];
   __shared__ uint32_t tmem_s;
-  __shared__ int scan[kThreadsT / 32], tile_of[4], found_n, dead;
+  __shared__ int scan[kThreadsT / 32], tile_of[4], dead;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
   // ---- which tile: those of a sequence's last tokens, which see the most keys, come first
   const int TT = kRowsT / p.G.d;  // tokens per tile
   const int h = blockIdx.x % p.H, order = blockIdx.x / p.H;
   if (tid == 0) {
-    found_n = 0;
     dead = 0;
     tile_of[0] = -1;
   }
@@ -264,7 +282,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   const uint32_t tmem = tmem_s;
   // a bounded wait; after one gave up none waits any more
   auto hold = [&](uint64_t* bar, uint32_t parity) {
-    if (!*(volatile int*)&dead && !wait(su32(bar), parity)) *(volatile int*)&dead = 1;
+    if (!mbar_try(su32(bar), parity)) hold_on(su32(bar), parity, &dead);
   };
 
   const T* q = static_cast<const T*>(p.q);
@@ -353,48 +371,58 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     };
 
     if (warp == 4) {
-      // ---- copies.  Pages are looked up 32 pieces at a time, a lane each
-      int have32 = 0, y32 = 0;
-      for (int k = 0; k < n; ++k) {
-        const int g = done + k, st = g % kStages;
-        const uint32_t ph = (g / kStages + 1) & 1;
-        const int in32 = k << log_pc & 31;
-        if (in32 == 0) {
-          const int key = key_of((k << log_pc) + lane);
-          have32 = key < 0 ? 0 : max(0, min(BR, lim_max - key));
-          if (have32 > 0) {
-            const int id = table[key >> p.log_page];
-            if (id < 0 || id >= p.pages) {
-              atomicOr(p.status, PP_CACHE_BAD_PAGE);
-              have32 = 0;
-            }
-            y32 = (int)(((int64_t)id * p.H + h) * p.page) + (key & (p.page - 1));
+      // ---- copies.  Pages are looked up 32 pieces at a time, a lane each; the warp's leader then has the blocks
+      // copied
+      const uint32_t leader = elect();
+      for (int k0 = 0; k0 < n; k0 += 32 >> log_pc) {
+        const int key = key_of((k0 << log_pc) + lane);
+        int have = key < 0 ? 0 : max(0, min(BR, lim_max - key)), y = 0;
+        if (have > 0) {
+          const int id = table[key >> p.log_page];
+          if (id < 0 || id >= p.pages) {
+            atomicOr(p.status, PP_CACHE_BAD_PAGE);
+            have = 0;
           }
-        }
-        const int j = lane & pieces - 1, have = __shfl_sync(~0u, have32, in32 + j), y = __shfl_sync(~0u, y32, in32 + j);
-        const unsigned live = __ballot_sync(~0u, lane < pieces && have > 0);
-        const bool whole = __all_sync(~0u, have == BR);
-        const int bytes = __popc(live) * BR * DP * 2, boxes = pieces * (DP / 64), c = lane >> log_pc;
-        hold(&k_empty[st], ph);
-        // the softmax is done with what was said of block g - 4: the scores of g - 2, just found done, were asked for after it
-        if (lane < pieces) info[g % kInfo].have[lane] = have;
-        if (lane == 0) info[g % kInfo].full = whole;
-        __syncwarp();
-        bool go = !*(volatile int*)&dead;
-        if (lane == 0) {
-          mbar_arrive(su32(&info_full[g % kInfo]));
-          mbar_arrive_expect_tx(su32(&k_full[st]), go ? bytes : 0);
+          y = (int)(((int64_t)id * p.H + h) * p.page) + (key & (p.page - 1));
         }
         __syncwarp();
-        if (go && lane < boxes && (live >> j & 1))
-          copy_box(su32(kbuf + st * S::KV) + c * CHUNK_KV + j * BR * 128, &mk, c * 64, y, su32(&k_full[st]));
-        hold(&v_empty[st], ph);
+        found[lane] = make_int2(have, y);
         __syncwarp();
-        go = !*(volatile int*)&dead;
-        if (lane == 0) mbar_arrive_expect_tx(su32(&v_full[st]), go ? bytes : 0);
+        const int k1 = min(n, k0 + (32 >> log_pc));
+        for (int k = k0; k < k1; ++k) {
+          const int g = done + k, st = g % kStages;
+          const uint32_t ph = (g / kStages + 1) & 1;
+          const int2* at = found + ((k - k0) << log_pc);
+          hold(&k_empty[st], ph);
+          // the softmax is done with what was said of block g - 4: the scores of g - 2, just found done, were asked for after
+          // it
+          int bytes = 0, full = 1;
+          for (int j = 0; j < pieces; ++j) {
+            const int some = at[j].x;
+            if (lane == 0) info[g % kInfo].have[j] = some;
+            full &= some == BR;
+            bytes += some > 0 ? BR * DP * 2 : 0;
+          }
+          if (lane == 0) {
+            info[g % kInfo].full = full;
+            mbar_arrive(su32(&info_full[g % kInfo]));
+          }
+          if (*(volatile int*)&dead) bytes = 0;
+          auto copy = [&](const CUtensorMap* m, uint32_t to, uint32_t bar) {
+            expect(bar, bytes, leader);
+            for (int j = 0; j < pieces; ++j) {
+              const int2 piece = at[j];
+              if (bytes == 0 || piece.x <= 0) continue;
+#pragma unroll
+              for (int c = 0; c < DP / 64; ++c) copy_box(to + c * CHUNK_KV + j * BR * 128, m, c * 64, piece.y, bar, leader);
+            }
+          };
+          copy(&mk, su32(kbuf) + st * S::KV, su32(&k_full[st]));
+          hold(&v_empty[st], ph);
+          if (*(volatile int*)&dead) bytes = 0;
+          copy(&mv, su32(vbuf) + st * S::KV, su32(&v_full[st]));
+        }
         __syncwarp();
-        if (go && lane < boxes && (live >> j & 1))
-          copy_box(su32(vbuf + st * S::KV) + c * CHUNK_KV + j * BR * 128, &mv, c * 64, y, su32(&v_full[st]));
       }
     } else if (warp == 5) {
       // ---- products
