@@ -516,7 +516,8 @@ void pp_rope_destroy(pp_rope* rope);
  *   q, k     views (token stride q_ts, head stride q_hs, ...); Hq or Hk may be 0
  *   q_out    [T][Hq][D], k_out [T][Hk][D]; each may be its own input where that is dense
  * Asynchronous on stream; T = 0 does nothing.  Errors: PP_ERR_INVALID_ARG (null
- * pointer, negative size or stride, dtype, alignment), PP_ERR_CUDA.
+ * pointer, negative size or stride, dtype, alignment), PP_ERR_UNSUPPORTED (more than
+ * 65535 heads), PP_ERR_CUDA.
  */
 pp_status pp_qk_rotate(const pp_rope* rope, int dtype, int T, const int32_t* pos, float eps, const void* q, int64_t q_ts,
                        int64_t q_hs, int Hq, const float* qw, void* q_out, const void* k, int64_t k_ts, int64_t k_hs,

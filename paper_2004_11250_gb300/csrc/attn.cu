@@ -917,7 +917,7 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
   if (units * c.H >= INT32_MAX / deep || (int64_t)T * G >= INT32_MAX) return PP_ERR_UNSUPPORTED;
   AttnParams p = {q,     q_ts,   q_hs,        c.k,        c.v,     starts, table, lens, sel,  out, lse, c.status, c.counters,
                   c.partial, scale, T, B, c.H, c.D, c.page, log2_of(c.page), c.pages, width, keep, flags & PP_ATTN_CAUSAL,
-                  FastDiv(G), FastDiv(c.H)};
+                  FastDiv(G), FastDiv(c.H), FastDiv(std::max(keep, 1))};
   const cudaStream_t s = (cudaStream_t)stream;
   const cudaError_t e = tile_applicable(p, c.dtype, sms) ? tile_launch(p, c, s)
                         : c.dtype == PP_F32 ? by_head<float>(p, c, sms, s)

@@ -25,7 +25,7 @@ struct AttnParams {
   float* partial;  // [CTAs][2] x (16 rows of DP sums, 16 maxima, 16 totals)
   float scale;
   int T, B, H, D, page, log_page, pages, width, keep, causal;
-  FastDiv G, by_head;  // by_head: by H
+  FastDiv G, by_head, by_keep;  // by the group's heads, by H, by keep
 };
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {

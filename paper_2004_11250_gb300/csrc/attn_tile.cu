@@ -326,12 +326,22 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       __syncthreads();
       for (int i = tid; i < wn * words; i += kThreadsT) masks[i] = 0;
       __syncthreads();
-      for (int i = tid; i < nt * p.keep; i += kThreadsT) {
-        const int tk = i / p.keep, e = i - tk * p.keep, Pt = (limit(tk) + p.page - 1) >> p.log_page;
-        if (e >= Pt) continue;
-        const int w = p.sel[((int64_t)(t0 + tk) * p.H + h) * p.keep + e];
-        if (w >= p.width) atomicOr(p.status, PP_CACHE_BAD_PAGE);
-        if (w >= w0 && w < w0 + wn && w < Pt) atomicOr(&masks[(w - w0) * words + tk / 32], 1u << (tk % 32));
+      const int* lists = p.sel + ((int64_t)t0 * p.H + h) * p.keep;
+      constexpr int U = 8;  // entries in flight per thread
+      for (int i0 = tid; i0 < nt * p.keep; i0 += U * kThreadsT) {
+        int tk[U], w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u * kThreadsT;
+          tk[u] = p.by_keep.div(i);
+          w[u] = i < nt * p.keep ? lists[(int64_t)tk[u] * p.H * p.keep + p.by_keep.mod(i)] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int Pt = (limit(tk[u]) + p.page - 1) >> p.log_page, e = p.by_keep.mod(i0 + u * kThreadsT);
+          if (w[u] >= p.width) atomicOr(p.status, PP_CACHE_BAD_PAGE);
+          if (e < Pt && w[u] >= w0 && w[u] < w0 + wn && w[u] < Pt) atomicOr(&masks[(w[u] - w0) * words + tk[u] / 32], 1u << (tk[u] % 32));
+        }
       }
       __syncthreads();
       // the pages that some token uses, in order

@@ -64,7 +64,7 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { retu
 struct FastDiv {
   uint32_t m;
   int shift, d;
-  explicit FastDiv(int by = 1) : m(0), shift(0), d(by) {
+  FastDiv(int by = 1) : m(0), shift(0), d(by) {
     while ((int64_t(1) << shift) < by) ++shift;
     m = (uint32_t)((((uint64_t(1) << shift) - (uint64_t)by) << 32) / (uint64_t)by + 1);
   }

@@ -7,11 +7,12 @@
 // product keeps the exact fraction of a turn whatever the position, and sincospi
 // gets a number in [-1, 1).
 //
-// Bound by device memory (each value read and written once).  A lane holds V
-// pairs of one head, both halves of each (two loads of 16 bytes; one run of 2 V
-// values when interleaved), so the rotation needs no exchange and the mean one
-// butterfly over the group of lanes that share a head.  A group keeps its token
-// over a run of heads, whose sines are computed once, and has U heads in flight.
+// Bound by device memory (each value read and written once).  A lane holds V pairs
+// of one head, both halves of each (two loads of 16 bytes; one run of 2 V values
+// when interleaved), so the rotation needs no exchange and the mean one butterfly
+// over the group of lanes that share a head.  A block has up to J heads per group,
+// of one token or of neighbours: it asks for all of them at once, and while they
+// are under way its threads work out the sines, one each, into shared memory.
 // Rows off 16-byte boundaries, or pairs that do not divide into whole lanes, take
 // the form with single elements, pair j in lane j % 32.
 #include <algorithm>
@@ -21,14 +22,16 @@
 
 #include "cache.h"
 #include "internal.h"
+#include "tc_ptx.cuh"
 
 namespace {
 
 using namespace ppc;
+using namespace ppc_ptx;
 
 constexpr int kThreads = 128;
-constexpr int U = 4;       // heads in flight per group of lanes
-constexpr int kSingle = 4; // pairs per lane of the form with single elements (D / 2 <= 128)
+constexpr int kSingle = 4;    // pairs per lane of the form with single elements (D / 2 <= 128)
+constexpr int kAngles = 2048; // pairs of a block's tokens at most
 
 struct View {
   const void* p;
@@ -45,23 +48,23 @@ struct QkParams {
   const uint8_t* axis;
   int* status;
   int T, Hq, Hk, Hv, D, pairs;
-  int page, H;
+  int page, log_page, H;
   int64_t nslots;
-  int run;            // heads per group of lanes
-  float eps;
+  int64_t items;      // (token, head) pairs
+  int span;           // tokens of a block at most
+  FastDiv heads;      // by the heads of all three
+  float eps, inv_D;
 };
 
 template <class T, bool WIDE>
 constexpr int kPairs = WIDE ? 16 / (int)sizeof(T) : kSingle;
 
-template <class T, bool WIDE, bool INTER, int GROUP>
+template <class T, bool WIDE, bool INTER, int GROUP, int J>
 __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
-  constexpr int V = kPairs<T, WIDE>;
-  const int64_t group = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / GROUP;
-  const int lane = threadIdx.x % GROUP;
-  const int heads = p.Hq + p.Hk + p.Hv, runs = (heads + p.run - 1) / p.run;
-  if (group >= (int64_t)p.T * runs) return;  // whole groups leave: the butterfly below names its own lanes
-  const int t = (int)(group / runs), h0 = (int)(group % runs) * p.run, h1 = min(h0 + p.run, heads);
+  constexpr int V = kPairs<T, WIDE>, W = V / 2, GROUPS = kThreads / GROUP;
+  __shared__ __align__(16) float cosines[kAngles], sines[kAngles];
+  __shared__ __align__(16) float weights[2][256];
+  const int lane = threadIdx.x % GROUP, grp = threadIdx.x / GROUP;
   const unsigned mask = GROUP == 32 ? 0xFFFFFFFFu : ((1u << (GROUP & 31)) - 1u) << (threadIdx.x % 32 / GROUP * GROUP);
   const int half = p.D / 2, R = half - p.pairs;
   // pair i of the lane; beyond the rotated ones, what is not turned as pairs of its own two halves
@@ -69,147 +72,172 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
   auto first = [&](int j) { return INTER ? 2 * j : j < p.pairs ? j : p.pairs + j; };
   auto second = [&](int j) { return INTER ? 2 * j + 1 : j < p.pairs ? p.pairs + j : p.pairs + j + R; };
   const bool on = pair(0) < half;
+  auto valid = [&](int i) { return WIDE ? on : pair(i) < half; };
   const int ia = first(pair(0)), ib = INTER ? ia + V : second(pair(0));  // WIDE: where the lane's two runs begin
+  // element k of pair i in the lane's two vectors: (vector, place)
+  auto vec_of = [](int i, int k) { return WIDE && INTER ? (2 * i + k) / V : k; };
+  auto place_of = [](int i, int k) { return WIDE && INTER ? (2 * i + k) % V : i; };
 
-  float cs[V], sn[V];
+  // ---- the heads' values are asked for
+  const int64_t i0 = (int64_t)blockIdx.x * GROUPS * J;
+  const int t0 = (int)(i0 / p.heads.d), rest = (int)(i0 - (int64_t)t0 * p.heads.d);  // the first item's token, and its head
+  Vec<T, V> ab[J][2];
+  T* to[J];
+  int tok[J], part[J];
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    cs[i] = 1.f;
-    sn[i] = 0.f;
-    const int j = pair(i);
-    if (h0 < p.Hq + p.Hk && j < p.pairs) {
-      const int64_t at = p.pos[(int64_t)p.axis[j] * p.T + t];
-      const uint64_t f = (uint64_t)at * p.turn[j];
-      sincospif((float)(int32_t)(f >> 32) * 0x1p-31f, &sn[i], &cs[i]);
+  for (int j = 0; j < J; ++j) {
+    const int i = rest + grp + j * GROUPS;
+    tok[j] = p.heads.div(i);
+    int h = i - tok[j] * p.heads.d;
+    const int64_t t = t0 + tok[j];
+    part[j] = h < p.Hq ? 0 : h < p.Hq + p.Hk ? 1 : 2;
+    to[j] = nullptr;
+    if (i0 + grp + j * GROUPS >= p.items) {
+      part[j] = 3;
+      continue;
+    }
+    h -= part[j] == 0 ? 0 : part[j] == 1 ? p.Hq : p.Hq + p.Hk;
+    if (part[j] == 0) {
+      to[j] = static_cast<T*>(p.qo) + (t * p.Hq + h) * p.D;
+    } else if (part[j] == 1 && p.ko) {
+      to[j] = static_cast<T*>(p.ko) + (t * p.Hk + h) * p.D;
+    } else {
+      const int64_t slot = p.slots[t];
+      if (slot >= 0 && slot < p.nslots) {
+        const int64_t page = slot >> p.log_page;
+        to[j] = static_cast<T*>(part[j] == 1 ? p.ck : p.cv) + (((page * p.H + h) << p.log_page) + (slot & (p.page - 1))) * p.D;
+      } else if (slot != -1 && lane == 0) {
+        atomicOr(p.status, PP_CACHE_BAD_SLOT);
+      }
+    }
+    if (!on || !to[j]) continue;
+    const View& x = p.x[part[j]];
+    const T* from = static_cast<const T*>(x.p) + t * x.ts + h * x.hs;
+    if (WIDE) {
+      ab[j][0] = *reinterpret_cast<const Vec<T, V>*>(from + ia);
+      ab[j][1] = *reinterpret_cast<const Vec<T, V>*>(from + ib);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (pair(i) < half) {
+          ab[j][0].v[i] = from[first(pair(i))];
+          ab[j][1].v[i] = from[second(pair(i))];
+        }
     }
   }
-  int64_t slot = -1;
-  if (p.slots) {
-    slot = p.slots[t];
-    if (slot >= p.nslots || slot < -1) {
-      if (lane == 0) atomicOr(p.status, PP_CACHE_BAD_SLOT);
-      slot = -1;
-    }
+  // ---- meanwhile the sines of the block's tokens, and the weights
+  for (int i = threadIdx.x; i < p.span * p.pairs; i += kThreads) {
+    const int tk = i / p.pairs, j = i - tk * p.pairs;
+    if (t0 + tk >= p.T) break;
+    const int64_t at = p.pos[(int64_t)p.axis[j] * p.T + t0 + tk];
+    const uint64_t f = (uint64_t)at * p.turn[j];
+    sincospif((float)(int32_t)(f >> 32) * 0x1p-31f, &sines[i], &cosines[i]);
   }
-  const int64_t cell = slot < 0 ? 0 : (slot / p.page * p.H * p.page + slot % p.page) * p.D;
-
-  for (int hb = h0; hb < h1; hb += U) {
-    Vec<T, V> a[U], b[U];
+  for (int i = threadIdx.x; i < 2 * p.D; i += kThreads) {
+    const int k = i >= p.D, d = i - k * p.D;
+    weights[k][d] = p.w[k] ? p.w[k][d] : 1.f;
+  }
+  __syncthreads();
+  // ---- each head, its V pairs as packs of two for the two-way fp32 instructions
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = hb + u;
-      if (h >= h1 || !on) continue;
-      const int part = h < p.Hq ? 0 : h < p.Hq + p.Hk ? 1 : 2;
-      const int hh = part == 0 ? h : part == 1 ? h - p.Hq : h - p.Hq - p.Hk;
-      const T* x = static_cast<const T*>(p.x[part].p) + t * p.x[part].ts + hh * p.x[part].hs;
-      if (WIDE) {
-        a[u] = *reinterpret_cast<const Vec<T, V>*>(x + ia);
-        b[u] = *reinterpret_cast<const Vec<T, V>*>(x + ib);
-      } else {
+  for (int j = 0; j < J; ++j) {
+    if (part[j] < 2) {  // the same for a group
+      uint64_t fa[W], fb[W], s2 = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int j = pair(i);
-          if (j < half) {
-            a[u].v[i] = x[first(j)];
-            b[u].v[i] = x[second(j)];
-          }
+      for (int i = 0; i < W; ++i) {
+        float v[2][2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            v[k][e] = valid(2 * i + e) ? to_f32(ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)]) : 0.f;
+        fa[i] = pack2(v[0][0], v[0][1]);
+        fb[i] = pack2(v[1][0], v[1][1]);
+        s2 = fma2(fa[i], fa[i], s2);
+        s2 = fma2(fb[i], fb[i], s2);
+      }
+      if (p.eps >= 0.f) {
+        float s, s1;
+        unpack2(s2, s, s1);
+        s += s1;
+#pragma unroll
+        for (int d = GROUP / 2; d > 0; d >>= 1) s += __shfl_xor_sync(mask, s, d);
+        const float r = rsqrtf(s * p.inv_D + p.eps);
+        const uint64_t r2 = pack2(r, r);
+        const float* w = weights[part[j]];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const int pa = pair(2 * i), pb = pair(2 * i + 1);
+          const bool va = valid(2 * i), vb = valid(2 * i + 1);
+          fa[i] = mul2(mul2(fa[i], r2), pack2(va ? w[first(pa)] : 1.f, vb ? w[first(pb)] : 1.f));
+          fb[i] = mul2(mul2(fb[i], r2), pack2(va ? w[second(pa)] : 1.f, vb ? w[second(pb)] : 1.f));
         }
+      }
+      const float *cs = cosines + tok[j] * p.pairs, *sn = sines + tok[j] * p.pairs;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        float c[2], n[2], v[2][2], o[2][2];
+        bool turned[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          turned[e] = pair(2 * i + e) < p.pairs;  // the others stay as they are, infinities too
+          c[e] = turned[e] ? cs[pair(2 * i + e)] : 1.f;
+          n[e] = turned[e] ? sn[pair(2 * i + e)] : 0.f;
+        }
+        const uint64_t c2 = pack2(c[0], c[1]), n2 = pack2(n[0], n[1]), m2 = pack2(-n[0], -n[1]);
+        unpack2(fma2(fb[i], m2, mul2(fa[i], c2)), v[0][0], v[0][1]);
+        unpack2(fma2(fa[i], n2, mul2(fb[i], c2)), v[1][0], v[1][1]);
+        unpack2(fa[i], o[0][0], o[0][1]);
+        unpack2(fb[i], o[1][0], o[1][1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)] = from_f32<T>(turned[e] ? v[k][e] : o[k][e]);
       }
     }
+    if (!on || !to[j]) continue;
+    if (WIDE) {
+      *reinterpret_cast<Vec<T, V>*>(to[j] + ia) = ab[j][0];
+      *reinterpret_cast<Vec<T, V>*>(to[j] + ib) = ab[j][1];
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = hb + u;
-      if (h >= h1) continue;
-      const int part = h < p.Hq ? 0 : h < p.Hq + p.Hk ? 1 : 2;
-      const int hh = part == 0 ? h : part == 1 ? h - p.Hq : h - p.Hq - p.Hk;
-      if (part < 2) {
-        float fa[V], fb[V];  // WIDE and INTER: the first V and the last V of the lane's 2 V values
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const bool in = WIDE ? on : pair(i) < half;
-          fa[i] = in ? to_f32(a[u].v[i]) : 0.f;
-          fb[i] = in ? to_f32(b[u].v[i]) : 0.f;
+      for (int i = 0; i < V; ++i)
+        if (pair(i) < half) {
+          to[j][first(pair(i))] = ab[j][0].v[i];
+          to[j][second(pair(i))] = ab[j][1].v[i];
         }
-        if (p.eps >= 0.f) {
-          float s = 0.f;
-#pragma unroll
-          for (int i = 0; i < V; ++i) s += fa[i] * fa[i] + fb[i] * fb[i];
-#pragma unroll
-          for (int d = GROUP / 2; d > 0; d >>= 1) s += __shfl_xor_sync(mask, s, d);
-          const float r = rsqrtf(s / (float)p.D + p.eps);
-          const float* w = p.w[part];
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const bool in = w && (WIDE ? on : pair(i) < half);
-            fa[i] *= r * (in ? w[WIDE ? ia + i : first(pair(i))] : 1.f);
-            fb[i] *= r * (in ? w[WIDE ? ib + i : second(pair(i))] : 1.f);
-          }
-        }
-        float ra[V], rb[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          // element of a pair in the lane's run of 2 V values
-          const float x0 = !(WIDE && INTER) ? fa[i] : 2 * i < V ? fa[(2 * i) % V] : fb[(2 * i) % V];
-          const float x1 = !(WIDE && INTER) ? fb[i] : 2 * i < V ? fa[(2 * i + 1) % V] : fb[(2 * i + 1) % V];
-          const bool turned = pair(i) < p.pairs;  // the others stay as they are, infinities too
-          ra[i] = turned ? x0 * cs[i] - x1 * sn[i] : x0;
-          rb[i] = turned ? x1 * cs[i] + x0 * sn[i] : x1;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int k = WIDE && INTER ? 2 * i : i, l = WIDE && INTER ? 2 * i + 1 : i;
-          (k < V ? a : b)[u].v[k % V] = from_f32<T>(ra[i]);
-          (WIDE && INTER ? (l < V ? a : b) : b)[u].v[l % V] = from_f32<T>(rb[i]);
-        }
-      }
-      T* y;
-      if (part == 0)
-        y = static_cast<T*>(p.qo) + ((int64_t)t * p.Hq + hh) * p.D;
-      else if (part == 1 && p.ko)
-        y = static_cast<T*>(p.ko) + ((int64_t)t * p.Hk + hh) * p.D;
-      else
-        y = slot < 0 ? nullptr : static_cast<T*>(part == 1 ? p.ck : p.cv) + cell + (int64_t)hh * p.page * p.D;
-      if (!on || !y) continue;
-      if (WIDE) {
-        *reinterpret_cast<Vec<T, V>*>(y + ia) = a[u];
-        *reinterpret_cast<Vec<T, V>*>(y + ib) = b[u];
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int j = pair(i);
-          if (j < half) {
-            y[first(j)] = a[u].v[i];
-            y[second(j)] = b[u].v[i];
-          }
-        }
-      }
     }
   }
 }
 
-template <class T, bool WIDE, bool INTER, int GROUP>
-cudaError_t launch(QkParams p, cudaStream_t stream, int sms) {
-  // Runs of heads: whole tokens when there are enough of them to fill the GPU (the sines are then computed once per
-  // token), else as few heads per group as give every SM about 512 threads.
-  const int heads = p.Hq + p.Hk + p.Hv;
-  const int64_t want = (int64_t)sms * 512 / GROUP;
-  const int64_t runs = std::min<int64_t>(heads, std::max<int64_t>(1, (want + p.T - 1) / p.T));
-  p.run = (int)((heads + runs - 1) / runs);
-  const int64_t groups = (int64_t)p.T * ((heads + p.run - 1) / p.run);
-  const int64_t blocks = (groups * GROUP + kThreads - 1) / kThreads;
+template <class T, bool WIDE, bool INTER, int GROUP, int J>
+cudaError_t launch(QkParams p, cudaStream_t stream) {
+  const int per = kThreads / GROUP * J;
+  p.span = (per - 1) / p.heads.d + 2;
+  const int64_t blocks = (p.items + per - 1) / per;
   if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-  qk_kernel<T, WIDE, INTER, GROUP><<<(unsigned)blocks, kThreads, 0, stream>>>(p);
+  qk_kernel<T, WIDE, INTER, GROUP, J><<<(unsigned)blocks, kThreads, 0, stream>>>(p);
   return cudaGetLastError();
+}
+
+// Four heads per group of lanes where that still gives every SM 8 blocks and the angles fit, else one: more blocks for
+// few heads, whose latency counts.
+template <class T, bool WIDE, bool INTER, int GROUP>
+cudaError_t by_items(const QkParams& p, cudaStream_t stream, int sms) {
+  constexpr int J = 4, per = kThreads / GROUP * J;
+  const bool many = p.items >= (int64_t)sms * 8 * per && ((per - 1) / p.heads.d + 2) * (int64_t)p.pairs <= kAngles;
+  return many ? launch<T, WIDE, INTER, GROUP, J>(p, stream) : launch<T, WIDE, INTER, GROUP, 1>(p, stream);
 }
 
 template <class T, bool INTER>
 cudaError_t by_group(const QkParams& p, bool wide, cudaStream_t stream, int sms) {
-  if (!wide) return launch<T, false, INTER, 32>(p, stream, sms);
+  if (!wide) return by_items<T, false, INTER, 32>(p, stream, sms);
   const int lanes = p.D / 2 / kPairs<T, true>;
-  if (lanes <= 4) return launch<T, true, INTER, 4>(p, stream, sms);
-  if (lanes <= 8) return launch<T, true, INTER, 8>(p, stream, sms);
-  if (lanes <= 16) return launch<T, true, INTER, 16>(p, stream, sms);
-  return launch<T, true, INTER, 32>(p, stream, sms);
+  if (lanes <= 4) return by_items<T, true, INTER, 4>(p, stream, sms);
+  if (lanes <= 8) return by_items<T, true, INTER, 8>(p, stream, sms);
+  if (lanes <= 16) return by_items<T, true, INTER, 16>(p, stream, sms);
+  return by_items<T, true, INTER, 32>(p, stream, sms);
 }
 
 template <class T>
@@ -221,12 +249,16 @@ bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) &
 
 pp_status run(const pp_rope* rope, int dtype, QkParams& p, void* stream) {
   if (p.T == 0 || p.Hq + p.Hk + p.Hv == 0) return PP_OK;
+  if ((int64_t)p.Hq + p.Hk + p.Hv > 65535) return PP_ERR_UNSUPPORTED;
   const size_t e = (size_t)dtype_size(dtype);
   const int n[3] = {p.Hq, p.Hk, p.Hv};
   const int W = 16 / (int)e;
   p.turn = rope->turn;
   p.axis = rope->axis;
   p.D = rope->D;
+  p.inv_D = 1.f / (float)rope->D;
+  p.items = (int64_t)p.T * (p.Hq + p.Hk + p.Hv);
+  p.heads = FastDiv(p.Hq + p.Hk + p.Hv);
   p.pairs = rope->pairs;
   bool wide = p.pairs % W == 0 && p.D / 2 % W == 0;
   for (int i = 0; i < 3; ++i) {
@@ -344,6 +376,7 @@ pp_status pp_qkv_store(const pp_rope* rope, const pp_cache* cache, int T, const 
   p.Hq = Hq;
   p.Hk = p.Hv = cache->H;
   p.page = cache->page;
+  p.log_page = log2_of(cache->page);
   p.H = cache->H;
   p.nslots = (int64_t)cache->pages * cache->page;
   p.eps = eps;
