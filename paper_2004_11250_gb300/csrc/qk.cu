@@ -59,6 +59,24 @@ struct QkParams {
 template <class T, bool WIDE>
 constexpr int kPairs = WIDE ? 16 / (int)sizeof(T) : kSingle;
 
+// Where entry e of n lies in shared memory.  A lane reads V consecutive ones, 16 bytes at a time: with V = 8 the first
+// four of all lanes come first, then the other four, so that neighbours read neighbouring words.
+template <int V>
+__device__ __forceinline__ int place(int e, int n) {
+  return V == 8 ? (e >> 2 & 1) * (n / 2) + (e >> 3) * 4 + (e & 3) : e;
+}
+template <int V>
+__device__ __forceinline__ void read_run(const float* from, int e, int n, float* to) {
+#pragma unroll
+  for (int i = 0; i < V; i += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(from + place<V>(e + i, n));
+    to[i] = v.x;
+    to[i + 1] = v.y;
+    to[i + 2] = v.z;
+    to[i + 3] = v.w;
+  }
+}
+
 template <class T, bool WIDE, bool INTER, int GROUP, int J>
 __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
   constexpr int V = kPairs<T, WIDE>, W = V / 2, GROUPS = kThreads / GROUP;
@@ -131,11 +149,12 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
     if (t0 + tk >= p.T) break;
     const int64_t at = p.pos[(int64_t)p.axis[j] * p.T + t0 + tk];
     const uint64_t f = (uint64_t)at * p.turn[j];
-    sincospif((float)(int32_t)(f >> 32) * 0x1p-31f, &sines[i], &cosines[i]);
+    const int to = tk * p.pairs + (WIDE ? place<V>(j, p.pairs) : j);
+    sincospif((float)(int32_t)(f >> 32) * 0x1p-31f, &sines[to], &cosines[to]);
   }
   for (int i = threadIdx.x; i < 2 * p.D; i += kThreads) {
     const int k = i >= p.D, d = i - k * p.D;
-    weights[k][d] = p.w[k] ? p.w[k][d] : 1.f;
+    weights[k][WIDE ? place<V>(d, p.D) : d] = p.w[k] ? p.w[k][d] : 1.f;
   }
   __syncthreads();
   // ---- each head, its V pairs as packs of two for the two-way fp32 instructions
@@ -150,50 +169,80 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            v[k][e] = valid(2 * i + e) ? to_f32(ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)]) : 0.f;
+            v[k][e] = valid(2 * i + e) && to[j] ? to_f32(ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)]) : 0.f;
         fa[i] = pack2(v[0][0], v[0][1]);
         fb[i] = pack2(v[1][0], v[1][1]);
         s2 = fma2(fa[i], fa[i], s2);
         s2 = fma2(fb[i], fb[i], s2);
       }
       if (p.eps >= 0.f) {
-        float s, s1;
+        float s, s1, w[2 * V];  // the weights in the order of the lane's two vectors
         unpack2(s2, s, s1);
         s += s1;
 #pragma unroll
         for (int d = GROUP / 2; d > 0; d >>= 1) s += __shfl_xor_sync(mask, s, d);
         const float r = rsqrtf(s * p.inv_D + p.eps);
         const uint64_t r2 = pack2(r, r);
-        const float* w = weights[part[j]];
+        if (WIDE) {
+          read_run<V>(weights[part[j]], on ? ia : 0, p.D, w);
+          read_run<V>(weights[part[j]], on ? ib : 0, p.D, w + V);
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            w[i] = valid(i) ? weights[part[j]][first(pair(i))] : 1.f;
+            w[V + i] = valid(i) ? weights[part[j]][second(pair(i))] : 1.f;
+          }
+        }
+        auto weight = [&](int i, int k) { return w[vec_of(i, k) * V + place_of(i, k)]; };
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          const int pa = pair(2 * i), pb = pair(2 * i + 1);
-          const bool va = valid(2 * i), vb = valid(2 * i + 1);
-          fa[i] = mul2(mul2(fa[i], r2), pack2(va ? w[first(pa)] : 1.f, vb ? w[first(pb)] : 1.f));
-          fb[i] = mul2(mul2(fb[i], r2), pack2(va ? w[second(pa)] : 1.f, vb ? w[second(pb)] : 1.f));
+          fa[i] = mul2(mul2(fa[i], r2), pack2(weight(2 * i, 0), weight(2 * i + 1, 0)));
+          fb[i] = mul2(mul2(fb[i], r2), pack2(weight(2 * i, 1), weight(2 * i + 1, 1)));
         }
       }
-      const float *cs = cosines + tok[j] * p.pairs, *sn = sines + tok[j] * p.pairs;
+      // WIDE: a lane's pairs are turned all or not at all.  Those that are not stay as they are, infinities too
+      if (WIDE ? pair(0) < p.pairs : true) {
+        float c[V], n[V];
+        if (WIDE) {
+          read_run<V>(cosines + tok[j] * p.pairs, pair(0), p.pairs, c);
+          read_run<V>(sines + tok[j] * p.pairs, pair(0), p.pairs, n);
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            c[i] = pair(i) < p.pairs ? cosines[tok[j] * p.pairs + pair(i)] : 1.f;
+            n[i] = pair(i) < p.pairs ? sines[tok[j] * p.pairs + pair(i)] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const uint64_t c2 = pack2(c[2 * i], c[2 * i + 1]), n2 = pack2(n[2 * i], n[2 * i + 1]);
+          const uint64_t ra = fma2(fb[i], pack2(-n[2 * i], -n[2 * i + 1]), mul2(fa[i], c2));
+          const uint64_t rb = fma2(fa[i], n2, mul2(fb[i], c2));
+          if (WIDE) {
+            fa[i] = ra;
+            fb[i] = rb;
+          } else {
+            float v[2][2], o[2][2];
+            unpack2(ra, v[0][0], v[0][1]);
+            unpack2(rb, v[1][0], v[1][1]);
+            unpack2(fa[i], o[0][0], o[0][1]);
+            unpack2(fb[i], o[1][0], o[1][1]);
+            const bool t0 = pair(2 * i) < p.pairs, t1 = pair(2 * i + 1) < p.pairs;
+            fa[i] = pack2(t0 ? v[0][0] : o[0][0], t1 ? v[0][1] : o[0][1]);
+            fb[i] = pack2(t0 ? v[1][0] : o[1][0], t1 ? v[1][1] : o[1][1]);
+          }
+        }
+      }
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        float c[2], n[2], v[2][2], o[2][2];
-        bool turned[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          turned[e] = pair(2 * i + e) < p.pairs;  // the others stay as they are, infinities too
-          c[e] = turned[e] ? cs[pair(2 * i + e)] : 1.f;
-          n[e] = turned[e] ? sn[pair(2 * i + e)] : 0.f;
-        }
-        const uint64_t c2 = pack2(c[0], c[1]), n2 = pack2(n[0], n[1]), m2 = pack2(-n[0], -n[1]);
-        unpack2(fma2(fb[i], m2, mul2(fa[i], c2)), v[0][0], v[0][1]);
-        unpack2(fma2(fa[i], n2, mul2(fb[i], c2)), v[1][0], v[1][1]);
-        unpack2(fa[i], o[0][0], o[0][1]);
-        unpack2(fb[i], o[1][0], o[1][1]);
+        float v[2][2];
+        unpack2(fa[i], v[0][0], v[0][1]);
+        unpack2(fb[i], v[1][0], v[1][1]);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)] = from_f32<T>(turned[e] ? v[k][e] : o[k][e]);
+            ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)] = from_f32<T>(v[k][e]);
       }
     }
     if (!on || !to[j]) continue;
