@@ -46,14 +46,6 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-template <class T>
-__device__ __forceinline__ uint32_t pack(float a, float b) {
-  T v[2] = {from_f32<T>(a), from_f32<T>(b)};
-  uint32_t r;
-  memcpy(&r, v, 4);
-  return r;
-}
-
 // attn_tile.cu: tiles of 128 query rows on the tensor cores, for 16-bit types and heads of up to 128.
 bool tile_applicable(const AttnParams& p, int dtype, int sms);
 cudaError_t tile_prepare();

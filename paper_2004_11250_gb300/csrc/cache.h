@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "ppconv.h"
 
@@ -84,6 +85,38 @@ template <class T, int V>
 struct alignas(sizeof(T) * V) Vec {
   T v[V];
 };
+
+// Two neighbours of a vector at once, as the word that holds them: one conversion instruction where the type has one for
+// two (bf16 to fp32 is a shift or a mask).
+template <class T, int V>
+__device__ __forceinline__ float2 get2(const Vec<T, V>& a, int i) {
+  if constexpr (sizeof(T) == 4) {
+    return make_float2(a.v[2 * i], a.v[2 * i + 1]);
+  } else {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&a)[i];
+    if constexpr (std::is_same<T, __half>::value) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  }
+}
+template <class T>
+__device__ __forceinline__ uint32_t pack(float x, float y) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+template <class T, int V>
+__device__ __forceinline__ void put2(Vec<T, V>& a, int i, float x, float y) {
+  if constexpr (sizeof(T) == 4) {
+    a.v[2 * i] = x;
+    a.v[2 * i + 1] = y;
+  } else {
+    reinterpret_cast<uint32_t*>(&a)[i] = pack<T>(x, y);
+  }
+}
 
 // A token of a call on the cache: its sequence and how many of that sequence's keys it sees.
 struct Seen {

@@ -80,8 +80,8 @@ __device__ __forceinline__ void read_run(const float* from, int e, int n, float*
 template <class T, bool WIDE, bool INTER, int GROUP, int J>
 __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
   constexpr int V = kPairs<T, WIDE>, W = V / 2, GROUPS = kThreads / GROUP;
-  __shared__ __align__(16) float cosines[kAngles], sines[kAngles];
-  __shared__ __align__(16) float weights[2][256];
+  extern __shared__ __align__(16) float shared[];  // weights of queries and keys, then the span's cosines and its sines
+  float *weights = shared, *cosines = shared + 2 * p.D, *sines = cosines + p.span * p.pairs;
   const int lane = threadIdx.x % GROUP, grp = threadIdx.x / GROUP;
   const unsigned mask = GROUP == 32 ? 0xFFFFFFFFu : ((1u << (GROUP & 31)) - 1u) << (threadIdx.x % 32 / GROUP * GROUP);
   const int half = p.D / 2, R = half - p.pairs;
@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
     const int64_t t = t0 + tok[j];
     part[j] = h < p.Hq ? 0 : h < p.Hq + p.Hk ? 1 : 2;
     to[j] = nullptr;
+    ab[j][0] = ab[j][1] = {};
     if (i0 + grp + j * GROUPS >= p.items) {
       part[j] = 3;
       continue;
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
   }
   for (int i = threadIdx.x; i < 2 * p.D; i += kThreads) {
     const int k = i >= p.D, d = i - k * p.D;
-    weights[k][WIDE ? place<V>(d, p.D) : d] = p.w[k] ? p.w[k][d] : 1.f;
+    weights[k * p.D + (WIDE ? place<V>(d, p.D) : d)] = p.w[k] ? p.w[k][d] : 1.f;
   }
   __syncthreads();
   // ---- each head, its V pairs as packs of two for the two-way fp32 instructions
@@ -164,14 +165,15 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
       uint64_t fa[W], fb[W], s2 = 0;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        float v[2][2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            v[k][e] = valid(2 * i + e) && to[j] ? to_f32(ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)]) : 0.f;
-        fa[i] = pack2(v[0][0], v[0][1]);
-        fb[i] = pack2(v[1][0], v[1][1]);
+        if (WIDE && INTER) {  // a neighbour pair is a pair of the rotation
+          const float2 x = get2(ab[j][4 * i / V], 2 * i % W), y = get2(ab[j][4 * i / V], (2 * i + 1) % W);
+          fa[i] = pack2(x.x, y.x);
+          fb[i] = pack2(x.y, y.y);
+        } else {
+          const float2 x = get2(ab[j][0], i), y = get2(ab[j][1], i);
+          fa[i] = pack2(x.x, x.y);
+          fb[i] = pack2(y.x, y.y);
+        }
         s2 = fma2(fa[i], fa[i], s2);
         s2 = fma2(fb[i], fb[i], s2);
       }
@@ -184,13 +186,13 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
         const float r = rsqrtf(s * p.inv_D + p.eps);
         const uint64_t r2 = pack2(r, r);
         if (WIDE) {
-          read_run<V>(weights[part[j]], on ? ia : 0, p.D, w);
-          read_run<V>(weights[part[j]], on ? ib : 0, p.D, w + V);
+          read_run<V>(weights + part[j] * p.D, on ? ia : 0, p.D, w);
+          read_run<V>(weights + part[j] * p.D, on ? ib : 0, p.D, w + V);
         } else {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            w[i] = valid(i) ? weights[part[j]][first(pair(i))] : 1.f;
-            w[V + i] = valid(i) ? weights[part[j]][second(pair(i))] : 1.f;
+            w[i] = valid(i) ? weights[part[j] * p.D + first(pair(i))] : 1.f;
+            w[V + i] = valid(i) ? weights[part[j] * p.D + second(pair(i))] : 1.f;
           }
         }
         auto weight = [&](int i, int k) { return w[vec_of(i, k) * V + place_of(i, k)]; };
@@ -238,11 +240,13 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
         float v[2][2];
         unpack2(fa[i], v[0][0], v[0][1]);
         unpack2(fb[i], v[1][0], v[1][1]);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            ab[j][vec_of(2 * i + e, k)].v[place_of(2 * i + e, k)] = from_f32<T>(v[k][e]);
+        if (WIDE && INTER) {
+          put2(ab[j][4 * i / V], 2 * i % W, v[0][0], v[1][0]);
+          put2(ab[j][4 * i / V], (2 * i + 1) % W, v[0][1], v[1][1]);
+        } else {
+          put2(ab[j][0], i, v[0][0], v[0][1]);
+          put2(ab[j][1], i, v[1][0], v[1][1]);
+        }
       }
     }
     if (!on || !to[j]) continue;
@@ -266,15 +270,16 @@ cudaError_t launch(QkParams p, cudaStream_t stream) {
   p.span = (per - 1) / p.heads.d + 2;
   const int64_t blocks = (p.items + per - 1) / per;
   if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-  qk_kernel<T, WIDE, INTER, GROUP, J><<<(unsigned)blocks, kThreads, 0, stream>>>(p);
+  const size_t shared = (2 * (size_t)p.D + 2 * (size_t)p.span * p.pairs) * 4;
+  qk_kernel<T, WIDE, INTER, GROUP, J><<<(unsigned)blocks, kThreads, shared, stream>>>(p);
   return cudaGetLastError();
 }
 
-// Four heads per group of lanes where that still gives every SM 8 blocks and the angles fit, else one: more blocks for
+// Two heads per group of lanes where that still gives every SM 8 blocks and the angles fit, else one: more blocks for
 // few heads, whose latency counts.
 template <class T, bool WIDE, bool INTER, int GROUP>
 cudaError_t by_items(const QkParams& p, cudaStream_t stream, int sms) {
-  constexpr int J = 4, per = kThreads / GROUP * J;
+  constexpr int J = 2, per = kThreads / GROUP * J;
   const bool many = p.items >= (int64_t)sms * 8 * per && ((per - 1) / p.heads.d + 2) * (int64_t)p.pairs <= kAngles;
   return many ? launch<T, WIDE, INTER, GROUP, J>(p, stream) : launch<T, WIDE, INTER, GROUP, 1>(p, stream);
 }
