@@ -29,9 +29,9 @@ namespace {
 using namespace ppc;
 using namespace ppc_ptx;
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 256;
 constexpr int kSingle = 4;    // pairs per lane of the form with single elements (D / 2 <= 128)
-constexpr int kAngles = 2048; // pairs of a block's tokens at most
+constexpr int kAngles = 4096; // pairs of a block's tokens at most
 
 struct View {
   const void* p;

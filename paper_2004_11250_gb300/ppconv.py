@@ -443,29 +443,48 @@ def pp_net_destroy(net):
 # ------------------------------------------------------------------ decoder operators
 
 
+class _Types:
+    """torch's types and the library's codes of them, made at the first use (the convolutions need no torch)."""
+
+    def __init__(self):
+        import torch
+        self.code = {torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16}
+        self.f32, self.i32, self.i8 = torch.float32, torch.int32, torch.int8
+
+
+_types: Optional[_Types] = None
+
+
+def _torch_types() -> _Types:
+    global _types
+    if _types is None:
+        _types = _Types()
+    return _types
+
+
 def _dtype(t) -> int:
-    """The library's type code of a tensor; PP_ERR_INVALID_ARG for types it does not take."""
-    name = str(t.dtype)
+    """The library's code of a tensor's type; PP_ERR_INVALID_ARG for types it does not take."""
     try:
-        return {"torch.float32": PP_F32, "torch.float16": PP_F16, "torch.bfloat16": PP_BF16}[name]
+        return _torch_types().code[t.dtype]
     except KeyError:
-        raise PPError(PP_ERR_INVALID_ARG, f"dtype {name}") from None
+        raise PPError(PP_ERR_INVALID_ARG, f"dtype {t.dtype}") from None
 
 
 def _heads(t, dtype, T, D):
-    """(pointer, token stride, head stride, heads) of a view [T][heads][D]; None is no heads."""
+    """(pointer, token stride, head stride, heads) of a view [T][heads][D] of torch type dtype; None is no heads."""
     if t is None:
         return None, 0, 0, 0
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or (t.stride(2) != 1 and D > 1) or _dtype(t) != dtype:
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype or len(shape) != 3 or shape[0] != T or shape[2] != D or stride[2] != 1:
         raise PPError(PP_ERR_INVALID_ARG, "a token tensor is [T][heads][D] of the call's type, dense in D")
-    return t.data_ptr(), t.stride(0), t.stride(1), t.shape[1]
+    return t.data_ptr(), stride[0], stride[1], shape[1]
 
 
 def _dense(t, shape, dtype, where):
-    """Pointer of a dense tensor of this shape and torch type name."""
+    """Pointer of a dense tensor of this shape and torch type; None stays NULL."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or str(t.dtype) != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise PPError(PP_ERR_INVALID_ARG, f"{where}: expected a dense {dtype} of {tuple(shape)}")
     return t.data_ptr()
 
@@ -478,7 +497,7 @@ class Rope(int):
 
 class Cache(int):
     """A cache's handle with what the binding checks shapes by; it keeps the pools alive."""
-    dtype: int
+    dtype: object
     shape: tuple
 
 
@@ -503,14 +522,14 @@ def pp_rope_destroy(rope):
 def pp_qk_rotate(rope, pos, eps, q, qw, q_out, k, kw, k_out, stream=None):
     """q [T][Hq][D], k [T][Hk][D] (either may be None) normalised and rotated into q_out, k_out; pos [axes][T] int32."""
     x = q if q is not None else k
-    T, D, dt = x.shape[0], rope.D, _dtype(x)
-    name = str(x.dtype)
+    T, D, code, y = x.shape[0], rope.D, _dtype(x), _torch_types()
+    dt = x.dtype
     qp, qt, qh, Hq = _heads(q, dt, T, D)
     kp, kt, kh, Hk = _heads(k, dt, T, D)
-    _check(lib.pp_qk_rotate(rope, dt, T, _dense(pos, (rope.axes, T), "torch.int32", "pos"), eps, qp, qt, qh, Hq,
-                            _dense(qw, (D,), "torch.float32", "qw"), _dense(q_out, (T, Hq, D), name, "q_out"), kp, kt,
-                            kh, Hk, _dense(kw, (D,), "torch.float32", "kw"), _dense(k_out, (T, Hk, D), name, "k_out"),
-                            _stream(stream)), "pp_qk_rotate")
+    _check(lib.pp_qk_rotate(rope, code, T, _dense(pos, (rope.axes, T), y.i32, "pos"), eps, qp, qt, qh, Hq,
+                            _dense(qw, (D,), y.f32, "qw"), _dense(q_out, (T, Hq, D), dt, "q_out"), kp, kt, kh, Hk,
+                            _dense(kw, (D,), y.f32, "kw"), _dense(k_out, (T, Hk, D), dt, "k_out"), _stream(stream)),
+           "pp_qk_rotate")
 
 
 def pp_cache_create(k, v, codes=None, scales=None) -> Cache:
@@ -518,14 +537,13 @@ def pp_cache_create(k, v, codes=None, scales=None) -> Cache:
     if k.dim() != 4:
         raise PPError(PP_ERR_INVALID_ARG, "pp_cache_create shapes")
     pages, H, page, D = k.shape
-    name = str(k.dtype)
+    y = _torch_types()
     out = ctypes.c_void_p()
-    _check(lib.pp_cache_create(_dtype(k), pages, page, H, D, _dense(k, k.shape, name, "k"),
-                               _dense(v, k.shape, name, "v"), _dense(codes, (pages, H, 2, D), "torch.int8", "codes"),
-                               _dense(scales, (pages, H), "torch.float32", "scales"), ctypes.byref(out)),
-           "pp_cache_create")
+    _check(lib.pp_cache_create(_dtype(k), pages, page, H, D, _dense(k, k.shape, k.dtype, "k"),
+                               _dense(v, k.shape, k.dtype, "v"), _dense(codes, (pages, H, 2, D), y.i8, "codes"),
+                               _dense(scales, (pages, H), y.f32, "scales"), ctypes.byref(out)), "pp_cache_create")
     c = Cache(out.value)
-    c.dtype, c.shape, c.pools = _dtype(k), (pages, H, page, D), (k, v, codes, scales)
+    c.dtype, c.shape, c.pools = k.dtype, (pages, H, page, D), (k, v, codes, scales)
     return c
 
 
@@ -542,48 +560,47 @@ def pp_cache_device_status(cache) -> int:
 
 def pp_qkv_store(rope, cache, pos, slots, eps, q, qw, q_out, k, kw, v, stream=None):
     """pp_qk_rotate with the keys, and the values as they are, stored to slots [T] (int32) of the cache."""
-    T, D, dt = k.shape[0], rope.D, cache.dtype
+    T, D, dt, y = k.shape[0], rope.D, cache.dtype, _torch_types()
     H = cache.shape[1]
     qp, qt, qh, Hq = _heads(q, dt, T, D)
     kp, kt, kh, Hk = _heads(k, dt, T, D)
     vp, vt, vh, Hv = _heads(v, dt, T, D)
     if Hk != H or Hv != H:
         raise PPError(PP_ERR_INVALID_ARG, "pp_qkv_store: k and v have the cache's heads")
-    _check(lib.pp_qkv_store(rope, cache, T, _dense(pos, (rope.axes, T), "torch.int32", "pos"),
-                            _dense(slots, (T,), "torch.int32", "slots"), eps, qp, qt, qh, Hq,
-                            _dense(qw, (D,), "torch.float32", "qw"), _dense(q_out, (T, Hq, D), str(k.dtype), "q_out"),
-                            kp, kt, kh, _dense(kw, (D,), "torch.float32", "kw"), vp, vt, vh, _stream(stream)),
-           "pp_qkv_store")
+    _check(lib.pp_qkv_store(rope, cache, T, _dense(pos, (rope.axes, T), y.i32, "pos"), _dense(slots, (T,), y.i32, "slots"),
+                            eps, qp, qt, qh, Hq, _dense(qw, (D,), y.f32, "qw"), _dense(q_out, (T, Hq, D), dt, "q_out"),
+                            kp, kt, kh, _dense(kw, (D,), y.f32, "kw"), vp, vt, vh, _stream(stream)), "pp_qkv_store")
 
 
 def pp_cache_summarize(cache, ids, stream=None):
     """Summaries of the full pages ids [n] (int32) into the cache's codes and scales."""
-    _check(lib.pp_cache_summarize(cache, _dense(ids, (ids.numel(),), "torch.int32", "ids"), ids.numel(),
-                                  _stream(stream)), "pp_cache_summarize")
+    n = ids.shape[0]
+    _check(lib.pp_cache_summarize(cache, _dense(ids, (n,), _torch_types().i32, "ids"), n, _stream(stream)),
+           "pp_cache_summarize")
 
 
-def _sequences(q, cache, starts, table, lens):
+def _sequences(q, cache, starts, table, lens, y):
     """The arguments that pp_cache_select and pp_attn_forward share: tokens, queries, sequences."""
     T = q.shape[0]
     qp, qt, qh, Hq = _heads(q, cache.dtype, T, cache.shape[3])
     B, width = table.shape
-    return (cache, T, qp, qt, qh, Hq, B, _dense(starts, (B + 1,), "torch.int32", "starts"),
-            _dense(table, (B, width), "torch.int32", "table"), width, _dense(lens, (B,), "torch.int32", "lens"))
+    return (cache, T, qp, qt, qh, Hq, B, _dense(starts, (B + 1,), y.i32, "starts"),
+            _dense(table, (B, width), y.i32, "table"), width, _dense(lens, (B,), y.i32, "lens"))
 
 
 def pp_cache_select(cache, q, starts, table, lens, flags, first, last, sel, stream=None):
     """The pages of each token and cache head worth reading, into sel [T][H][keep] (int32); see the header."""
-    keep = sel.shape[2]
-    _check(lib.pp_cache_select(*_sequences(q, cache, starts, table, lens), flags, first, last, keep,
-                               _dense(sel, (q.shape[0], cache.shape[1], keep), "torch.int32", "sel"), _stream(stream)),
+    keep, y = sel.shape[2], _torch_types()
+    _check(lib.pp_cache_select(*_sequences(q, cache, starts, table, lens, y), flags, first, last, keep,
+                               _dense(sel, (q.shape[0], cache.shape[1], keep), y.i32, "sel"), _stream(stream)),
            "pp_cache_select")
 
 
 def pp_attn_forward(cache, q, starts, table, lens, scale, flags, sel, out, lse=None, stream=None):
     """Attention of q [T][Hq][D] over the cache into out; sel None: every visible page.  lse [T][Hq] fp32 or None."""
-    T, Hq, D = q.shape
+    (T, Hq, _), y = q.shape, _torch_types()
     keep = 0 if sel is None else sel.shape[2]
-    _check(lib.pp_attn_forward(*_sequences(q, cache, starts, table, lens), scale, flags,
-                               _dense(sel, (T, cache.shape[1], keep), "torch.int32", "sel"), keep,
-                               _dense(out, (T, Hq, D), str(q.dtype), "out"),
-                               _dense(lse, (T, Hq), "torch.float32", "lse"), _stream(stream)), "pp_attn_forward")
+    _check(lib.pp_attn_forward(*_sequences(q, cache, starts, table, lens, y), scale, flags,
+                               _dense(sel, (T, cache.shape[1], keep), y.i32, "sel"), keep,
+                               _dense(out, q.shape, q.dtype, "out"), _dense(lse, (T, Hq), y.f32, "lse"),
+                               _stream(stream)), "pp_attn_forward")
