@@ -17,7 +17,9 @@
 // join at the end of a unit.  mma.sync and not tcgen05: at most 16 rows meet a
 // key, and the copies set the pace.  With 16-bit values the products are
 // transposed (m16n8k16: keys x rows, then values x rows), so that groups of up to
-// 8 rows fill an instruction; fp32 takes three tf32 products (m16n8k8) per one.
+// 8 rows fill an instruction.  fp32 takes plain fp32 multiply-adds, for 2, 4 or 8
+// rows: mma.sync in tf32 runs no faster on this GPU, and needs three products and
+// 16 rows (measured: 5600 cycles per tile against 1100).
 #include <algorithm>
 #include <cmath>
 
@@ -40,7 +42,7 @@ constexpr int kJoin = kMaxCtas / kGroup;
 template <class T, int DP, int RB>
 struct Shape {
   static constexpr int E = sizeof(T);
-  static constexpr int R = 8 * RB;              // query rows of a unit
+  static constexpr int R = E == 4 ? RB : 8 * RB;  // query rows of a unit
   static constexpr int TK = E == 4 ? 32 : 64;   // keys per tile
   static constexpr int LOG_TK = E == 4 ? 5 : 6;
   static constexpr int KW = TK / kWarps;        // keys per warp
@@ -48,10 +50,9 @@ struct Shape {
   static constexpr int NCH = DP / CH;
   static constexpr int TILE = TK * DP * E;      // bytes of a K or V tile
   static constexpr int CTAS = DP <= 128 ? 2 : 1;
-  static constexpr int QW = DP + 4;             // row stride of fp32 queries, which stay in shared memory as two tf32 parts
-  static constexpr int QS = E == 4 ? R * QW * 8 : 0;
-  static constexpr int AS = DP + (E == 4 ? 8 : 4);          // row stride of the joining buffers, free of bank conflicts
-  static constexpr int NB = RB == 1 ? 2 : 1;                // joining buffers
+  static constexpr int QS = E == 4 ? R * DP * 4 : 0;  // fp32 queries stay in shared memory
+  static constexpr int AS = DP + 4;             // row stride of the joining buffers, free of bank conflicts
+  static constexpr int NB = R <= 8 ? 2 : 1;     // joining buffers
   static constexpr int ACC = NB * R * AS * 4;
   // as many stages as fit: with 228 KB per SM, 1 KB of it taken and 6 KB static per CTA, 190 KB are in flight (16 bits)
   static constexpr int STAGES = (233472 / CTAS - 1024 - 6144 - 1024 - ACC - QS) / (2 * TILE);
@@ -87,28 +88,6 @@ __device__ __forceinline__ void mma16<__nv_bfloat16>(float (&c)[4], const uint32
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma8(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// v = hi + lo in tf32, both rounded to nearest: what is left is below 2^-23 |v| and of either sign (cut off instead, all
-// products would be too small, and sums of them off by five times as much)
-__device__ __forceinline__ void split_tf32(float v, uint32_t& hi, uint32_t& lo) {
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(v));
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(v - __uint_as_float(hi)));
-}
-// a b with fp32 operands as three tf32 products (lo lo, below 2^-22, is left out).  They start from 0 and are added to a
-// running sum outside: a tensor-core sum is cut off at each product, always towards 0, and over many of them that shows.
-__device__ __forceinline__ void mma8x3(float (&c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], float b0, float b1) {
-  uint32_t h0, l0, h1, l1;
-  split_tf32(b0, h0, l0);
-  split_tf32(b1, h1, l1);
-  c[0] = c[1] = c[2] = c[3] = 0.f;
-  mma8(c, al, h0, h1);
-  mma8(c, ah, l0, l1);
-  mma8(c, ah, h0, h1);
 }
 // An 8 x 8 matrix of 16-bit values over the warp, two per lane, transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
@@ -195,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* acc = reinterpret_cast<float*>(smem + ST * 2 * S::TILE);
-  [[maybe_unused]] uint2* qs = reinterpret_cast<uint2*>(acc + S::NB * R * S::AS);
+  [[maybe_unused]] float* qs = acc + S::NB * R * S::AS;
   __shared__ alignas(8) uint64_t full_bar[ST], empty_bar[ST];
   __shared__ Stage stage[ST];
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], rm[kRows], rl[kRows];
@@ -387,12 +366,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
   }
 
   // ---- consumers
-  // A lane's sums: 16 bits, values i * 16 + g, + 8 of rows 8 rb + 2t, + 1 (o[rb][i]); fp32, rows g, g + 8 of values
-  // i * 8 + 2t, + 1 (o[0][i]).
-  constexpr int NO = S::E == 2 ? DP / 16 : DP / 8, OB = S::E == 2 ? RB : 1, NR = 2 * (S::E == 2 ? RB : 1);
+  // A lane's sums: 16 bits, values i * 16 + g, + 8 of rows 8 rb + 2t, + 1 (o[rb][i]); fp32, four values from (lane + 32 i) * 4
+  // on of every row (o[r][i]).
+  constexpr int NO = S::E == 2 ? DP / 16 : (DP + 127) / 128, OB = S::E == 2 ? RB : R, NR = S::E == 2 ? 2 * RB : R;
   const int g = lane / 4, t = lane % 4;
   // the r-th of the lane's NR rows
-  auto row_of = [&](int r) { return S::E == 2 ? (r >> 1) * 8 + 2 * t + (r & 1) : g + 8 * r; };
+  auto row_of = [&](int r) { return S::E == 2 ? (r >> 1) * 8 + 2 * t + (r & 1) : r; };
   const T* q = static_cast<const T*>(p.q);
   [[maybe_unused]] const bool q16 = ((reinterpret_cast<uintptr_t>(q) & 15) | (p.q_ts & 7) | (p.q_hs & 7)) == 0;
   int s = 0;
@@ -454,9 +433,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       group_sync<kWarps * 32>();  // the last unit's are read
       for (int i = tid; i < R * DP; i += kWarps * 32) {
         const int r = i / DP, d = i % DP;
-        uint2 v;
-        split_tf32(r < nrows && d < p.D ? to_f32(qrow(r)[d]) : 0.f, v.x, v.y);
-        qs[r * S::QW + d] = v;
+        qs[i] = r < nrows && d < p.D ? to_f32(qrow(r)[d]) : 0.f;
       }
       group_sync<kWarps * 32>();
     }
@@ -479,62 +456,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       const uint32_t kt = su32(smem + s * 2 * S::TILE), vt = kt + S::TILE;
       const Stage& sg = stage[s];
       const bool clean = sg.full && (listed || (k + 1) * TK <= lim_min);
-      // ---- scores of this warp's keys.  16 bits: sc[rb] is keys g (0, 1) and g + 8 (2, 3) by the lane's two rows;
-      // fp32: rows g (0, 1) and g + 8 (2, 3) by keys 2t, 2t + 1
-      float sc[OB][4];
-#pragma unroll
-      for (int rb = 0; rb < OB; ++rb) sc[rb][0] = sc[rb][1] = sc[rb][2] = sc[rb][3] = 0.f;
-      if constexpr (S::E == 2) {
-        float odd[OB][4];  // every other step apart: two chains of products instead of one
-#pragma unroll
-        for (int rb = 0; rb < OB; ++rb) odd[rb][0] = odd[rb][1] = odd[rb][2] = odd[rb][3] = 0.f;
-        const int key = warp * KW + lane % 16;
-#pragma unroll
-        for (int kk = 0; kk < DP / 16; ++kk) {
-          uint32_t a[4];
-          ldsm4(kt + kk / 4 * TK * 128 + key * 128 + ((((kk % 4) * 2 + lane / 16) ^ (key & 7)) << 4), a);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) mma16<T>(kk % 2 ? odd[rb] : sc[rb], a, qf[rb][kk][0], qf[rb][kk][1]);
-        }
-#pragma unroll
-        for (int rb = 0; rb < OB; ++rb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[rb][e] += odd[rb][e];
-      } else {
-        const int key = warp * KW + g;
-        const float* kp = reinterpret_cast<const float*>(smem + s * 2 * S::TILE);
-#pragma unroll 4
-        for (int kk = 0; kk < DP / 8; ++kk) {
-          const float* row = kp + kk / 4 * TK * 32 + key * 32;
-          const int c = kk % 4 * 2;
-          const uint2* qa = qs + g * S::QW + kk * 8 + t;
-          const uint2 q0 = qa[0], q2 = qa[4];
-          uint2 q1 = make_uint2(0, 0), q3 = q1;
-          if (nrows > 8) {
-            q1 = qa[8 * S::QW];
-            q3 = qa[8 * S::QW + 4];
-          }
-          const uint32_t ah[4] = {q0.x, q1.x, q2.x, q3.x}, al[4] = {q0.y, q1.y, q2.y, q3.y};
-          float part[4];
-          mma8x3(part, ah, al, row[((c ^ (key & 7)) << 2) + t], row[(((c + 1) ^ (key & 7)) << 2) + t]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[0][e] += part[e];
-        }
-      }
-      // entry e of sc[rb]: its row among the lane's, its key in the tile
-      auto row_in = [&](int rb, int e) { return S::E == 2 ? 2 * rb + (e & 1) : e >> 1; };
-      auto key_in = [&](int e) { return warp * KW + (S::E == 2 ? g + 8 * (e >> 1) : 2 * t + (e & 1)); };
-#pragma unroll
-      for (int rb = 0; rb < OB; ++rb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sc[rb][e] *= sl;
-          if (!clean) {
-            const int j = key_in(e);
-            if ((j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim[row_in(rb, e)])) sc[rb][e] = -INFINITY;
-          }
-        }
-      if (!clean) {  // values that no row sees: 0 x them has to be 0
+      // a key of the tile that row r of the lane's may not use; keys whose values have to be 0, as no row uses them
+      auto hidden = [&](int j, int r) { return (j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim[r]); };
+      if (!clean) {  // 0 x the values that no row sees has to be 0
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
           const int j = warp * KW + i;
@@ -545,44 +469,64 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
         }
         __syncwarp();
       }
-      // ---- softmax over what this warp has seen
       float f[NR];
       bool moved = false;
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        // the row's entries of this lane, and the lanes that hold its others
-        float& s0 = S::E == 2 ? sc[r >> 1][r & 1] : sc[0][2 * r];
-        float& s1 = S::E == 2 ? sc[r >> 1][2 + (r & 1)] : sc[0][2 * r + 1];
-        float mx = fmaxf(s0, s1);
-        if constexpr (S::E == 2) {
-          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
-          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
-          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
-        } else {
-          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
-        }
+      // the running maximum of row r after mx, the factor of what came before it, and where exponents are taken from
+      auto raise = [&](int r, float mx) {
         mx = fmaxf(m[r], mx);
         const float at = mx == -INFINITY ? 0.f : mx;
         f[r] = ex2(m[r] - at);
         moved = moved || m[r] != mx;
         m[r] = mx;
-        s0 = ex2(s0 - at);
-        s1 = ex2(s1 - at);
-        l[r] = l[r] * f[r] + (s0 + s1);
-      }
-      if (__any_sync(~0u, moved)) {
-#pragma unroll
-        for (int rb = 0; rb < OB; ++rb)
-#pragma unroll
-          for (int i = 0; i < NO; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[rb][i][e] *= f[row_in(rb, e)];
-      }
-      // ---- their product with V
+        return at;
+      };
       if constexpr (S::E == 2) {
-        // the weights as two halves of the inputs' type, so that they keep 16 bits and more (22 in f16): bound by the
-        // copies, the kernel has the time, and the output's own rounding stays the largest error
+        // ---- scores of this warp's keys: sc[rb] is keys g (0, 1) and g + 8 (2, 3) by the lane's two rows
+        float sc[RB][4], odd[RB][4];  // every other step apart: two chains of products instead of one
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[rb][e] = odd[rb][e] = 0.f;
+        {
+          const int key = warp * KW + lane % 16;
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk) {
+            uint32_t a[4];
+            ldsm4(kt + kk / 4 * TK * 128 + key * 128 + ((((kk % 4) * 2 + lane / 16) ^ (key & 7)) << 4), a);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) mma16<T>(kk % 2 ? odd[rb] : sc[rb], a, qf[rb][kk][0], qf[rb][kk][1]);
+          }
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sc[rb][e] = (sc[rb][e] + odd[rb][e]) * sl;
+            if (!clean && hidden(warp * KW + g + 8 * (e >> 1), 2 * rb + (e & 1))) sc[rb][e] = -INFINITY;
+          }
+        // ---- softmax over what this warp has seen
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          float &s0 = sc[r >> 1][r & 1], &s1 = sc[r >> 1][2 + (r & 1)];
+          float mx = fmaxf(s0, s1);
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+          const float at = raise(r, mx);
+          s0 = ex2(s0 - at);
+          s1 = ex2(s1 - at);
+          l[r] = l[r] * f[r] + (s0 + s1);
+        }
+        if (__any_sync(~0u, moved)) {
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int i = 0; i < NO; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[rb][i][e] *= f[2 * rb + (e & 1)];
+        }
+        // ---- their product with V.  The weights as two halves of the inputs' type, so that they keep 16 bits and more (22
+        // in f16): bound by the copies, the kernel has the time, and the output's own rounding stays the largest error
         uint32_t bh[RB][2], bl[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
@@ -590,10 +534,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
           for (int i = 0; i < 2; ++i) {
             const float a = sc[rb][2 * i], b = sc[rb][2 * i + 1];
             const uint32_t hi = pack<T>(a, b);
-            T two[2];
-            memcpy(two, &hi, 4);
+            Vec<T, 2> two;
+            memcpy(&two, &hi, 4);
+            const float2 back = get2(two, 0);
             bh[rb][i] = transpose8(hi);  // keys x rows to rows x keys
-            bl[rb][i] = transpose8(pack<T>(a - to_f32(two[0]), b - to_f32(two[1])));
+            bl[rb][i] = transpose8(pack<T>(a - back.x, b - back.y));
           }
         const int key = warp * KW + (lane / 16) * 8 + lane % 8;
 #pragma unroll
@@ -607,22 +552,66 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
           }
         }
       } else {
-        // columns t and t + 4 of the product's left side are keys 2t and 2t + 1: the sum does not mind
-        uint32_t ah[4], al[4];
-        split_tf32(sc[0][0], ah[0], al[0]);
-        split_tf32(sc[0][2], ah[1], al[1]);
-        split_tf32(sc[0][1], ah[2], al[2]);
-        split_tf32(sc[0][3], ah[3], al[3]);
-        const float* vp = reinterpret_cast<const float*>(smem + s * 2 * S::TILE + S::TILE);
-        const int key = warp * KW + 2 * t;
+        // ---- scores: lane (g, t) has a quarter of key g, 16 bytes at a time.  Which ones goes by where they lie: of each
+        // column's eight, 2t + (g & 1) and its neighbour, so that eight lanes meet eight banks
+        const int key = warp * KW + g;
+        const float* kp = reinterpret_cast<const float*>(smem + s * 2 * S::TILE) + key * 32;
+        float sc[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) sc[r] = 0.f;
+        const int columns = (p.D + 31) / 32;
+#pragma unroll 2
+        for (int c = 0; c < columns; ++c) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int at = 2 * t + ((g & 1) ^ e);
+            const float4 a = *reinterpret_cast<const float4*>(kp + c * TK * 32 + at * 4);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const float4 b = *reinterpret_cast<const float4*>(qs + r * DP + c * 32 + ((at ^ (key & 7)) << 2));
+              sc[r] = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, sc[r]))));
+            }
+          }
+        }
+        // ---- softmax over what this warp has seen
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          sc[r] += __shfl_xor_sync(~0u, sc[r], 1);
+          sc[r] = (sc[r] + __shfl_xor_sync(~0u, sc[r], 2)) * sl;
+          if (!clean && hidden(key, r)) sc[r] = -INFINITY;
+          float mx = sc[r];
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+          sc[r] = ex2(sc[r] - raise(r, mx));
+          l[r] = l[r] * f[r] + sc[r];
+        }
+        if (moved) {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < NO; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[r][i][e] *= f[r];
+        }
+        // ---- their product with V: key after key, a lane's four values of each
 #pragma unroll
         for (int i = 0; i < NO; ++i) {
-          const float* row = vp + i / 4 * TK * 32 + key * 32;
-          const int c = i % 4 * 2 + g / 4;
-          float part[4];
-          mma8x3(part, ah, al, row[((c ^ (key & 7)) << 2) + g % 4], row[32 + ((c ^ (key + 1 & 7)) << 2) + g % 4]);
+          const int c = DP == 64 ? lane % 16 : lane + 32 * i;  // of 64 values, two lanes have the same
+          const float* vp = reinterpret_cast<const float*>(smem + s * 2 * S::TILE + S::TILE) + c / 8 * TK * 32;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[0][i][e] += part[e];
+          for (int j = 0; j < KW; ++j) {
+            const int row = warp * KW + j;
+            const float4 v = *reinterpret_cast<const float4*>(vp + row * 32 + ((c % 8 ^ (row & 7)) << 2));
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const float w = __shfl_sync(~0u, sc[r], j * 4);
+              o[r][i][0] = fmaf(w, v.x, o[r][i][0]);
+              o[r][i][1] = fmaf(w, v.y, o[r][i][1]);
+              o[r][i][2] = fmaf(w, v.z, o[r][i][2]);
+              o[r][i][3] = fmaf(w, v.w, o[r][i][3]);
+            }
+          }
         }
       }
       if (!clean) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the zeros before the next copy
@@ -637,15 +626,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     // ---- the four warps' parts into one
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      if constexpr (S::E == 2) {
-        l[r] += __shfl_xor_sync(~0u, l[r], 4);
-        l[r] += __shfl_xor_sync(~0u, l[r], 8);
-        l[r] += __shfl_xor_sync(~0u, l[r], 16);
-      } else {
-        l[r] += __shfl_xor_sync(~0u, l[r], 1);
-        l[r] += __shfl_xor_sync(~0u, l[r], 2);
-      }
-      if (S::E == 2 ? g == 0 : t == 0) {
+      l[r] += __shfl_xor_sync(~0u, l[r], 4);
+      l[r] += __shfl_xor_sync(~0u, l[r], 8);
+      l[r] += __shfl_xor_sync(~0u, l[r], 16);
+      if (S::E == 2 ? g == 0 : lane == 0) {
         wm[warp][row_of(r)] = m[r];
         wl[warp][row_of(r)] = l[r];
       }
@@ -671,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     // warp i adds to buffer i % NB in round i / NB
 #pragma unroll
     for (int round = 0; round < kWarps / S::NB; ++round) {
-      if (warp / S::NB == round) {
+      if (warp / S::NB == round && !(S::E == 4 && DP == 64 && lane >= 16)) {
         float* buf = acc + warp % S::NB * R * S::AS;
 #pragma unroll
         for (int rb = 0; rb < OB; ++rb) {
@@ -681,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
             float v[C][4];
             auto place = [&](int i, int e) {
               return S::E == 2 ? buf + row_of(2 * rb + (e & 1)) * S::AS + i * 16 + g + 8 * (e >> 1)
-                               : buf + row_of(e >> 1) * S::AS + i * 8 + 2 * t + (e & 1);
+                               : buf + rb * S::AS + (DP == 64 ? lane % 16 : lane + 32 * i) * 4 + e;
             };
 #pragma unroll
             for (int i = 0; i < C && i0 + i < NO; ++i)
@@ -690,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
 #pragma unroll
             for (int i = 0; i < C && i0 + i < NO; ++i)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) *place(i0 + i, e) = v[i][e] + o[rb][i0 + i][e] * f[S::E == 2 ? 2 * rb + (e & 1) : e >> 1];
+              for (int e = 0; e < 4; ++e) *place(i0 + i, e) = v[i][e] + o[rb][i0 + i][e] * f[S::E == 2 ? 2 * rb + (e & 1) : rb];
           }
         }
       }
@@ -844,13 +828,17 @@ cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t
   return cudaGetLastError();
 }
 
-// Units of 8 rows where a sequence (or, with selected pages, a token) has no more, else of 16: fp32 always of 16.
+// Units of as many rows as a sequence (or, with selected pages, a token) has, up to 8 or 16; in fp32 up to 8.
 template <class T, int DP>
 cudaError_t by_rows(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
+  const int64_t rows = p.sel || !p.starts ? p.G.d : ((int64_t)p.T * p.G.d + p.B - 1) / p.B;
   if constexpr (sizeof(T) == 2) {
-    if (p.G.d <= 8 && (p.sel || !p.starts || (int64_t)p.T * p.G.d <= (int64_t)p.B * 8)) return launch<T, DP, 1>(p, c, sms, stream);
+    return rows <= 8 ? launch<T, DP, 1>(p, c, sms, stream) : launch<T, DP, 2>(p, c, sms, stream);
+  } else {
+    return rows <= 2   ? launch<T, DP, 2>(p, c, sms, stream)
+           : rows <= 4 ? launch<T, DP, 4>(p, c, sms, stream)
+                       : launch<T, DP, 8>(p, c, sms, stream);
   }
-  return launch<T, DP, 2>(p, c, sms, stream);
 }
 
 template <class T>
@@ -884,6 +872,8 @@ cudaError_t attn_prepare() {
   return g_attn_once.run([](int) {
     cudaError_t e = tile_prepare();
     if (e == cudaSuccess) e = prepare_type<float, 2>();
+    if (e == cudaSuccess) e = prepare_type<float, 4>();
+    if (e == cudaSuccess) e = prepare_type<float, 8>();
     if (e == cudaSuccess) e = prepare_type<__half, 1>();
     if (e == cudaSuccess) e = prepare_type<__half, 2>();
     if (e == cudaSuccess) e = prepare_type<__nv_bfloat16, 1>();
@@ -912,7 +902,7 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
   const pp_cache& c = *cache;
   const int G = Hq / c.H;
   // all tiles, at most: they are counted in 32 bits
-  const int64_t units = sel ? (int64_t)T * ((G + 7) / 8) : ((int64_t)T * G + (int64_t)B * 7) / 8;
+  const int64_t units = sel ? (int64_t)T * ((G + 1) / 2) : ((int64_t)T * G + B) / 2;
   const int64_t deep = std::max<int64_t>(1, ((int64_t)(sel ? std::min(width, keep) : width) * c.page + tile_keys(c.dtype) - 1) / tile_keys(c.dtype));
   if (units * c.H >= INT32_MAX / deep || (int64_t)T * G >= INT32_MAX) return PP_ERR_UNSUPPORTED;
   AttnParams p = {q,     q_ts,   q_hs,        c.k,        c.v,     starts, table, lens, sel,  out, lse, c.status, c.counters,
