@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  after_previous();
   // every thread looks after a run of items
   const int per = (NI + kThreads - 1) / kThreads;
   const int i0 = min(NI, tid * per), i1 = min(NI, i0 + per);
@@ -824,8 +825,7 @@ cudaError_t prepare_one() {
 template <class T, int DP, int RB>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
   const int grid = std::min(sms * Shape<T, DP, RB>::CTAS, kMaxCtas);
-  attn_kernel<T, DP, RB><<<grid, kThreads, Shape<T, DP, RB>::SMEM, stream>>>(p, c.mk, c.mv);
-  return cudaGetLastError();
+  return launch_after(attn_kernel<T, DP, RB>, dim3(grid), kThreads, Shape<T, DP, RB>::SMEM, stream, 1, p, c.mk, c.mv);
 }
 
 // Units of as many rows as a sequence (or, with selected pages, a token) has, up to 8 or 16; in fp32 up to 8.

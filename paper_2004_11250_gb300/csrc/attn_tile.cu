@@ -195,6 +195,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     tile_of[0] = -1;
   }
   __syncthreads();
+  after_previous();
   const int per = (p.B + kThreadsT - 1) / kThreadsT, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
   int mine = 0;
   bool bad = false;
@@ -651,11 +652,9 @@ cudaError_t prepare_one() {
 
 template <class T>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int64_t grid, cudaStream_t stream) {
-  if (p.D <= 64)
-    attn_tile_kernel<T, 64><<<(unsigned)grid, kThreadsT, TileShape<64>::SMEM, stream>>>(p, c.mk, c.mv);
-  else
-    attn_tile_kernel<T, 128><<<(unsigned)grid, kThreadsT, TileShape<128>::SMEM, stream>>>(p, c.mk, c.mv);
-  return cudaGetLastError();
+  const dim3 blocks((unsigned)grid);
+  return p.D <= 64 ? launch_after(attn_tile_kernel<T, 64>, blocks, kThreadsT, TileShape<64>::SMEM, stream, 1, p, c.mk, c.mv)
+                   : launch_after(attn_tile_kernel<T, 128>, blocks, kThreadsT, TileShape<128>::SMEM, stream, 1, p, c.mk, c.mv);
 }
 
 }  // namespace

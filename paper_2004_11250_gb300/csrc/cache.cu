@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(kThreads) summarize_kernel(const T* __restrict
   constexpr int V = 16 / sizeof(T);
   __shared__ float hi[kThreads * V], lo[kThreads * V];
   __shared__ float big[kThreads / 32];
+  after_previous();
   const int id = ids[blockIdx.x], h = blockIdx.y, tid = threadIdx.x;
   if (id < 0 || id >= pages) {
     if (tid == 0) atomicOr(status, PP_CACHE_BAD_PAGE);
@@ -181,15 +182,14 @@ pp_status pp_cache_summarize(const pp_cache* cache, const int32_t* ids, int n, v
   const dim3 grid(n, cache->H);
   const pp_cache& c = *cache;
   auto run = [&](auto* k) {
-    summarize_kernel<<<grid, kThreads, 0, s>>>(k, ids, c.pages, c.page, c.H, c.D, c.codes, c.scales, c.status);
+    using T = std::remove_const_t<std::remove_pointer_t<decltype(k)>>;
+    return launch_after(summarize_kernel<T>, grid, kThreads, 0, s, 1, k, ids, c.pages, c.page, c.H, c.D, c.codes, c.scales,
+                        c.status);
   };
-  if (c.dtype == PP_F32)
-    run(static_cast<const float*>(c.k));
-  else if (c.dtype == PP_F16)
-    run(static_cast<const __half*>(c.k));
-  else
-    run(static_cast<const __nv_bfloat16*>(c.k));
-  return cudaGetLastError() == cudaSuccess ? PP_OK : PP_ERR_CUDA;
+  const cudaError_t e = c.dtype == PP_F32   ? run(static_cast<const float*>(c.k))
+                        : c.dtype == PP_F16 ? run(static_cast<const __half*>(c.k))
+                                            : run(static_cast<const __nv_bfloat16*>(c.k));
+  return e == cudaSuccess ? PP_OK : PP_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -45,6 +45,30 @@ AttnSpace attn_space(int dtype, int D, int sms);
 cudaError_t attn_prepare();
 cudaError_t select_prepare();
 
+// Launches that may begin while the stream's kernel before them ends (programmatic dependent launch): their kernels call
+// after_previous() before they touch any memory, and let the next one begin at once.  A step's calls are small and follow
+// each other, so a launch's latency hides behind the kernel before it.
+template <class... P, class... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, int cluster, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 inline int dtype_size(int dtype) { return dtype == PP_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == PP_F32 || dtype == PP_F16 || dtype == PP_BF16; }
 

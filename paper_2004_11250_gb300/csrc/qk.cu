@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
   auto vec_of = [](int i, int k) { return WIDE && INTER ? (2 * i + k) / V : k; };
   auto place_of = [](int i, int k) { return WIDE && INTER ? (2 * i + k) % V : i; };
 
+  after_previous();
   // ---- the heads' values are asked for
   const int64_t i0 = (int64_t)blockIdx.x * GROUPS * J;
   const int t0 = (int)(i0 / p.heads.d), rest = (int)(i0 - (int64_t)t0 * p.heads.d);  // the first item's token, and its head
@@ -271,8 +272,7 @@ cudaError_t launch(QkParams p, cudaStream_t stream) {
   const int64_t blocks = (p.items + per - 1) / per;
   if (blocks > INT32_MAX) return cudaErrorInvalidValue;
   const size_t shared = (2 * (size_t)p.D + 2 * (size_t)p.span * p.pairs) * 4;
-  qk_kernel<T, WIDE, INTER, GROUP, J><<<(unsigned)blocks, kThreads, shared, stream>>>(p);
-  return cudaGetLastError();
+  return launch_after(qk_kernel<T, WIDE, INTER, GROUP, J>, dim3((unsigned)blocks), kThreads, shared, stream, 1, p);
 }
 
 // Two heads per group of lanes where that still gives every SM 8 blocks and the angles fit, else one: more blocks for

@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
   __shared__ int hist[256], warp_sum[kThreads / 32], digit_of, left_of;
   const int rank = cluster_rank(), ranks = cluster_size();
   const int t = blockIdx.x / ranks, h = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+  after_previous();
   const Seen s = seen_keys(t, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
   const int P = (s.keys + p.page - 1) / p.page;
   int* out = p.sel + ((int64_t)t * p.H + h) * p.keep;
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(kThreads, 3) select_tile_kernel(const SelectPa
   __shared__ int row_b[kTokens], row_P[kTokens];
   const int t0 = blockIdx.x * kTokens, h = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   const int nt = min(kTokens, p.T - t0), D2 = 2 * p.D, cs = D2 + 4, stride = p.width + 4;  // rows 2 and 4 banks apart
+  after_previous();
   // ---- the tokens' sequences and integers, a warp per token
   for (int r = warp; r < kTokens; r += kThreads / 32) {
     Seen s = {0, 0};
@@ -452,24 +454,13 @@ cudaError_t launch(const SelectParams& p, int sms, cudaStream_t stream) {
   // Not where a sum of queries passes what f16 holds exactly, nor where the scores of 16 tokens do not fit.
   if (p.starts && (int64_t)p.T >= (int64_t)p.B * 4 && p.Q * p.G <= kExact && p.width <= kTileWidth) {
     const dim3 grid((p.T + kTokens - 1) / kTokens, p.H);
-    select_tile_kernel<T><<<grid, kThreads, (size_t)kTokens * (p.width + 4) * 4, stream>>>(p);
-    return cudaGetLastError();
+    return launch_after(select_tile_kernel<T>, grid, kThreads, (size_t)kTokens * (p.width + 4) * 4, stream, 1, p);
   }
   // CTAs per (token, head): more where there are few, so that long tables are read by enough of them
   int ranks = 1;
   while (ranks < 8 && (int64_t)p.T * p.H * ranks * 2 <= sms * 2 && p.width >= ranks * 2 * 128) ranks *= 2;
   if ((int64_t)p.T * ranks > INT32_MAX) return cudaErrorInvalidValue;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.T * ranks, p.H);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)p.width * 4;
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)ranks, 1, 1};
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, select_kernel<T>, p);
+  return launch_after(select_kernel<T>, dim3(p.T * ranks, p.H), kThreads, (size_t)p.width * 4, stream, ranks, p);
 }
 
 DeviceOnce g_select_once;
