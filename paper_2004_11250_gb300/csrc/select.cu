@@ -143,25 +143,30 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
       for (int i = tid; i < p.keep; i += kThreads) out[i] = i < P ? i : -1;
     return;
   }
+  // every CTA of the cluster has begun before one writes to the first's shared memory
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  // candidates: pages first .. P - last - 1; this CTA's are from .. to - 1.  Their ids first, where the scores will be
+  const int N = P - p.first - p.last, share = (N + ranks - 1) / ranks, from = min(N, rank * share), to = min(N, from + share);
+  const int* row = p.table + (int64_t)s.b * p.width + p.first;
+  for (int w = from + tid; w < to; w += kThreads) key[w] = (uint32_t)row[w];
   if (warp == 0)
     query_codes<T>(p, t, h, lane, [&](int d, int up, int down) {
       code[d] = (short)up;
       code[p.D + d] = (short)down;
     });
+  if (ranks > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   __syncthreads();
-  // candidates: pages first .. P - last - 1; 2 D / 16 lanes a page, in a power of two
-  const int N = P - p.first - p.last, chunks = p.D / 8;
+  // 2 D / 16 lanes a page, in a power of two
+  const int chunks = p.D / 8;
   int span = 2;
   while (span < chunks) span *= 2;
   const int at = lane % span, per = 32 / span;  // pages per warp at a time
   int mine[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) mine[i] = at < chunks ? reinterpret_cast<const int*>(code)[at * 8 + i] : 0;
-  const int* row = p.table + (int64_t)s.b * p.width + p.first;
   const uint32_t keys0 = map_rank((uint32_t)__cvta_generic_to_shared(key), 0);
-  const int step = (kThreads / 32) * per;
-  constexpr int U = 4;
-  for (int w0 = (rank * U * (kThreads / 32) + warp * U) * per; w0 < N; w0 += ranks * U * step) {
+  constexpr int U = 8;
+  for (int w0 = from + warp * U * per; w0 < to; w0 += (kThreads / 32) * U * per) {
     int4 c[U];
     float sc[U];
 #pragma unroll
@@ -169,8 +174,8 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
       const int w = w0 + u * per + lane / span;
       c[u] = make_int4(0, 0, 0, 0);
       sc[u] = nanf("");
-      if (w < N) {
-        const int id = row[w];
+      if (w < to) {
+        const int id = (int)key[w];
         if (id < 0 || id >= p.pages) {
           if (at == 0) atomicOr(p.status, PP_CACHE_BAD_PAGE);
         } else {
@@ -180,6 +185,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
         }
       }
     }
+    __syncwarp();  // the ids are read before scores take their places
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       int sum = dot2_hi(mine[1], c[u].x, dot2_lo(mine[0], c[u].x, 0));
@@ -188,11 +194,14 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
       sum = dot2_hi(mine[7], c[u].w, dot2_lo(mine[6], c[u].w, sum));
       for (int d = span / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
       const int w = w0 + u * per + lane / span;
-      if (at == 0 && w < N)
+      if (at == 0 && w < to)
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys0 + 4 * w), "r"(ordered(__fmul_rn((float)sum, sc[u]))) : "memory");
     }
   }
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (ranks > 1)
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else
+    __syncthreads();
   if (rank != 0) return;
   // the need-th largest key: thr, with `need` of those equal to it (under the mask of the digits found)
   int need = p.keep - p.first - p.last;
