@@ -288,25 +288,38 @@ __global__ void __launch_bounds__(kThreadsT, 2)
 
   const T* q = static_cast<const T*>(p.q);
   if (warp < 4) {  // the queries, swizzled as a copy would
-    const bool q16 = ((reinterpret_cast<uintptr_t>(q) & 15) | (p.q_ts & 7) | (p.q_hs & 7)) == 0;
-    for (int i = tid; i < kRowsT * (DP / 8); i += kSoft) {
-      const int r = i / (DP / 8), c = i % (DP / 8);
-      Vec<T, 8> v = {};
-      if (r < rows && c * 8 < p.D) {
-        const T* from = q + (t0 + p.G.div(r)) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs + c * 8;
-        if (q16) {
-          v = *reinterpret_cast<const Vec<T, 8>*>(from);
-        } else {
+    auto fill = [&](auto wide) {  // one kind of load, without branches between those in flight
+      constexpr int U = 8;
+      for (int i0 = tid; i0 < kRowsT * (DP / 8); i0 += U * kSoft) {
+        Vec<T, 8> v[U];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v.v[e] = from[e];
+        for (int u = 0; u < U; ++u) {
+          const int r = (i0 + u * kSoft) / (DP / 8), c = (i0 + u * kSoft) % (DP / 8);
+          const int from_r = min(r, rows - 1), from_c = min(c * 8, p.D - 8);
+          const T* from = q + (t0 + p.G.div(from_r)) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(from_r)) * p.q_hs + from_c;
+          if constexpr (decltype(wide)::value) {
+            v[u] = *reinterpret_cast<const Vec<T, 8>*>(from);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u].v[e] = from[e];
+          }
         }
-        if (p.scale <= 0.f) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v.v[e] = from_f32<T>(p.scale < 0.f ? -to_f32(v.v[e]) : 0.f);
+        for (int u = 0; u < U; ++u) {
+          const int r = (i0 + u * kSoft) / (DP / 8), c = (i0 + u * kSoft) % (DP / 8);
+          if (r >= rows || c * 8 >= p.D || p.scale == 0.f) v[u] = {};
+          if (p.scale < 0.f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u].v[e] = from_f32<T>(-to_f32(v[u].v[e]));
+          }
+          *reinterpret_cast<Vec<T, 8>*>(smem + c / 8 * CHUNK_Q + r * 128 + ((c % 8 ^ (r & 7)) << 4)) = v[u];
         }
       }
-      *reinterpret_cast<Vec<T, 8>*>(smem + c / 8 * CHUNK_Q + r * 128 + ((c % 8 ^ (r & 7)) << 4)) = v;
-    }
+    };
+    if (((reinterpret_cast<uintptr_t>(q) & 15) | (p.q_ts & 7) | (p.q_hs & 7)) == 0)
+      fill(std::true_type{});
+    else
+      fill(std::false_type{});
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     mbar_arrive(su32(&q_full));
   }
