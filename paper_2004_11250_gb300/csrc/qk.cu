@@ -103,46 +103,46 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
   Vec<T, V> ab[J][2];
   T* to[J];
   int tok[J], part[J];
+  int head[J];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    const int i = rest + grp + j * GROUPS;
+    // an item beyond the last is the last once more, and not stored: no conditions around the loads
+    const int i = (int)min((int64_t)(rest + grp + j * GROUPS), p.items - 1 - i0 + rest);
     tok[j] = p.heads.div(i);
-    int h = i - tok[j] * p.heads.d;
-    const int64_t t = t0 + tok[j];
+    const int h = i - tok[j] * p.heads.d;
     part[j] = h < p.Hq ? 0 : h < p.Hq + p.Hk ? 1 : 2;
-    to[j] = nullptr;
-    ab[j][0] = ab[j][1] = {};
-    if (i0 + grp + j * GROUPS >= p.items) {
-      part[j] = 3;
-      continue;
+    head[j] = h - (part[j] == 0 ? 0 : part[j] == 1 ? p.Hq : p.Hq + p.Hk);
+    const View& x = p.x[part[j]];
+    const T* from = static_cast<const T*>(x.p) + (t0 + tok[j]) * x.ts + head[j] * x.hs;
+    if (WIDE) {
+      ab[j][0] = *reinterpret_cast<const Vec<T, V>*>(from + (on ? ia : 0));
+      ab[j][1] = *reinterpret_cast<const Vec<T, V>*>(from + (on ? ib : 0));
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int e = min(pair(k), half - 1);
+        ab[j][0].v[k] = from[first(e)];
+        ab[j][1].v[k] = from[second(e)];
+      }
     }
-    h -= part[j] == 0 ? 0 : part[j] == 1 ? p.Hq : p.Hq + p.Hk;
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int64_t t = t0 + tok[j];
+    to[j] = nullptr;
+    if (i0 + grp + j * GROUPS >= p.items) continue;
     if (part[j] == 0) {
-      to[j] = static_cast<T*>(p.qo) + (t * p.Hq + h) * p.D;
+      to[j] = static_cast<T*>(p.qo) + (t * p.Hq + head[j]) * p.D;
     } else if (part[j] == 1 && p.ko) {
-      to[j] = static_cast<T*>(p.ko) + (t * p.Hk + h) * p.D;
+      to[j] = static_cast<T*>(p.ko) + (t * p.Hk + head[j]) * p.D;
     } else {
       const int64_t slot = p.slots[t];
       if (slot >= 0 && slot < p.nslots) {
         const int64_t page = slot >> p.log_page;
-        to[j] = static_cast<T*>(part[j] == 1 ? p.ck : p.cv) + (((page * p.H + h) << p.log_page) + (slot & (p.page - 1))) * p.D;
+        to[j] = static_cast<T*>(part[j] == 1 ? p.ck : p.cv) + (((page * p.H + head[j]) << p.log_page) + (slot & (p.page - 1))) * p.D;
       } else if (slot != -1 && lane == 0) {
         atomicOr(p.status, PP_CACHE_BAD_SLOT);
       }
-    }
-    if (!on || !to[j]) continue;
-    const View& x = p.x[part[j]];
-    const T* from = static_cast<const T*>(x.p) + t * x.ts + h * x.hs;
-    if (WIDE) {
-      ab[j][0] = *reinterpret_cast<const Vec<T, V>*>(from + ia);
-      ab[j][1] = *reinterpret_cast<const Vec<T, V>*>(from + ib);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (pair(i) < half) {
-          ab[j][0].v[i] = from[first(pair(i))];
-          ab[j][1].v[i] = from[second(pair(i))];
-        }
     }
   }
   // ---- meanwhile the sines of the block's tokens, and the weights
@@ -174,6 +174,13 @@ __global__ void __launch_bounds__(kThreads) qk_kernel(const QkParams p) {
           const float2 x = get2(ab[j][0], i), y = get2(ab[j][1], i);
           fa[i] = pack2(x.x, x.y);
           fb[i] = pack2(y.x, y.y);
+        }
+        if (!valid(2 * i) || !valid(2 * i + 1)) {  // beyond the head: 0
+          float v[2];
+          unpack2(fa[i], v[0], v[1]);
+          fa[i] = pack2(valid(2 * i) ? v[0] : 0.f, valid(2 * i + 1) ? v[1] : 0.f);
+          unpack2(fb[i], v[0], v[1]);
+          fb[i] = pack2(valid(2 * i) ? v[0] : 0.f, valid(2 * i + 1) ? v[1] : 0.f);
         }
         s2 = fma2(fa[i], fa[i], s2);
         s2 = fma2(fb[i], fb[i], s2);

@@ -41,61 +41,54 @@ __device__ __forceinline__ uint32_t ordered(float v) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// Eight consecutive values as fp32.
-template <class T>
-__device__ __forceinline__ void load8(const T* x, bool wide, float (&v)[8]) {
-  if (wide) {
-    constexpr int V = 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < 8; i += V) {
-      const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(x + i);
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[i + e] = to_f32(a.v[e]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_f32(x[i]);
-  }
-}
-
 // The integers of token t's queries of head h, by one warp: store(d, up, down) for every value d of the head.  A lane
 // takes 8 values of every per-th head of the group; the largest first, then the rounded ones, summed over the group.
-template <class T, class F>
-__device__ __forceinline__ void query_codes(const SelectParams& p, int t, int h, int lane, F&& store) {
-  const T* q = static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)h * p.G * p.q_hs;
-  const bool wide = ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(p.q_hs * sizeof(T))) & 15) == 0;
+// Loads are asked for together and without conditions (a clamped place instead), so that they wait for memory once.
+template <class T, bool WIDE, class F>
+__device__ __forceinline__ void group_values(const T* q, int64_t q_hs, int G, int g0, int per, bool in, F&& use) {
+  constexpr int U = 4;
+  for (int g = g0; g - g0 < G; g += U * per) {
+    Vec<T, 8> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const T* from = q + min(g + u * per, G - 1) * q_hs;
+      if (WIDE) {
+        v[u] = *reinterpret_cast<const Vec<T, 8>*>(from);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u].v[i] = from[i];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (in && g + u * per < G)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) use(i, to_f32(v[u].v[i]));
+  }
+}
+template <class T, bool WIDE, class F>
+__device__ __forceinline__ void query_codes_of(const SelectParams& p, const T* q, int lane, F&& store) {
   const int chunks = p.D / 8;
   int span = 2;
   while (span < chunks) span *= 2;
   const int c = lane & (span - 1), per = 32 / span;
   const bool in = c < chunks;
+  const T* from = q + min(c, chunks - 1) * 8;
   float m = 0.f;
-#pragma unroll 4
-  for (int g = lane / span; g < p.G; g += per) {
-    float v[8] = {};
-    if (in) load8(q + g * p.q_hs + c * 8, wide, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float a = fabsf(v[i]);
-      m = a <= 3.402823466e38f ? fmaxf(m, a) : INFINITY;  // a NaN too
-    }
-  }
+  group_values<T, WIDE>(from, p.q_hs, p.G, lane / span, per, in, [&](int, float v) {
+    m = fabsf(v) <= 3.402823466e38f ? fmaxf(m, fabsf(v)) : INFINITY;  // a NaN too
+  });
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
   const bool zero = !(m >= kTiny) || m == INFINITY;
   const float r = zero ? 0.f : __fdiv_rn((float)p.Q, m);
   int up[8] = {}, down[8] = {};
-#pragma unroll 4
-  for (int g = lane / span; g < p.G; g += per) {
-    float v[8] = {};
-    if (in && !zero) load8(q + g * p.q_hs + c * 8, wide, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int k = (int)rintf(__fmul_rn(v[i], r));
+  if (!zero)
+    group_values<T, WIDE>(from, p.q_hs, p.G, lane / span, per, in, [&](int i, float v) {
+      const int k = (int)rintf(__fmul_rn(v, r));
       up[i] += max(k, 0);
       down[i] += min(k, 0);
-    }
-  }
+    });
   for (int d = span; d < 32; d *= 2)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -105,6 +98,14 @@ __device__ __forceinline__ void query_codes(const SelectParams& p, int t, int h,
   if (lane < chunks)
 #pragma unroll
     for (int i = 0; i < 8; ++i) store(c * 8 + i, up[i], down[i]);
+}
+template <class T, class F>
+__device__ __forceinline__ void query_codes(const SelectParams& p, int t, int h, int lane, F&& store) {
+  const T* q = static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)h * p.G * p.q_hs;
+  if (((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(p.q_hs * sizeof(T))) & (sizeof(Vec<T, 8>) - 1) & 15) == 0)
+    query_codes_of<T, true>(p, q, lane, store);
+  else
+    query_codes_of<T, false>(p, q, lane, store);
 }
 
 __device__ __forceinline__ int dot2_lo(int a, int b, int c) {  // c + a's two 16-bit halves times b's bytes 0 and 1
@@ -169,21 +170,22 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
   for (int w0 = from + warp * U * per; w0 < to; w0 += (kThreads / 32) * U * per) {
     int4 c[U];
     float sc[U];
+    bool bad[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int w = w0 + u * per + lane / span;
-      c[u] = make_int4(0, 0, 0, 0);
+      // no conditions around the loads, so that they are under way together: page 0 in the place of what is none
+      const int w = w0 + u * per + lane / span, id = (int)key[min(w, to - 1)];
+      const bool good = id >= 0 && id < p.pages;
+      const int64_t cell = (int64_t)(good ? id : 0) * p.H + h;
+      c[u] = *reinterpret_cast<const int4*>(p.codes + cell * 2 * p.D + min(at, chunks - 1) * 16);
+      sc[u] = p.scales[cell];
+      bad[u] = !good;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!bad[u]) continue;
       sc[u] = nanf("");
-      if (w < to) {
-        const int id = (int)key[w];
-        if (id < 0 || id >= p.pages) {
-          if (at == 0) atomicOr(p.status, PP_CACHE_BAD_PAGE);
-        } else {
-          const int64_t cell = (int64_t)id * p.H + h;
-          if (at < chunks) c[u] = *reinterpret_cast<const int4*>(p.codes + cell * 2 * p.D + at * 16);
-          sc[u] = p.scales[cell];
-        }
-      }
+      if (at == 0 && w0 + u * per + lane / span < to) atomicOr(p.status, PP_CACHE_BAD_PAGE);
     }
     __syncwarp();  // the ids are read before scores take their places
 #pragma unroll
@@ -370,30 +372,23 @@ __global__ void __launch_bounds__(kThreads, 3) select_tile_kernel(const SelectPa
     const int* row = p.table + (int64_t)b * p.width;
     for (int w0 = p.first + warp * 32; w0 < w1; w0 += kThreads) {
       float c[4][4] = {};
+      // no conditions around the loads, so that they are under way together: page 0 in the place of what is none
       float scale[4];
       const int8_t* from[4];
+      int id[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) id[j] = row[min(w0 + j * 8 + g, w1 - 1)];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int w = w0 + j * 8 + g;
-        scale[j] = nanf("");
-        from[j] = nullptr;
-        if (w < w1) {
-          const int id = row[w];
-          if (id < 0 || id >= p.pages) {
-            if (t == 0) atomicOr(p.status, PP_CACHE_BAD_PAGE);
-          } else {
-            const int64_t cell = (int64_t)id * p.H + h;
-            scale[j] = p.scales[cell];
-            from[j] = p.codes + cell * D2 + t * 16;
-          }
-        }
+        const int64_t cell = (int64_t)(id[j] >= 0 && id[j] < p.pages ? id[j] : 0) * p.H + h;
+        scale[j] = p.scales[cell];
+        from[j] = p.codes + cell * D2;
       }
       for (int d0 = 0; d0 < D2; d0 += 64) {
         const bool in = d0 + t * 16 < D2;
         uint4 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          x[j] = in && from[j] ? *reinterpret_cast<const uint4*>(from[j] + d0) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const uint4*>(from[j] + (in ? d0 + t * 16 : 0));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint2 lo = make_uint2(0, 0), hi = lo;
@@ -412,6 +407,12 @@ __global__ void __launch_bounds__(kThreads, 3) select_tile_kernel(const SelectPa
           }
         }
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (id[j] < 0 || id[j] >= p.pages) {
+          scale[j] = nanf("");
+          if (t == 0 && w0 + j * 8 + g < w1) atomicOr(p.status, PP_CACHE_BAD_PAGE);
+        }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
