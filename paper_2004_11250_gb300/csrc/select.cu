@@ -108,17 +108,6 @@ __device__ __forceinline__ void query_codes(const SelectParams& p, int t, int h,
     query_codes_of<T, false>(p, q, lane, store);
 }
 
-__device__ __forceinline__ int dot2_lo(int a, int b, int c) {  // c + a's two 16-bit halves times b's bytes 0 and 1
-  int d;
-  asm("dp2a.lo.s32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ int dot2_hi(int a, int b, int c) {
-  int d;
-  asm("dp2a.hi.s32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-
 __device__ __forceinline__ uint32_t cluster_size() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
@@ -126,12 +115,13 @@ __device__ __forceinline__ uint32_t cluster_size() {
 }
 
 // Single tokens: a cluster per (token, head), its CTAs sharing the pages.  Bound by reading the codes, 2 D bytes a page:
-// a lane keeps 16 of the query's integers and meets 16 codes of every page with two-way integer products.  The first
+// a lane keeps 16 of the query's integers, as 128 hi + lo, and meets 16 codes of every page with four-way integer products.  The first
 // CTA has all scores in shared memory and finds the keep-th largest digit by digit (8 bits each).
 template <class T>
 __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) {
   extern __shared__ uint32_t key[];
-  __shared__ __align__(16) short code[512];
+  __shared__ __align__(16) int8_t code[2][512];  // lo (0 .. 127) and hi of the query's integers
+  __shared__ uint2 ends[8 * kThreads / 32];  // the least and the largest key of every warp of the cluster
   __shared__ int hist[256], warp_sum[kThreads / 32], digit_of, left_of;
   const int rank = cluster_rank(), ranks = cluster_size();
   const int t = blockIdx.x / ranks, h = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
@@ -152,8 +142,10 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
   for (int w = from + tid; w < to; w += kThreads) key[w] = (uint32_t)row[w];
   if (warp == 0)
     query_codes<T>(p, t, h, lane, [&](int d, int up, int down) {
-      code[d] = (short)up;
-      code[p.D + d] = (short)down;
+      code[0][d] = (int8_t)(up & 127);
+      code[1][d] = (int8_t)(up >> 7);
+      code[0][p.D + d] = (int8_t)(down & 127);
+      code[1][p.D + d] = (int8_t)(down >> 7);
     });
   if (ranks > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   __syncthreads();
@@ -162,10 +154,13 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
   int span = 2;
   while (span < chunks) span *= 2;
   const int at = lane % span, per = 32 / span;  // pages per warp at a time
-  int mine[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) mine[i] = at < chunks ? reinterpret_cast<const int*>(code)[at * 8 + i] : 0;
+  int4 lo = make_int4(0, 0, 0, 0), hi = lo;
+  if (at < chunks) {
+    lo = reinterpret_cast<const int4*>(code[0])[at];
+    hi = reinterpret_cast<const int4*>(code[1])[at];
+  }
   const uint32_t keys0 = map_rank((uint32_t)__cvta_generic_to_shared(key), 0);
+  uint32_t mn = ~0u, mx = 0;  // of the keys that this warp makes
   constexpr int U = 8;
   for (int w0 = from + warp * U * per; w0 < to; w0 += (kThreads / 32) * U * per) {
     int4 c[U];
@@ -188,31 +183,50 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
       if (at == 0 && w0 + u * per + lane / span < to) atomicOr(p.status, PP_CACHE_BAD_PAGE);
     }
     __syncwarp();  // the ids are read before scores take their places
+    int sum[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      int sum = dot2_hi(mine[1], c[u].x, dot2_lo(mine[0], c[u].x, 0));
-      sum = dot2_hi(mine[3], c[u].y, dot2_lo(mine[2], c[u].y, sum));
-      sum = dot2_hi(mine[5], c[u].z, dot2_lo(mine[4], c[u].z, sum));
-      sum = dot2_hi(mine[7], c[u].w, dot2_lo(mine[6], c[u].w, sum));
-      for (int d = span / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+      sum[u] = __dp4a(hi.x, c[u].x, __dp4a(hi.y, c[u].y, __dp4a(hi.z, c[u].z, __dp4a(hi.w, c[u].w, 0)))) * 128;
+      sum[u] = __dp4a(lo.x, c[u].x, __dp4a(lo.y, c[u].y, __dp4a(lo.z, c[u].z, __dp4a(lo.w, c[u].w, sum[u]))));
+    }
+    for (int d = span / 2; d > 0; d >>= 1)
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum[u] += __shfl_xor_sync(~0u, sum[u], d);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
       const int w = w0 + u * per + lane / span;
-      if (at == 0 && w < to)
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys0 + 4 * w), "r"(ordered(__fmul_rn((float)sum, sc[u]))) : "memory");
+      const uint32_t v = ordered(__fmul_rn((float)sum[u], sc[u]));
+      mn = min(mn, w < to ? v : ~0u);
+      mx = max(mx, w < to ? v : 0);
+      if (at == 0 && w < to) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys0 + 4 * w), "r"(v) : "memory");
     }
   }
+  mn = __reduce_min_sync(~0u, mn);
+  mx = __reduce_max_sync(~0u, mx);
+  if (lane == 0)
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(map_rank((uint32_t)__cvta_generic_to_shared(&ends[rank * (kThreads / 32) + warp]), 0)),
+                 "r"(mn), "r"(mx) : "memory");
   if (ranks > 1)
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   else
     __syncthreads();
   if (rank != 0) return;
-  // the need-th largest key: thr, with `need` of those equal to it (under the mask of the digits found)
+  // the need-th largest key: thr, with `need` of those equal to it (under the mask of the bits found), digit by digit of 8
+  // bits below the bits that all keys have in common
   int need = p.keep - p.first - p.last;
-  uint32_t thr = 0, mask = 0;
-  for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
+  for (int i = 0; i < ranks * (kThreads / 32); ++i) {
+    mn = min(mn, ends[i].x);
+    mx = max(mx, ends[i].y);
+  }
+  int low = 32 - __clz(mn ^ mx);  // bits not found yet
+  uint32_t mask = low == 32 ? 0 : ~0u << low, thr = mx & mask;
+  while (low > 0 && need > 0) {
+    const int bits = min(low, 8), shift = low - bits;
+    low = shift;
     hist[tid] = 0;
     __syncthreads();
     for (int w = tid; w < N; w += kThreads)
-      if ((key[w] & mask) == thr) atomicAdd(&hist[key[w] >> shift & 255], 1);
+      if ((key[w] & mask) == thr) atomicAdd(&hist[key[w] >> shift & (1 << bits) - 1], 1);
     __syncthreads();
     const int have = hist[255 - tid];  // digits from the largest down
     int sum = have;
@@ -230,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
     }
     __syncthreads();
     thr |= (uint32_t)digit_of << shift;
-    mask |= 255u << shift;
+    mask |= (1u << bits) - 1 << shift;
     need = left_of;
     if (hist[digit_of] == need) break;  // all that start like this
     __syncthreads();
