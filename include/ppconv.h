@@ -531,7 +531,7 @@ typedef struct pp_cache pp_cache;
  *   page    tokens per page: 8, 16, 32, 64, 128 or 256
  *   codes   [pages][H][2][D] int8 and scales [pages][H] fp32 device memory of the
  *           page summaries (pp_cache_summarize), or both NULL: no page selection
- * The handle owns a workspace for attention split over the cache's length, so
+ * The handle owns a workspace (5 to 25 MB) for attention split over the cache's length, so
  * its calls must be ordered with each other (one stream, or events); callers that
  * attend on several streams at once make a handle for each over the same memory.
  * Errors: PP_ERR_INVALID_ARG (null pointer, size, dtype, alignment),
@@ -546,7 +546,7 @@ void pp_cache_destroy(pp_cache* cache);
  * nothing); the word is cleared.  A call that sets a bit skips the entry. */
 #define PP_CACHE_BAD_PAGE 1    /* a page id outside 0..pages-1, or a selected index outside the table */
 #define PP_CACHE_BAD_LENGTH 2  /* a length below 0 or beyond the table (cut to it), or token ranges that do not fit
-                                * (their tokens get no output) */
+                                * (the call's output is then not defined) */
 #define PP_CACHE_BAD_SLOT 4    /* a slot outside -1..pages*page-1 */
 #define PP_CACHE_TIMEOUT 8     /* a bounded wait gave up: the call's output is invalid */
 pp_status pp_cache_device_status(const pp_cache* cache, int* device_error);

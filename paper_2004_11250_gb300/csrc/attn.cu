@@ -862,10 +862,10 @@ DeviceOnce g_attn_once;
 
 namespace ppc {
 
-AttnSpace attn_space(int, int D, int sms) {
+AttnSpace attn_space(int dtype, int D, int sms) {
   const int DP = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   const size_t ctas = (size_t)std::min(sms * (DP <= 128 ? 2 : 1), kMaxCtas);
-  return {ctas * 3 * 4, ctas * 2 * (kRows * DP + 2 * kRows) * 4};
+  return {ctas * 3 * 4, ctas * 2 * (kRows * DP + 2 * kRows) * 4, tile_space(dtype, D, sms)};
 }
 
 cudaError_t attn_prepare() {
@@ -907,9 +907,9 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
   if (units * c.H >= INT32_MAX / deep || (int64_t)T * G >= INT32_MAX) return PP_ERR_UNSUPPORTED;
   AttnParams p = {q,     q_ts,   q_hs,        c.k,        c.v,     starts, table, lens, sel,  out, lse, c.status, c.counters,
                   c.partial, scale, T, B, c.H, c.D, c.page, log2_of(c.page), c.pages, width, keep, flags & PP_ATTN_CAUSAL,
-                  FastDiv(G), FastDiv(c.H), FastDiv(std::max(keep, 1))};
+                  FastDiv(G), FastDiv(c.H), FastDiv(std::max(keep, 1)), 1, nullptr, nullptr};
   const cudaStream_t s = (cudaStream_t)stream;
-  const cudaError_t e = tile_applicable(p, c.dtype, sms) ? tile_launch(p, c, s)
+  const cudaError_t e = tile_applicable(p, c.dtype, sms) ? tile_launch(p, c, sms, s)
                         : c.dtype == PP_F32 ? by_head<float>(p, c, sms, s)
                         : c.dtype == PP_F16 ? by_head<__half>(p, c, sms, s)
                                             : by_head<__nv_bfloat16>(p, c, sms, s);

@@ -26,6 +26,10 @@ struct AttnParams {
   float scale;
   int T, B, H, D, page, log_page, pages, width, keep, causal;
   FastDiv G, by_head, by_keep;  // by the group's heads, by H, by keep
+  // tiles: shares that their blocks are split into, and the rows' sums and (maximum, total) of each share
+  int splits;
+  float* split_sums;
+  float2* split_stats;
 };
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
@@ -49,6 +53,7 @@ __device__ __forceinline__ float ex2(float x) {
 // attn_tile.cu: tiles of 128 query rows on the tensor cores, for 16-bit types and heads of up to 128.
 bool tile_applicable(const AttnParams& p, int dtype, int sms);
 cudaError_t tile_prepare();
-cudaError_t tile_launch(const AttnParams& p, const pp_cache& c, cudaStream_t stream);
+size_t tile_space(int dtype, int D, int sms);  // device bytes of the shares' sums
+cudaError_t tile_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t stream);
 
 }  // namespace ppc_attn

@@ -34,6 +34,7 @@ constexpr int kKeys = 64;              // keys per block
 constexpr int kStages = 2;             // of K and of V
 constexpr int kInfo = 4;               // blocks that the copying warp may be ahead of the softmax, and one
 constexpr int kMaskWords = 2048;       // token bits of the pages in one window
+constexpr int kSplits = 8;             // shares of a tile's blocks at most
 constexpr float kGrow = 8.f;           // log2 of how far a row's scores may pass its m
 
 template <int DP>
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
 
   // ---- which tile: those of a sequence's last tokens, which see the most keys, come first
   const int TT = kRowsT / p.G.d;  // tokens per tile
-  const int h = blockIdx.x % p.H, order = blockIdx.x / p.H;
+  const int z = blockIdx.x % p.splits, h = blockIdx.x / p.splits % p.H, order = blockIdx.x / p.splits / p.H;
   if (tid == 0) {
     dead = 0;
     tile_of[0] = -1;
@@ -387,8 +388,10 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       __syncthreads();
       npieces = sum << log_pp;
     }
-    const int n = (npieces + pieces - 1) >> log_pc;  // blocks of the window
-    // piece i: its first key, -1 beyond the last
+    // this CTA's share of the window's blocks, and its first piece
+    const int blocks = (npieces + pieces - 1) >> log_pc, first = blocks * z / p.splits;
+    const int n = blocks * (z + 1) / p.splits - first, i0 = first << log_pc;
+    // piece i of the window: its first key, -1 beyond the last
     auto key_of = [&](int i) {
       if (i >= npieces) return -1;
       return p.sel ? ((w0 + list[i >> log_pp]) << p.log_page) + ((i & (1 << log_pp) - 1) << log_br) : i << log_br;
@@ -399,7 +402,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       // copied
       const uint32_t leader = elect();
       for (int k0 = 0; k0 < n; k0 += 32 >> log_pc) {
-        const int key = key_of((k0 << log_pc) + lane);
+        const int key = key_of(i0 + (k0 << log_pc) + lane);
         int have = key < 0 ? 0 : max(0, min(BR, lim_max - key)), y = 0;
         if (have > 0) {
           const int id = table[key >> p.log_page];
@@ -489,9 +492,9 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         uint64_t see = 0;
         const Block& bl = info[g % kInfo];
         if (log_pc == 0) {  // a page, or a piece of one
-          const int key = key_of(k);
+          const int key = key_of(i0 + k);
           bool on = live_row && key >= 0;
-          if (on && p.sel) on = masks[list[k >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
+          if (on && p.sel) on = masks[list[i0 + k >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
           hold(&info_full[g % kInfo], g / kInfo & 1);
           const int c = on ? min(bl.have[0], lim - key) : 0;
           see = c >= 64 ? ~0ull : c > 0 ? (1ull << c) - 1 : 0;
@@ -499,7 +502,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           hold(&info_full[g % kInfo], g / kInfo & 1);
 #pragma unroll 1
           for (int j = 0; j < pieces; ++j) {
-            const int i = (k << log_pc) + j, key = key_of(i);
+            const int i = i0 + (k << log_pc) + j, key = key_of(i);
             bool on = live_row && key >= 0;
             if (on && p.sel) on = masks[list[i >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
             const int c = on ? min(bl.have[j], lim - key) : 0;
@@ -601,6 +604,25 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     __syncwarp();
     tm_fence_after();
     const int64_t cell = (int64_t)(t0 + p.G.div(live_row ? tid : 0)) * p.H * p.G.d + h * p.G.d + p.G.mod(live_row ? tid : 0);
+    if (p.splits > 1) {  // sums as they are, for the joining kernel
+      const int64_t at = (int64_t)z * p.T * p.H * p.G.d + cell;
+#pragma unroll
+      for (int c = 0; c < DP; c += 32) {
+        float o[32];
+        if (done > 0) {
+          tm_ld32(row_tm + c, o);
+          tm_wait_ld();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+        }
+        if (live_row)
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            *reinterpret_cast<float4*>(p.split_sums + at * DP + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+      }
+      if (live_row) p.split_stats[at] = make_float2(m, l);
+    } else {
     T* dst = static_cast<T*>(p.out) + cell * p.D;
     const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 15) == 0;
     const float scale = l == 0.f ? 0.f : 1.f / l;
@@ -639,8 +661,9 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       again &= again - 1;
       const int64_t at = (int64_t)(t0 + tk) * p.H * p.G.d + h * p.G.d + p.G.mod(r);
       redo_row<T, DP>(p, q + (t0 + tk) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs, table,
-                      p.sel ? p.sel + ((int64_t)(t0 + tk) * p.H + h) * p.keep : nullptr, h, limit(tk), sl,
+                      p.sel ? p.sel + ((int64_t)(t0 + tk) * p.H + h) * p.keep : nullptr, h, limit(tk), p.scale * 1.44269504f,
                       static_cast<T*>(p.out) + at * p.D, p.lse ? p.lse + at : nullptr);
+    }
     }
     tm_fence_before();
   }
@@ -658,16 +681,70 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   }
 }
 
+// The splits' sums of a row into its output: a warp per (token, query head).
+template <class T, int DP>
+__global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_constant__ AttnParams p) {
+  after_previous();
+  const int Hq = p.H * p.G.d, lane = threadIdx.x % 32;
+  const int64_t cells = (int64_t)p.T * Hq, cell = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  if (cell >= cells) return;
+  float m = -INFINITY, l = 0.f;
+  float2 st[kSplits];
+#pragma unroll
+  for (int z = 0; z < kSplits; ++z) {
+    st[z] = z < p.splits ? p.split_stats[z * cells + cell] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(m, st[z].x);
+  }
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int d = lane * 4 < DP ? lane * 4 : 0;
+#pragma unroll
+  for (int z = 0; z < kSplits; ++z) {
+    if (st[z].y == 0.f) continue;
+    const float w = ex2(st[z].x - m);
+    const float4 a = *reinterpret_cast<const float4*>(p.split_sums + (z * cells + cell) * DP + d);
+    l += w * st[z].y;
+    o.x += w * a.x;
+    o.y += w * a.y;
+    o.z += w * a.z;
+    o.w += w * a.w;
+  }
+  const bool in = lane * 4 < p.D;
+  const bool odd = in && !(isfinite(o.x) && isfinite(o.y) && isfinite(o.z) && isfinite(o.w));
+  const int t = (int)(cell / Hq), hq = (int)(cell - (int64_t)t * Hq);
+  T* out = static_cast<T*>(p.out) + cell * p.D;
+  float* lse = p.lse ? p.lse + cell : nullptr;
+  if (__any_sync(~0u, odd) && (p.sel || p.causal)) {
+    const Seen s = seen_keys(t, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
+    const int h = p.G.div(hq);
+    redo_row<T, DP>(p, static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)hq * p.q_hs, p.table + (int64_t)s.b * p.width,
+                    p.sel ? p.sel + ((int64_t)t * p.H + h) * p.keep : nullptr, h, s.keys, p.scale * 1.44269504f, out, lse);
+    return;
+  }
+  const float n = l == 0.f ? 0.f : 1.f / l;
+  if (in) {
+    const Vec<T, 4> y = {from_f32<T>(o.x * n), from_f32<T>(o.y * n), from_f32<T>(o.z * n), from_f32<T>(o.w * n)};
+    if ((reinterpret_cast<uintptr_t>(p.out) & 7) == 0) {
+      *reinterpret_cast<Vec<T, 4>*>(out + d) = y;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[d + e] = y.v[e];
+    }
+  }
+  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
+}
+
 template <class T, int DP>
 cudaError_t prepare_one() {
   return cudaFuncSetAttribute(attn_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
 }
 
-template <class T>
+template <class T, int DP>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int64_t grid, cudaStream_t stream) {
-  const dim3 blocks((unsigned)grid);
-  return p.D <= 64 ? launch_after(attn_tile_kernel<T, 64>, blocks, kThreadsT, TileShape<64>::SMEM, stream, 1, p, c.mk, c.mv)
-                   : launch_after(attn_tile_kernel<T, 128>, blocks, kThreadsT, TileShape<128>::SMEM, stream, 1, p, c.mk, c.mv);
+  const cudaError_t e = launch_after(attn_tile_kernel<T, DP>, dim3((unsigned)grid), kThreadsT, TileShape<DP>::SMEM, stream, 1,
+                                     p, c.mk, c.mv);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  const int64_t cells = (int64_t)p.T * p.H * p.G.d;
+  return launch_after(attn_tile_join_kernel<T, DP>, dim3((unsigned)((cells + 7) / 8)), 256, 0, stream, 1, p);
 }
 
 }  // namespace
@@ -676,10 +753,12 @@ namespace ppc_attn {
 
 bool tile_applicable(const AttnParams& p, int dtype, int sms) {
   if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
-  // Rows of units (attn.cu) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where
-  // pages are selected) at about 1 us per 64 keys and CTA; a tile meets it with 128 in about half of that.
-  const int64_t tiles = ((int64_t)p.T * p.G.d + kRowsT - 1) / kRowsT * p.H, units = ((int64_t)p.T * p.G.d + 15) / 16 * p.H;
-  return (tiles + 2 * sms - 1) / (2 * sms) * sms < units;
+  // Units of rows (attn.cu) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where pages
+  // are selected) at about 1 us per 64 keys and CTA; a tile meets it with 128 in about the same, split 8 times at most.
+  // Selected pages: neighbouring tokens' together are some four times one token's.
+  const int64_t tiles = ((int64_t)p.T * p.G.d + kRowsT - 1) / kRowsT * p.H;
+  const int64_t units = p.sel ? (int64_t)p.T * ((p.G.d + 7) / 8) * p.H : ((int64_t)p.T * p.G.d + 15) / 16 * p.H;
+  return std::max<int64_t>(tiles, 2 * sms / kSplits) * (p.sel ? 4 : 1) < units;
 }
 
 cudaError_t tile_prepare() {
@@ -690,12 +769,27 @@ cudaError_t tile_prepare() {
   return e;
 }
 
-cudaError_t tile_launch(const AttnParams& p, const pp_cache& c, cudaStream_t stream) {
+size_t tile_space(int dtype, int D, int sms) {
+  return dtype == PP_F32 || D > 128 ? 0 : (size_t)2 * sms * kRowsT * ((D <= 64 ? 64 : 128) + 2) * 4;
+}
+
+cudaError_t tile_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t stream) {
   // each sequence adds at most one tile that is not full; CTAs beyond the last tile leave
-  const int TT = kRowsT / p.G.d;
-  const int64_t grid = ((int64_t)p.T / TT + std::min(p.T, p.B)) * p.H;
+  const int TT = kRowsT / p.G.d, DP = p.D <= 64 ? 64 : 128;
+  const int64_t tiles = ((int64_t)p.T / TT + std::min(p.T, p.B)) * p.H;
+  // Few tiles are split along their blocks, up to two CTAs per SM, where a share still has some 16 blocks: a CTA spends
+  // the time of about 8 on its queries and masks (3 chunks of 333 tokens, 8 heads of 64: 71 us whole).
+  const int64_t cells = (int64_t)p.T * p.H * p.G.d, room = (int64_t)2 * sms * kRowsT;
+  const int64_t pages = p.sel ? std::min<int64_t>(p.width, (int64_t)TT * p.keep) : p.width;
+  const int64_t splits = std::min({(int64_t)kSplits, 2 * sms / tiles, pages * p.page / kKeys / 16, room / cells});
+  p.splits = (int)std::max<int64_t>(1, splits);
+  p.split_sums = c.tiles;
+  p.split_stats = reinterpret_cast<float2*>(c.tiles + room * DP);
+  const int64_t grid = tiles * p.splits;
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return c.dtype == PP_F16 ? launch<__half>(p, c, grid, stream) : launch<__nv_bfloat16>(p, c, grid, stream);
+  return c.dtype == PP_F16 ? (DP == 64 ? launch<__half, 64>(p, c, grid, stream) : launch<__half, 128>(p, c, grid, stream))
+                           : (DP == 64 ? launch<__nv_bfloat16, 64>(p, c, grid, stream)
+                                       : launch<__nv_bfloat16, 128>(p, c, grid, stream));
 }
 
 }  // namespace ppc_attn

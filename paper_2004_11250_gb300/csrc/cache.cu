@@ -139,7 +139,8 @@ pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k,
   }
   const AttnSpace space = attn_space(dtype, D, sms);
   const size_t head = 256 + (space.counters + 255) / 256 * 256;
-  cudaError_t e = cudaMalloc(&c->dmem, head + space.partial);
+  const size_t partial = (space.partial + 255) / 256 * 256;
+  cudaError_t e = cudaMalloc(&c->dmem, head + partial + space.tiles);
   if (e != cudaSuccess) {
     cudaGetLastError();
     delete c;
@@ -154,6 +155,7 @@ pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k,
   c->status = static_cast<int*>(c->dmem);
   c->counters = reinterpret_cast<int*>(static_cast<char*>(c->dmem) + 256);
   c->partial = reinterpret_cast<float*>(static_cast<char*>(c->dmem) + head);
+  c->tiles = reinterpret_cast<float*>(static_cast<char*>(c->dmem) + head + partial);
   *out = c;
   return PP_OK;
 }

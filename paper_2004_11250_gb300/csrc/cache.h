@@ -30,6 +30,7 @@ struct pp_cache {
   int* status = nullptr;
   int* counters = nullptr;   // zero between calls
   float* partial = nullptr;
+  float* tiles = nullptr;
   CUtensorMap mk, mv;        // the pools as rows of D values; boxes of one 128-byte column of a page's rows
 };
 
@@ -37,9 +38,9 @@ namespace ppc {
 
 // The row kernel's keys per tile (attn.cu): 64 rows of 16-bit values, 32 of fp32.
 inline int tile_keys(int dtype) { return dtype == PP_F32 ? 32 : 64; }
-// Device bytes that attention needs beside the status word: counters, then partial results.
+// Device bytes that attention needs beside the status word: counters, partial results, shares of tiles.
 struct AttnSpace {
-  size_t counters, partial;
+  size_t counters, partial, tiles;
 };
 AttnSpace attn_space(int dtype, int D, int sms);
 cudaError_t attn_prepare();

@@ -681,8 +681,8 @@ TILES = [
 ]
 
 
-def tile_kernel_runs(c, tmp_path, sel=None):
-    """Whether this call launches the tile kernel, from a captured graph's dump."""
+def kernels_of(c, tmp_path, sel=None):
+    """The names of the attention kernels that this call launches, from a captured graph's dump."""
     g = torch.cuda.CUDAGraph(keep_graph=True)
     g.enable_debug_mode()
     with torch.cuda.graph(g):
@@ -693,7 +693,11 @@ def tile_kernel_runs(c, tmp_path, sel=None):
         g.debug_dump(str(dot))
     names = re.findall(r"attn_\w*kernel", dot.read_text())
     assert names
-    return any("tile" in n for n in names)
+    return names
+
+
+def tile_kernel_runs(c, tmp_path, sel=None):
+    return any("attn_tile_kernel" in n for n in kernels_of(c, tmp_path, sel))
 
 
 @pytest.mark.parametrize("dt,G,H,D,page,lens,tokens", TILES)
@@ -810,3 +814,54 @@ def test_tiles_same_bits(pp):
         c.check()
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("dt,G,H,D,page,lens,tokens", [(BF16, 4, 2, 128, 64, [7000], [300]), (F16, 8, 1, 64, 16, [3000, 500, 40], [300, 1, 40]),
+                                                      (BF16, 3, 2, 80, 128, [9000, 2500], [150, 200])])
+def test_tiles_split(pp, tmp_path, dt, G, H, D, page, lens, tokens):
+    """Few tiles over many blocks: shares of them in CTAs of their own, joined; a selection; values that are not finite."""
+    c = Case(pp, dt, G, H, D, page, lens, tokens, seed=D + G)
+    try:
+        assert any("join" in n for n in kernels_of(c, tmp_path))
+        c.check()
+        c.check(causal=False, scale=-0.3)
+        g = torch.Generator().manual_seed(2)
+        keep = 2048 // page
+        sel = torch.full((c.T, H, keep), -1, dtype=torch.int32)
+        for t, (b, n) in enumerate(ref.seen_keys(c.T, c.starts, lens, True)):
+            some = torch.randperm(-(-n // page), generator=g)[:keep]
+            sel[t, :, : len(some)] = some.to(torch.int32)
+        c.check(sel=sel)
+        again, _ = c.attend(sel=sel.cuda())
+        assert torch.equal(again, c.attend(sel=sel.cuda())[0])
+        key = lens[0] - tokens[0] // 2
+        c.v[int(c.table[0, key // page]), 0, key % page, 5] = math.nan
+        c.k[int(c.table[0, key // page]), 0, key % page, 3] = math.inf
+        c.kd.copy_(c.k)
+        c.vd.copy_(c.v)
+        for scale in (0.125, -0.125):
+            out, _ = c.attend(scale=scale)
+            want, _, tol, _ = ref.attend(c.q, c.k, c.v, c.table, c.starts, lens, scale, True)
+            fine, got = torch.isfinite(want), out.double().cpu()
+            assert torch.equal(torch.isfinite(got), fine)
+            assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
+def test_not_finite_at_a_negative_scale(pp):
+    """Rows computed again for a value that others see: with the sign of the scale."""
+    for tokens in ([400], [40]):
+        c = Case(pp, BF16, 4, 2, 64, 16, [500], tokens, seed=12)
+        try:
+            c.v[int(c.table[0, 480 // 16]), 0, 480 % 16, 5] = math.nan
+            c.vd.copy_(c.v)
+            for scale in (-0.2, 0.0):
+                out, _ = c.attend(scale=scale)
+                want, _, tol, _ = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.lens, scale, True)
+                fine, got = torch.isfinite(want), out.double().cpu()
+                assert torch.equal(torch.isfinite(got), fine)
+                assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
+        finally:
+            c.close()
