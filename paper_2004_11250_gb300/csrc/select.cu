@@ -355,20 +355,20 @@ __global__ void __launch_bounds__(kThreads, 3) select_tile_kernel(const SelectPa
   const int t0 = blockIdx.x * kTokens, h = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   const int nt = min(kTokens, p.T - t0), D2 = 2 * p.D, cs = D2 + 4, stride = p.width + 4;  // rows 2 and 4 banks apart
   after_previous();
-  // ---- the tokens' sequences and integers, a warp per token
+  // ---- the tokens' sequences, a lane each, and their integers, a warp per token
+  if (warp == 0 && lane < kTokens) {
+    Seen s = {-1, 0};
+    if (lane < nt) s = seen_keys(t0 + lane, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
+    row_b[lane] = s.b;
+    row_P[lane] = (s.keys + p.page - 1) / p.page;
+  }
+  __syncthreads();
   for (int r = warp; r < kTokens; r += kThreads / 32) {
-    Seen s = {0, 0};
-    if (r < nt) s = seen_keys(t0 + r, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
-    const int P = (s.keys + p.page - 1) / p.page;
-    if (lane == 0) {
-      row_b[r] = r < nt ? s.b : -1;
-      row_P[r] = P;
-    }
     auto store = [&](int d, int up, int down) {
       code[r * cs + d] = __int2half_rn(up);
       code[r * cs + p.D + d] = __int2half_rn(down);
     };
-    if (r < nt && P > p.keep) {
+    if (r < nt && row_P[r] > p.keep) {
       query_codes<T>(p, t0 + r, h, lane, store);
     } else {
       for (int d = lane; d < p.D; d += 32) store(d, 0, 0);
