@@ -195,9 +195,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   after_previous();
-  // every thread looks after a run of items
-  const int per = (NI + kThreads - 1) / kThreads;
-  const int i0 = min(NI, tid * per), i1 = min(NI, i0 + per);
+  // Every thread looks after a run of items; of few, every warp for itself, so that no warp waits for another.
+  const bool small = NI <= 128;
+  const int team = small ? 32 : kThreads, me = small ? lane : tid;
+  const int per = (NI + team - 1) / team;
+  const int i0 = min(NI, me * per), i1 = min(NI, i0 + per);
   int tiles = 0, units = 0;
   bool bad_range = false;
   Walk w;
@@ -208,14 +210,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     bad_range = bad_range || w.n < 0;
   }
   const int grid = gridDim.x;
-  // block-wide sums of N numbers
+  // sums of N numbers over the team
   auto sums_of = [&](auto& v) {
     constexpr int N = sizeof(v) / sizeof(int);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = __reduce_add_sync(~0u, v[i]);
-      if (lane == 0) scan[i][warp] = v[i];
-    }
+    for (int i = 0; i < N; ++i) v[i] = __reduce_add_sync(~0u, v[i]);
+    if (small) return;
+    if (lane == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) scan[i][warp] = v[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -261,28 +264,45 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     const int up = __shfl_up_sync(~0u, before, d);
     if (lane >= d) before += up;
   }
-  if (lane == 31) scan[0][warp] = before;
-  __syncthreads();
-  int total = 0;
+  int total = __shfl_sync(~0u, before, 31);
+  if (!small) {
+    if (lane == 31) scan[0][warp] = before;
+    __syncthreads();
+    total = 0;
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) {
-    if (i < warp) before += scan[0][i];
-    total += scan[0][i];
+    for (int i = 0; i < kThreads / 32; ++i) {
+      if (i < warp) before += scan[0][i];
+      total += scan[0][i];
+    }
   }
   before -= mine;
   if ((int64_t)blockIdx.x * run >= total) return;
   const int x0 = blockIdx.x * run, x1 = min(total, x0 + run);
-  if (x0 >= before && x0 < before + mine) {
+  const bool has = x0 >= before && x0 < before + mine;
+  if (has) {
     for (int i = i0;; ++i) {
       if (per > 1) load_item(p, TK, R, whole, i, w);
       if (x0 < before + w.places) break;
       before += w.places;
     }
     w.base = before;
-    found = w;
+    if (!small) found = w;
   }
-  __syncthreads();
-  w = found;
+  if (small) {
+    const int from = __ffs(__ballot_sync(~0u, has)) - 1;
+    w.base = __shfl_sync(~0u, w.base, from);
+    w.item = __shfl_sync(~0u, w.item, from);
+    w.t0 = __shfl_sync(~0u, w.t0, from);
+    w.n = __shfl_sync(~0u, w.n, from);
+    w.len = __shfl_sync(~0u, w.len, from);
+    w.rows = __shfl_sync(~0u, w.rows, from);
+    w.units = __shfl_sync(~0u, w.units, from);
+    w.kt = __shfl_sync(~0u, w.kt, from);
+    w.span = __shfl_sync(~0u, w.span, from);
+    w.places = __shfl_sync(~0u, w.places, from);
+  }
+  __syncthreads();  // the barriers are set up, too
+  if (!small) w = found;
   const int log_br = min(p.log_page, S::LOG_TK), BR = 1 << log_br, pieces = TK >> log_br;
   const float sl = p.scale * 1.44269504f;  // softmax in powers of two
 
