@@ -474,10 +474,13 @@ def _heads(t, dtype, T, D):
     """(pointer, token stride, head stride, heads) of a view [T][heads][D] of torch type dtype; None is no heads."""
     if t is None:
         return None, 0, 0, 0
-    shape, stride = t.shape, t.stride()
-    if t.dtype is not dtype or len(shape) != 3 or shape[0] != T or shape[2] != D or stride[2] != 1:
-        raise PPError(PP_ERR_INVALID_ARG, "a token tensor is [T][heads][D] of the call's type, dense in D")
-    return t.data_ptr(), stride[0], stride[1], shape[1]
+    try:
+        (t0, h, d), (ts, hs, ds) = t.shape, t.stride()
+        if t0 == T and d == D and ds == 1 and t.dtype is dtype:
+            return t.data_ptr(), ts, hs, h
+    except ValueError:  # not three axes
+        pass
+    raise PPError(PP_ERR_INVALID_ARG, "a token tensor is [T][heads][D] of the call's type, dense in D")
 
 
 def _dense(t, shape, dtype, where):
@@ -527,8 +530,9 @@ def pp_qk_rotate(rope, pos, eps, q, qw, q_out, k, kw, k_out, stream=None):
     qp, qt, qh, Hq = _heads(q, dt, T, D)
     kp, kt, kh, Hk = _heads(k, dt, T, D)
     _check(lib.pp_qk_rotate(rope, code, T, _dense(pos, (rope.axes, T), y.i32, "pos"), eps, qp, qt, qh, Hq,
-                            _dense(qw, (D,), y.f32, "qw"), _dense(q_out, (T, Hq, D), dt, "q_out"), kp, kt, kh, Hk,
-                            _dense(kw, (D,), y.f32, "kw"), _dense(k_out, (T, Hk, D), dt, "k_out"), _stream(stream)),
+                            _dense(qw, (D,), y.f32, "qw"), None if q is None else _dense(q_out, q.shape, dt, "q_out"), kp,
+                            kt, kh, Hk, _dense(kw, (D,), y.f32, "kw"),
+                            None if k is None else _dense(k_out, k.shape, dt, "k_out"), _stream(stream)),
            "pp_qk_rotate")
 
 
@@ -560,16 +564,18 @@ def pp_cache_device_status(cache) -> int:
 
 def pp_qkv_store(rope, cache, pos, slots, eps, q, qw, q_out, k, kw, v, stream=None):
     """pp_qk_rotate with the keys, and the values as they are, stored to slots [T] (int32) of the cache."""
-    T, D, dt, y = k.shape[0], rope.D, cache.dtype, _torch_types()
-    H = cache.shape[1]
+    D, dt, y = rope.D, cache.dtype, _torch_types()
+    H, shape = cache.shape[1], k.shape
+    T = shape[0]
+    kt, kh, kd = k.stride()
+    vt, vh, vd = v.stride()
+    if not (shape == v.shape == (T, H, D) and k.dtype is dt and v.dtype is dt and kd == 1 and vd == 1):
+        raise PPError(PP_ERR_INVALID_ARG, "pp_qkv_store: k and v are [T][the cache's heads][D] of its type, dense in D")
     qp, qt, qh, Hq = _heads(q, dt, T, D)
-    kp, kt, kh, Hk = _heads(k, dt, T, D)
-    vp, vt, vh, Hv = _heads(v, dt, T, D)
-    if Hk != H or Hv != H:
-        raise PPError(PP_ERR_INVALID_ARG, "pp_qkv_store: k and v have the cache's heads")
     _check(lib.pp_qkv_store(rope, cache, T, _dense(pos, (rope.axes, T), y.i32, "pos"), _dense(slots, (T,), y.i32, "slots"),
-                            eps, qp, qt, qh, Hq, _dense(qw, (D,), y.f32, "qw"), _dense(q_out, (T, Hq, D), dt, "q_out"),
-                            kp, kt, kh, _dense(kw, (D,), y.f32, "kw"), vp, vt, vh, _stream(stream)), "pp_qkv_store")
+                            eps, qp, qt, qh, Hq, _dense(qw, (D,), y.f32, "qw"),
+                            None if q is None else _dense(q_out, q.shape, dt, "q_out"), k.data_ptr(), kt, kh,
+                            _dense(kw, (D,), y.f32, "kw"), v.data_ptr(), vt, vh, _stream(stream)), "pp_qkv_store")
 
 
 def pp_cache_summarize(cache, ids, stream=None):
