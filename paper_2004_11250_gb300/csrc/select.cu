@@ -9,7 +9,11 @@
 // Two kernels: for single tokens, integer products by a cluster per (token, head),
 // bound by reading the codes once; for many tokens, 16 of them at a time on the
 // tensor cores (mma.sync m16n8k16, f16), bound by neither bytes nor products but
-// by the search for the keep-th largest score.
+// by instructions: the codes' conversion and the search for the keep-th largest score
+// (in 8-bit products, m16n8k32 with the integers as 128 hi + lo: 96 us against 71).
+//
+// Measured, 32 heads over 8, D = 128: one token over 625 pages 7.7 us, 32 tokens over up
+// to 512 pages 12.4 us (chains of latencies), 2048 tokens over 512 pages 71 us.
 #include <algorithm>
 
 #include "cache.h"
