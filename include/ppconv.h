@@ -534,6 +534,7 @@ typedef struct pp_cache pp_cache;
  * The handle owns a workspace (5 to 25 MB) for attention split over the cache's length, so
  * its calls must be ordered with each other (one stream, or events); callers that
  * attend on several streams at once make a handle for each over the same memory.
+ * Synchronous, allocates: not during stream capture.
  * Errors: PP_ERR_INVALID_ARG (null pointer, size, dtype, alignment),
  * PP_ERR_UNSUPPORTED (page size; D not a multiple of 8 in 16..256; pages * H *
  * page not below 2^31), PP_ERR_CUDA, PP_ERR_OOM.
@@ -614,7 +615,8 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  * What the cache holds outside the visible keys is never used, NaN and infinities included.
  * Asynchronous on stream, no allocation; the same inputs give the same bits.
  * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, flags, scale not finite),
- * PP_ERR_UNSUPPORTED (width * page not below 2^31), PP_ERR_CUDA.
+ * PP_ERR_UNSUPPORTED (width * page not below 2^31; or T * Hq * width * page above some 2^40 in
+ * fp32 or with D > 128), PP_ERR_CUDA.
  */
 pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
                           const int32_t* starts, const int32_t* table, int width, const int32_t* lens, float scale,

@@ -850,6 +850,11 @@ cudaError_t prepare_one() {
 
 template <class T, int DP, int RB>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
+  // all tiles, at most: they are counted in 32 bits
+  constexpr int R = Shape<T, DP, RB>::R, TK = Shape<T, DP, RB>::TK;
+  const int64_t units = (p.sel ? (int64_t)p.T * ((p.G.d + R - 1) / R) : ((int64_t)p.T * p.G.d + (int64_t)p.B * (R - 1)) / R) * p.H;
+  const int64_t deep = ((int64_t)(p.sel ? std::min(p.width, p.keep) : p.width) * p.page + TK - 1) / TK;
+  if (units >= INT32_MAX / deep) return cudaErrorNotSupported;
   const int grid = std::min(sms * Shape<T, DP, RB>::CTAS, kMaxCtas);
   return launch_after(attn_kernel<T, DP, RB>, dim3(grid), kThreads, Shape<T, DP, RB>::SMEM, stream, 1, p, c.mk, c.mv);
 }
@@ -927,10 +932,7 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
   if (sms <= 0) return PP_ERR_CUDA;
   const pp_cache& c = *cache;
   const int G = Hq / c.H;
-  // all tiles, at most: they are counted in 32 bits
-  const int64_t units = sel ? (int64_t)T * ((G + 1) / 2) : ((int64_t)T * G + B) / 2;
-  const int64_t deep = std::max<int64_t>(1, ((int64_t)(sel ? std::min(width, keep) : width) * c.page + tile_keys(c.dtype) - 1) / tile_keys(c.dtype));
-  if (units * c.H >= INT32_MAX / deep || (int64_t)T * G >= INT32_MAX) return PP_ERR_UNSUPPORTED;
+  if ((int64_t)T * G >= INT32_MAX) return PP_ERR_UNSUPPORTED;
   AttnParams p = {q,     q_ts,   q_hs,        c.k,        c.v,     starts, table, lens, sel,  out, lse, c.status, c.counters,
                   c.partial, scale, T, B, c.H, c.D, c.page, log2_of(c.page), c.pages, width, keep, flags & PP_ATTN_CAUSAL,
                   FastDiv(G), FastDiv(c.H), FastDiv(std::max(keep, 1)), 1, nullptr, nullptr};
@@ -939,5 +941,5 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
                         : c.dtype == PP_F32 ? by_head<float>(p, c, sms, s)
                         : c.dtype == PP_F16 ? by_head<__half>(p, c, sms, s)
                                             : by_head<__nv_bfloat16>(p, c, sms, s);
-  return e == cudaSuccess ? PP_OK : PP_ERR_CUDA;
+  return e == cudaSuccess ? PP_OK : e == cudaErrorNotSupported ? PP_ERR_UNSUPPORTED : PP_ERR_CUDA;
 }
