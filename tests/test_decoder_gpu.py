@@ -865,3 +865,27 @@ def test_not_finite_at_a_negative_scale(pp):
                 assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
         finally:
             c.close()
+
+
+@pytest.mark.parametrize("tokens", [None, [40]])
+@pytest.mark.parametrize("G,D", [(8, 128), (16, 64), (3, 256)])
+def test_select_sums_near_their_largest(pp, G, D, tokens):
+    """Integers of 23 and 24 bits whose last one decides: every code and every query near its largest."""
+    page, n, keep = 8, 900, 12
+    c = Case(pp, F32, G, 1, D, page, [n], tokens, seed=3, summaries=True, trash=False)
+    try:
+        g = torch.Generator().manual_seed(7)
+        pages = c.k.shape[0]
+        codes = torch.randint(125, 128, (pages, 1, 2, D), generator=g).to(torch.int8)
+        codes[:, :, 1] = torch.randint(-127, -120, (pages, 1, D), generator=g).to(torch.int8)
+        scales = torch.ones((pages, 1))
+        c.q = 1.0 - 0.02 * torch.rand(c.q.shape, generator=g)
+        c.q[:, 0, 0] = 1.0
+        c.codes.copy_(codes)
+        c.scales.copy_(scales)
+        c.qd.copy_(c.q)
+        sel = torch.empty((c.T, 1, keep), dtype=torch.int32, device="cuda")
+        pp.pp_cache_select(c.cache, c.qd, c.sd, c.td, c.ld, pp.PP_ATTN_CAUSAL, 1, 2, sel)
+        assert torch.equal(sel.cpu(), ref.select(c.q, codes, scales, c.table, c.starts, [n], True, page, 1, 2, keep))
+    finally:
+        c.close()
