@@ -784,11 +784,12 @@ cudaError_t tile_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t s
   // each sequence adds at most one tile that is not full; CTAs beyond the last tile leave
   const int TT = kRowsT / p.G.d, DP = p.D <= 64 ? 64 : 128;
   const int64_t tiles = ((int64_t)p.T / TT + std::min(p.T, p.B)) * p.H;
-  // Few tiles are split along their blocks, up to two CTAs per SM, where a share still has some 16 blocks: a CTA spends
-  // the time of about 8 on its queries and masks (3 chunks of 333 tokens, 8 heads of 64: 71 us whole).
+  // Few tiles are split along their blocks, up to two CTAs per SM, while a share can have 4 blocks (a CTA spends the time of
+  // about 8 on its queries and masks, but side by side with the others).  3 chunks of 333 tokens, 8 heads of 64: 71 us
+  // whole, 35 in four shares; 119 tokens of 2 heads over 1720 keys, with their selection: 50 us whole, 31 in shares.
   const int64_t cells = (int64_t)p.T * p.H * p.G.d, room = (int64_t)2 * sms * kRowsT;
   const int64_t pages = p.sel ? std::min<int64_t>(p.width, (int64_t)TT * p.keep) : p.width;
-  const int64_t splits = std::min({(int64_t)kSplits, 2 * sms / tiles, pages * p.page / kKeys / 16, room / cells});
+  const int64_t splits = std::min({(int64_t)kSplits, 2 * sms / tiles, pages * p.page / kKeys / 4, room / cells});
   p.splits = (int)std::max<int64_t>(1, splits);
   p.split_sums = c.tiles;
   p.split_stats = reinterpret_cast<float2*>(c.tiles + room * DP);
