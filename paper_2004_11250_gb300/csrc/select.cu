@@ -106,7 +106,7 @@ __device__ __forceinline__ void query_codes_of(const SelectParams& p, const T* q
 template <class T, class F>
 __device__ __forceinline__ void query_codes(const SelectParams& p, int t, int h, int lane, F&& store) {
   const T* q = static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)h * p.G * p.q_hs;
-  if (((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(p.q_hs * sizeof(T))) & (sizeof(Vec<T, 8>) - 1) & 15) == 0)
+  if (((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(p.q_hs * sizeof(T))) & (sizeof(Vec<T, 8>) - 1)) == 0)
     query_codes_of<T, true>(p, q, lane, store);
   else
     query_codes_of<T, false>(p, q, lane, store);

@@ -889,3 +889,49 @@ def test_select_sums_near_their_largest(pp, G, D, tokens):
         assert torch.equal(sel.cpu(), ref.select(c.q, codes, scales, c.table, c.starts, [n], True, page, 1, 2, keep))
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("tokens", [None, [30, 10]])
+def test_select_views(pp, dt, tokens):
+    """Queries in a fused product: on 32-byte boundaries, on 16-byte ones, on those of one value, heads first."""
+    page, D, G, H, keep = 8, 64, 2, 2, 6
+    c = Case(pp, dt, G, H, D, page, [300, 200], tokens, seed=5, summaries=True, trash=False)
+    try:
+        codes, scales = ref.summarize(c.k)
+        c.codes.copy_(codes)
+        c.scales.copy_(scales)
+        want = ref.select(c.q, codes, scales, c.table, c.starts, c.lens, True, page, 1, 2, keep)
+        step = 16 // c.q.element_size()
+        base = torch.randn((c.T, (H * G + 2) * D + 2 * step), device="cuda").to(dt)
+        views = [c.qd.transpose(0, 1).contiguous().transpose(0, 1)]
+        for off in (0, step, 1):
+            views.append(base[:, off: off + H * G * D].unflatten(1, (H * G, D)))
+            views[-1].copy_(c.qd)
+            sel = torch.empty((c.T, H, keep), dtype=torch.int32, device="cuda")
+            for q in views[-1:] + views[:1]:
+                pp.pp_cache_select(c.cache, q, c.sd, c.td, c.ld, pp.PP_ATTN_CAUSAL, 1, 2, sel)
+                assert torch.equal(sel.cpu(), want)
+        # heads of an odd distance
+        wide = torch.randn((c.T, H * G, D + step), device="cuda").to(dt)[:, :, :D]
+        wide.copy_(c.qd)
+        pp.pp_cache_select(c.cache, wide, c.sd, c.td, c.ld, pp.PP_ATTN_CAUSAL, 1, 2, sel)
+        assert torch.equal(sel.cpu(), want)
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+def test_rotate_and_attend_at_16_byte_offsets(pp, dt):
+    """Rows that begin 16 bytes, or one value, into a wider boundary: stores, tiles and rows."""
+    step = 16 // torch.empty(0, dtype=dt).element_size()
+    for off in (step, 1):
+        for tokens in (None, [90], [700]):
+            c = Case(pp, dt, 4, 2, 64, 16, [720], tokens, seed=2)
+            try:
+                T, Hq, D = c.q.shape
+                view = torch.zeros((T, Hq * D + 2 * step), device="cuda", dtype=dt)[:, off: off + Hq * D].unflatten(1, (Hq, D))
+                view.copy_(c.qd)
+                c.check(q=view)
+            finally:
+                c.close()
