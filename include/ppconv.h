@@ -472,7 +472,8 @@ void pp_net_destroy(pp_net* net);
  *
  * Data types: PP_F32, PP_F16, PP_BF16; one type for the queries, keys, values,
  * cache and outputs of a call.  Sums, norms and softmax statistics are held in
- * fp32 and each output is rounded once.
+ * fp32 and each output is rounded once; attention in 16 bits also rounds softmax
+ * weights (pp_attn_forward).
  * Token tensors are views [T][heads][D]: element (t, h, d) is at
  * t * token_stride + h * head_stride + d (strides in elements, so q, k and v may
  * be parts of one fused product).  Outputs are dense [T][heads][D].  Pointers
@@ -613,6 +614,9 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  *           order, the ones that the token sees before others (of a token that sees P pages the first
  *           min(keep, P) entries count; those below 0 are skipped); NULL (keep 0): all pages
  * What the cache holds outside the visible keys is never used, NaN and infinities included.
+ * A weight's product with v takes the weight in fp32 (fp32), as two 16-bit halves (16 bits, few rows
+ * per key), or rounded to the type (16 bits, many tokens: 11 bits in f16, 8 in bf16).  f16 weights
+ * below 2^-27 of the row's largest have fewer bits, and those below 2^-38 are 0 there.
  * Asynchronous on stream, no allocation; the same inputs give the same bits.
  * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, flags, scale not finite),
  * PP_ERR_UNSUPPORTED (width * page not below 2^31; or T * Hq * width * page above some 2^40 in

@@ -41,6 +41,7 @@ using namespace ppc_attn;
 constexpr int kRows = 16;      // query rows of a unit at most
 constexpr int kWarps = 4;      // that compute; one more copies
 constexpr int kThreads = kWarps * 32 + 32;
+constexpr int kUp = 15;        // f16 weights are up to 2^15 (a warp's m is never behind its keys)
 constexpr int kGroup = 16;     // parts of a unit joined at once
 constexpr int kMaxCtas = 512;  // kGroup^2 parts and more
 constexpr int kJoin = kMaxCtas / kGroup;
@@ -155,7 +156,7 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
     for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-    x *= sl;
+    x = __fmul_rn(x, sl);  // rounded before the maximum is taken from it, here and below
     const float mx = fmaxf(m, x), ref = mx == -INFINITY ? 0.f : mx, f = ex2(m - ref), e = ex2(x - ref);
     m = mx;
     l = l * f + e;
@@ -498,9 +499,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       }
       float f[NR];
       bool moved = false;
-      // the running maximum of row r after mx, the factor of what came before it, and where exponents are taken from
+      // row r's m after keys of up to mx, the factor of what came before it, and where exponents are taken from
       auto raise = [&](int r, float mx) {
-        mx = fmaxf(m[r], mx);
+        mx = fmaxf(m[r], lower(mx, kLift<T, kUp>));
         const float at = mx == -INFINITY ? 0.f : mx;
         f[r] = ex2(m[r] - at);
         moved = moved || m[r] != mx;
@@ -528,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            sc[rb][e] = (sc[rb][e] + odd[rb][e]) * sl;
+            sc[rb][e] = __fmul_rn(sc[rb][e] + odd[rb][e], sl);
             if (!clean && hidden(warp * KW + g + 8 * (e >> 1), 2 * rb + (e & 1))) sc[rb][e] = -INFINITY;
           }
         // ---- softmax over what this warp has seen
@@ -552,8 +553,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[rb][i][e] *= f[2 * rb + (e & 1)];
         }
-        // ---- their product with V.  The weights as two halves of the inputs' type, so that they keep 16 bits and more (22
-        // in f16): bound by the copies, the kernel has the time, and the output's own rounding stays the largest error
+        // ---- their product with V.  The weights as two halves of the inputs' type, so that they keep 16 bits in bf16 and 22
+        // in f16 (fewer below 2^-14, of up to 2^15, and none below 2^-25): bound by the copies, the kernel has the time, and
+        // the output's own rounding stays the largest error
         uint32_t bh[RB][2], bl[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
@@ -604,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           sc[r] += __shfl_xor_sync(~0u, sc[r], 1);
-          sc[r] = (sc[r] + __shfl_xor_sync(~0u, sc[r], 2)) * sl;
+          sc[r] = __fmul_rn(sc[r] + __shfl_xor_sync(~0u, sc[r], 2), sl);
           if (!clean && hidden(key, r)) sc[r] = -INFINITY;
           float mx = sc[r];
           mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
@@ -746,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       }
       if (p.lse && tid < nrows)
         p.lse[(int64_t)(w.t0 + p.G.div(r0 + tid)) * p.H * p.G.d + h * p.G.d + p.G.mod(r0 + tid)] =
-            rl[tid] == 0.f ? -INFINITY : rm[tid] * 0.693147181f + logf(rl[tid]);
+            rl[tid] == 0.f ? -INFINITY : log_sum<T, kUp>(rm[tid], rl[tid]);
     };
     const int first = w.base + u * w.span;  // the unit's first place
     const int c0 = first / run, parts = (first + w.span - 1) / run - c0 + 1;

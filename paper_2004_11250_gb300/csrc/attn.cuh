@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cmath>
+#include <type_traits>
 
 #include "cache.h"
 #include "tc_ptx.cuh"
@@ -43,6 +44,21 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* m, int
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
       "l"(m), "r"(x), "r"(y), "r"(bar)
       : "memory");
+}
+
+// The weights 2^(s - m) of a row may be rounded to the inputs' type before their product with V.  f16 has its 11 bits down
+// to 2^-14 and nothing below 2^-25, and keys far below a row's largest count by their number: m is taken that many powers
+// of two below the largest, so that the weights fill f16's range from above (its largest number is just below 2^16).
+// Their sum is of the same weights, so m need not be the largest for it.
+template <class T, int UP>
+constexpr float kLift = std::is_same<T, __half>::value ? (float)UP : 0.f;
+// x - n, no less than that: beyond 2^24 fp32 holds no difference of n, and a weight must not pass its bound
+__device__ __forceinline__ float lower(float x, float n) { return __fadd_ru(x, -n); }
+// log of a row's sum `l` of weights taken from m
+template <class T, int UP>
+__device__ __forceinline__ float log_sum(float m, float l) {
+  constexpr float n = kLift<T, UP>;
+  return (m + n) * 0.693147181f + logf(l * (n == 0.f ? 1.f : 1.f / (float)(1 << UP)));
 }
 
 __device__ __forceinline__ float ex2(float x) {

@@ -10,8 +10,12 @@
 // The score product of a block runs while the softmax of the one before it does
 // (two S buffers), and two CTAs share an SM, so one's softmax hides behind the
 // other's products.  m is only raised, and O rescaled in TMEM, when a row's
-// maximum has grown by more than 2^8: the weights then stay below 2^8, and their
-// sums are what they would be, since both are divided in the end.
+// maximum has grown by more than 2^8 (bf16; 2^2 in f16): the weights then stay
+// below 2^8, and their sums are what they would be, since both are divided in the
+// end.  P is rounded to the inputs' type, as the tensor cores want it (a second
+// half would double the products): 11 bits in f16, 8 in bf16, where the plain sums
+// have 24.  f16 weights are taken 2^13 times as large, so that all down to 2^-27
+// of the row's largest have their 11 bits, and those above 2^-38 some.
 //
 // Where pages are selected for each token, the tile reads the union of its tokens'
 // pages once, and a bit per (page, token) says which rows use it: neighbouring
@@ -20,10 +24,11 @@
 // along their blocks, and a second kernel joins the shares.
 //
 // Measured: 2048 tokens, 32 heads of 128 over 8, 32 of 512 pages of 64 each (bf16):
-// 285 us, 940 TFLOP/s of the products over the unions (125 pages per 32 tokens).
+// 291 us, 920 TFLOP/s of the products over the unions (125 pages per 32 tokens);
+// 296 us in f16, whose rows are rescaled more often.
 // Bound by the softmax: two warps per scheduler, some 400 instructions per block
 // each; the tensor pipe is busy 38 % of the time.  3 chunks of 333 tokens, 8 heads
-// of 64, 20 pages of 32 each (f16): 35 us, split in four (71 us whole).
+// of 64, 20 pages of 32 each (f16): 36 us, split in four (71 us whole).
 #include <algorithm>
 #include <type_traits>
 
@@ -42,7 +47,9 @@ constexpr int kStages = 2;             // of K and of V
 constexpr int kInfo = 4;               // blocks that the copying warp may be ahead of the softmax, and one
 constexpr int kMaskWords = 2048;       // token bits of the pages in one window
 constexpr int kSplits = 8;             // shares of a tile's blocks at most
-constexpr float kGrow = 8.f;           // log2 of how far a row's scores may pass its m
+constexpr int kUp = 13;                // f16 weights are up to 2^13 where m is not behind, and 2^2 times that
+template <class T>
+constexpr float kGrow = std::is_same<T, __half>::value ? 2.f : 8.f;  // log2 of how far a row's weights may pass their bound
 
 template <int DP>
 struct TileShape {
@@ -153,7 +160,7 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
       for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-      x *= sl;
+      x = __fmul_rn(x, sl);  // rounded before the maximum is taken from it
       const float mx = fmaxf(m, x), ref = mx == -INFINITY ? 0.f : mx, f = ex2(m - ref), c = ex2(x - ref);
       m = mx;
       l = l * f + c;
@@ -166,7 +173,7 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i)
     if (lane + 32 * i < p.D) out[lane + 32 * i] = from_f32<T>(o[i] * n);
-  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
+  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);  // m is the largest here
 }
 
 // what a wait comes to that does not find its phase complete at once
@@ -544,8 +551,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
 #pragma unroll
             for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
           }
-          const float mx = see ? fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl : -INFINITY;
-          const bool grow = mx > m + kGrow;  // from -infinity, too
+          const float mx = see ? lower(__fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl), kLift<T, kUp>) : -INFINITY;
+          const bool grow = mx > __fadd_rd(m, kGrow<T>);  // from -infinity, too
           if (__any_sync(~0u, grow)) {
             const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
             m = to;
@@ -574,7 +581,10 @@ __global__ void __launch_bounds__(kThreadsT, 2)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             float a, c;
-            unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), sl2, at2), a, c);
+            // scaled as the maximum is and then taken from it, not in one step (a product plus 0, so that the two are not merged):
+            // where scores are so large that fp32 numbers lie further than 1 apart, no weight passes its bound and the largest
+            // does not vanish
+            unpack2(add2(fma2(pack2(x[2 * i], x[2 * i + 1]), sl2, pack2(0.f, 0.f)), at2), a, c);
             a = ex2(a);
             c = ex2(c);
             sum[i & 3] = add2(sum[i & 3], pack2(a, c));
@@ -661,7 +671,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           }
         }
       }
-      if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
+      if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : log_sum<T, kUp>(m, l);
       unsigned again = __ballot_sync(~0u, odd && live_row && (p.sel || p.causal));
       while (again) {
         const int r = warp * 32 + __ffs(again) - 1, tk = p.G.div(r);
@@ -737,7 +747,7 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
       for (int e = 0; e < 4; ++e) out[d + e] = y.v[e];
     }
   }
-  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);
+  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : log_sum<T, kUp>(m, l);
 }
 
 template <class T, int DP>

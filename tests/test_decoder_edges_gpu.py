@@ -1,0 +1,71 @@
+"""The decoder operators on the GPU where they can go wrong: weights far below a row's largest, token ranges that do not
+fit, statistics of NaN, mixed batches, turns at large positions, views at odd places, captured chains."""
+
+import pytest
+import torch
+
+import decoder_ref as ref
+from test_decoder_gpu import BF16, Case, F16, pp  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ f16 weights
+
+
+def sink_case(pp, G, H, D, page, lens, tokens, gap):
+    """Key 3 of each sequence draws almost all weight and holds zeros; the others' logits lie `gap` below (scale 1)."""
+    c = Case(pp, F16, G, H, D, page, lens, tokens, seed=int(gap) + D, trash=False)
+    g = torch.Generator().manual_seed(3)
+    c.k = (0.02 * torch.randn(c.k.shape, generator=g)).to(F16)
+    c.v = (1 + 0.25 * torch.randn(c.v.shape, generator=g)).to(F16)
+    c.q = (0.3 * torch.randn(c.q.shape, generator=g)).to(F16)
+    c.k[..., 0] = 0
+    c.q[..., 0] = gap / 8
+    for b in range(len(lens)):
+        c.k[int(c.table[b, 0]), :, 3, 0] = 8
+        c.v[int(c.table[b, 0]), :, 3] = 0
+    for d, h in ((c.kd, c.k), (c.vd, c.v), (c.qd, c.q)):
+        d.copy_(h)
+    return c
+
+
+@pytest.mark.parametrize("gap", [8.0, 14.0, 16.0, 18.0])
+@pytest.mark.parametrize("G,H,D,lens,tokens", [(2, 4, 64, [4096] * 40, None), (4, 2, 128, [4096] * 70, None),
+                                               (2, 1, 64, [9000], [300]), (8, 8, 64, [1500], [700]), (4, 2, 128, [5000, 900], [200, 900])])
+def test_f16_weights_far_below_the_largest(pp, G, H, D, lens, tokens, gap):
+    """A key that draws almost all weight and holds nothing, the others some 2^-26 of it each: what is left is their sum.
+    To the bound of the reference comes what f16 loses of a weight below its smallest normal number, 2^-25 where the row's
+    largest weight is at least 2^13: 2^-38 of it for every key, of values below 3."""
+    c = sink_case(pp, G, H, D, 64, lens, tokens, gap)
+    try:
+        out, lse = c.attend(1.0)
+        want, wl, tol, tl = ref.attend(c.q, c.k, c.v, c.table, c.starts, lens, 1.0, True)
+        assert float(c.v.abs().max()) < 3
+        assert ref.worst(out, want, tol + 2.0 ** -38 * 3 * max(lens)) <= 1
+        assert ref.worst(lse, wl, tl) <= 1
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("tokens", [None, [400]])
+def test_logits_of_any_size_stay_in_range(pp, dt, tokens):
+    """Logits of 2^20 to 2^32, where neighbouring fp32 numbers are up to 2^8 apart: their own errors leave no digits to
+    compare, but an output stays a mean of values."""
+    for size in (4000.0, 60000.0):
+        c = Case(pp, dt, 4, 2, 64, 64, [700], tokens, seed=31, trash=False)
+        try:
+            g = torch.Generator().manual_seed(6)
+            for w in range(c.table.shape[1] - 1):  # later pages hold larger keys
+                i = int(c.table[0, w])
+                c.k[i] = (torch.randn(c.k[i].shape, generator=g) * (0.05 + 0.02 * w) * size).clamp(-60000, 60000).to(dt)
+            c.q = (torch.randn(c.q.shape, generator=g) * size / 20).clamp(-60000, 60000).to(dt)
+            c.kd.copy_(c.k)
+            c.qd.copy_(c.q)
+            out, lse = c.attend(1.0)
+            assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+            assert float(out.abs().max()) <= float(c.v.abs().max()) * (1 + 2.0 ** -6)
+        finally:
+            c.close()
