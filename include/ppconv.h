@@ -609,7 +609,7 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
 /*
  * Attention of the tokens over their visible keys, s = scale * q.k:
  *   out[t][h] = sum_j softmax_j(s) v_j, and lse[t][h] = log sum_j exp(s_j) if lse is not NULL.
- * A token that sees no key gets 0 and -infinity.
+ * A token that sees no key gets 0 and -infinity, one with a score of NaN NaN for both.
  *   sel     [T][H][keep] as pp_cache_select writes it, only those pages are read: distinct, in any
  *           order, the ones that the token sees before others (of a token that sees P pages the first
  *           min(keep, P) entries count; those below 0 are skipped); NULL (keep 0): all pages

@@ -677,7 +677,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, wm[i][tid]);
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) sum += wm[i][tid] == -INFINITY ? 0.f : wl[i][tid] * ex2(wm[i][tid] - mx);
+      for (int i = 0; i < kWarps; ++i)  // without keys 0 x 0; of scores that are all NaN, NaN
+        sum += wl[i][tid] * (wm[i][tid] == -INFINITY ? 0.f : ex2(wm[i][tid] - mx));
       rm[tid] = mx;
       rl[tid] = sum;
     }
@@ -797,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
           for (int i = 0; i < n; ++i) {
             const float c = wts[tid][i] == -INFINITY ? 0.f : ex2(wts[tid][i] - mx);
             wts[tid][i] = c;
-            sum += c == 0.f ? 0.f : c * sums[tid][i];
+            sum += c * sums[tid][i];  // NaN stays NaN
           }
           rm[tid] = mx;
           rl[tid] = sum;

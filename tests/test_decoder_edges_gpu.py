@@ -1,11 +1,12 @@
 """The decoder operators on the GPU where they can go wrong: weights far below a row's largest, token ranges that do not
 fit, statistics of NaN, mixed batches, turns at large positions, views at odd places, captured chains."""
+import math
 
 import pytest
 import torch
 
 import decoder_ref as ref
-from test_decoder_gpu import BF16, Case, F16, pp  # noqa: F401
+from test_decoder_gpu import BF16, Case, F16, F32, pp  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +70,41 @@ def test_logits_of_any_size_stay_in_range(pp, dt, tokens):
             assert float(out.abs().max()) <= float(c.v.abs().max()) * (1 + 2.0 ** -6)
         finally:
             c.close()
+
+
+# ------------------------------------------------------------------ statistics of NaN
+
+
+@pytest.mark.parametrize("dt,lens,tokens", [(F32, [100, 60], None), (F16, [100, 60], None), (BF16, [3000, 60], None), (F32, [6000, 60], None),
+                                            (BF16, [100, 60], [9, 3]), (BF16, [500, 400], [400, 300])])
+def test_rows_of_nan_have_nan_statistics(pp, dt, lens, tokens):
+    """A query that is NaN has an output and a log-sum of NaN; minus infinity is for rows that see no key."""
+    c = Case(pp, dt, 2, 2, 64, 16, lens, tokens, seed=9)
+    try:
+        n0 = 1 if tokens is None else tokens[0]
+        c.q[:n0, 1, 3] = math.nan
+        c.qd.copy_(c.q)
+        out, lse = c.attend()
+        assert torch.isnan(out[:n0, 1]).all() and torch.isnan(lse[:n0, 1]).all()
+        others = [0, 2, 3]
+        want, wl, tol, tl = ref.attend(c.q, c.k, c.v, c.table, c.starts, lens, 1 / 8.0, True)
+        assert ref.worst(out[:, others], want[:, others], tol[:, others]) <= 1
+        assert ref.worst(lse[:, others], wl[:, others], tl[:, others]) <= 1
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_one_nan_logit_among_far_larger_ones(pp, dt):
+    """A NaN in a part of a long sequence whose weights vanish beside another part's: NaN all the same."""
+    c = Case(pp, dt, 2, 1, 64, 64, [20000], None, seed=9)
+    try:
+        c.q[:] = 1
+        for key, value in ((15000, 30.0), (100, math.nan)):
+            c.k[int(c.table[0, key // 64]), 0, key % 64] = value
+        c.kd.copy_(c.k)
+        c.qd.copy_(c.q)
+        out, lse = c.attend()
+        assert torch.isnan(out).all() and torch.isnan(lse).all()
+    finally:
+        c.close()
