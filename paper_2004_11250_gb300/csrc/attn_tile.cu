@@ -768,14 +768,21 @@ cudaError_t launch(const AttnParams& p, const pp_cache& c, int64_t grid, cudaStr
 
 namespace ppc_attn {
 
+// Tiles of a call at most: each sequence adds at most one that is not full.
+static int64_t most_tiles(const AttnParams& p) { return ((int64_t)p.T / (kRowsT / p.G.d) + std::min(p.T, p.B)) * p.H; }
+
 bool tile_applicable(const AttnParams& p, int dtype, int sms) {
   if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
   // Units of rows (attn.cu) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where pages
   // are selected) at about 1 us per 64 keys and CTA; a tile meets it with 128 in about the same, split 8 times at most.
   // Selected pages: neighbouring tokens' together are some four times one token's.
-  const int64_t tiles = ((int64_t)p.T * p.G.d + kRowsT - 1) / kRowsT * p.H;
+  // How tokens are spread over sequences is not known here.  Where sequences have less than a unit's 16 rows each (then
+  // there can be more than 9 tiles to 8 units), a tile would hold no more rows than a unit and be walked whole by one CTA:
+  // one token each of 32 sequences, of which one has 65536 keys, 32 heads of 128 over 8: 101 us by units, 956 by tiles.
+  // With 4 tokens each of 32 sequences of up to 8192: 171 us by units, 143 by tiles.
+  const int64_t few = 2 * sms / kSplits, tiles = most_tiles(p);
   const int64_t units = p.sel ? (int64_t)p.T * ((p.G.d + 7) / 8) * p.H : ((int64_t)p.T * p.G.d + 15) / 16 * p.H;
-  return std::max<int64_t>(tiles, 2 * sms / kSplits) * (p.sel ? 4 : 1) < units;
+  return p.sel ? std::max(tiles, few) * 4 < units : few < units && tiles * 8 <= units * 9;
 }
 
 cudaError_t tile_prepare() {
@@ -791,9 +798,8 @@ size_t tile_space(int dtype, int D, int sms) {
 }
 
 cudaError_t tile_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t stream) {
-  // each sequence adds at most one tile that is not full; CTAs beyond the last tile leave
   const int TT = kRowsT / p.G.d, DP = p.D <= 64 ? 64 : 128;
-  const int64_t tiles = ((int64_t)p.T / TT + std::min(p.T, p.B)) * p.H;
+  const int64_t tiles = most_tiles(p);  // CTAs beyond the last tile leave
   // Few tiles are split along their blocks, up to two CTAs per SM, while a share can have 4 blocks (a CTA spends the time of
   // about 8 on its queries and masks, but side by side with the others).  3 chunks of 333 tokens, 8 heads of 64: 71 us
   // whole, 35 in four shares; 119 tokens of 2 heads over 1720 keys, with their selection: 50 us whole, 31 in shares.

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import decoder_ref as ref
-from test_decoder_gpu import BF16, Case, F16, F32, pp  # noqa: F401
+from test_decoder_gpu import BF16, Case, F16, F32, pp, tile_kernel_runs  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -70,6 +70,48 @@ def test_logits_of_any_size_stay_in_range(pp, dt, tokens):
             assert float(out.abs().max()) <= float(c.v.abs().max()) * (1 + 2.0 ** -6)
         finally:
             c.close()
+
+
+# ------------------------------------------------------------------ which kernel runs
+
+
+@pytest.mark.parametrize("selected", [False, True])
+def test_single_tokens_in_ranges_take_the_row_kernel(pp, tmp_path, selected):
+    """One token each of many sequences, given as ranges: tiles would hold a token's rows each.  The same bits as without
+    ranges."""
+    g = torch.Generator().manual_seed(1)
+    lens = torch.randint(0, 300, (64,), generator=g).tolist()
+    lens[5], lens[40] = 4000, 1
+    c = Case(pp, F16, 4, 8, 64, 16, lens, [1] * 64, seed=3)
+    try:
+        sel = None
+        if selected:
+            sel = torch.full((c.T, 8, 6), -1, dtype=torch.int32)
+            for t, n in enumerate(lens):
+                some = torch.randperm(-(-n // 16), generator=g)[:6]
+                sel[t, :, : len(some)] = some.to(torch.int32)
+        assert not tile_kernel_runs(c, tmp_path, None if sel is None else sel.cuda())
+        out = c.check(sel=sel)
+        c.sd = None
+        again, _ = c.attend(sel=None if sel is None else sel.cuda())
+        assert torch.equal(out, again)
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
+def test_a_chunk_among_single_tokens_takes_tiles(pp, tmp_path):
+    g = torch.Generator().manual_seed(2)
+    lens = torch.randint(1, 300, (24,), generator=g).tolist()
+    tokens = [1] * 24
+    tokens[7], lens[7] = 500, 700
+    c = Case(pp, BF16, 4, 2, 64, 16, lens, tokens, seed=3)
+    try:
+        assert tile_kernel_runs(c, tmp_path)
+        c.check()
+        assert c.status() == 0
+    finally:
+        c.close()
 
 
 # ------------------------------------------------------------------ statistics of NaN
