@@ -129,6 +129,7 @@ __device__ __forceinline__ void load_item(const AttnParams& p, int TK, int R, in
       atomicOr(p.status, PP_CACHE_BAD_LENGTH);
       len = min(max(len, 0), most);
     }
+    if (p.starts && ((i == 0 && w.t0 != 0) || (i == p.B - 1 && w.t0 + w.n != p.T))) atomicOr(p.status, PP_CACHE_BAD_LENGTH);
     if (w.t0 < 0 || w.n < 0 || w.t0 > p.T - w.n) w.n = -1;  // ranges that do not fit: the call does nothing
     w.len = len;
     seen = len;
@@ -390,6 +391,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       }
       x = next;
     }
+    if (p.sel && p.starts && blockIdx.x == 0) check_ranges(p.starts, p.T, p.B, lane, 32, p.status);
     return;
   }
 

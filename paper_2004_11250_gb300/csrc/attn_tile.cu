@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   for (int b = b0; b < b1; ++b) {
     const int s0 = p.starts ? p.starts[b] : b, n = p.starts ? p.starts[b + 1] - s0 : 1;
     bad = bad || s0 < 0 || n < 0 || s0 > p.T - n;
+    if ((b == 0 && s0 != 0) || (b == p.B - 1 && s0 + n != p.T)) atomicOr(p.status, PP_CACHE_BAD_LENGTH);
     mine += (max(n, 0) + TT - 1) / TT;
   }
   int before = mine;

@@ -161,7 +161,7 @@ __device__ __forceinline__ Seen seen_keys(int t, int T, int B, const int* __rest
     const int s0 = starts[b], s1 = starts[b + 1];
     n = s1 - s0;
     i = t - s0;
-    if (i < 0 || i >= n) {  // no sequence has this token
+    if (s0 < 0 || s1 > T || i < 0 || i >= n) {  // no sequence has this token, or one has others that there are not
       atomicOr(status, PP_CACHE_BAD_LENGTH);
       return {b, 0};
     }
@@ -173,6 +173,14 @@ __device__ __forceinline__ Seen seen_keys(int t, int T, int B, const int* __rest
   }
   const int keys = causal ? len - n + i + 1 : len;
   return {b, keys < 0 ? 0 : keys};
+}
+
+// Records token ranges that do not fit, of which a call by tokens meets only those that its tokens fall in: by the threads
+// of one block.
+__device__ __forceinline__ void check_ranges(const int* __restrict__ starts, int T, int B, int tid, int threads, int* status) {
+  bool bad = tid == 0 && (starts[0] != 0 || starts[B] != T);
+  for (int b = tid; b < B; b += threads) bad = bad || starts[b] > starts[b + 1];
+  if (bad) atomicOr(status, PP_CACHE_BAD_LENGTH);
 }
 
 }  // namespace ppc

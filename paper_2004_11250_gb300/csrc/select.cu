@@ -133,7 +133,12 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
   const Seen s = seen_keys(t, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
   const int P = (s.keys + p.page - 1) / p.page;
   int* out = p.sel + ((int64_t)t * p.H + h) * p.keep;
+  // by a warp that waits for the queries' integers
+  auto ranges = [&]() {
+    if (p.starts && blockIdx.x == 0 && h == 0 && warp == kThreads / 32 - 1) check_ranges(p.starts, p.T, p.B, lane, 32, p.status);
+  };
   if (P <= p.keep) {  // the whole cluster
+    ranges();
     if (rank == 0)
       for (int i = tid; i < p.keep; i += kThreads) out[i] = i < P ? i : -1;
     return;
@@ -151,6 +156,8 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectParams p) 
       code[0][p.D + d] = (int8_t)(down & 127);
       code[1][p.D + d] = (int8_t)(down >> 7);
     });
+  ranges();
+  __syncwarp();
   if (ranks > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   __syncthreads();
   // 2 D / 16 lanes a page, in a power of two
@@ -366,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, 3) select_tile_kernel(const SelectPa
     row_b[lane] = s.b;
     row_P[lane] = (s.keys + p.page - 1) / p.page;
   }
+  if (warp == 1 && p.starts && blockIdx.x == 0 && h == 0) check_ranges(p.starts, p.T, p.B, lane, 32, p.status);
   __syncthreads();
   for (int r = warp; r < kTokens; r += kThreads / 32) {
     auto store = [&](int d, int up, int down) {

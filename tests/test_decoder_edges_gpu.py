@@ -114,6 +114,44 @@ def test_a_chunk_among_single_tokens_takes_tiles(pp, tmp_path):
         c.close()
 
 
+# ------------------------------------------------------------------ token ranges that do not fit
+
+
+@pytest.mark.parametrize("call", ["rows", "tiles", "rows_selected", "tiles_selected", "select", "select_single"])
+@pytest.mark.parametrize("kind", ["late", "short", "long", "before", "descending"])
+def test_token_ranges_that_do_not_fit_are_recorded(pp, tmp_path, call, kind):
+    many = call.startswith("tiles")
+    tokens = [150, 60, 90] if many else [1, 1, 2] if call == "select_single" else [6, 4, 5]
+    c = Case(pp, F16, 8, 1, 64, 16, [400, 300, 200], tokens, seed=4, summaries=True, trash=False)
+    try:
+        T, s = c.T, list(c.starts)
+        s[0], s[-1] = {"late": (1, T), "short": (0, T - 1), "long": (0, T + 1), "before": (-1, T), "descending": (0, T)}[kind]
+        if kind == "descending":
+            s[1], s[2] = s[2], s[1]
+        sel = torch.zeros((T, 1, 4), dtype=torch.int32, device="cuda") if "select" in call else None
+        if call.startswith("tiles"):
+            assert tile_kernel_runs(c, tmp_path, sel)
+
+        def run():
+            if call.startswith("select"):
+                pp.pp_cache_select(c.cache, c.qd, c.sd, c.td, c.ld, pp.PP_ATTN_CAUSAL, 1, 2, sel)
+            else:
+                c.attend(sel=sel)
+
+        run()
+        assert c.status() == 0
+        c.sd.copy_(torch.tensor(s))
+        run()
+        assert c.status() & pp.PP_CACHE_BAD_LENGTH
+        if kind in ("late", "short") and not call.startswith("select"):  # ranges that fit are answered all the same
+            out, _ = c.attend(sel=sel)
+            want, _, tol, _ = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.lens, 1 / 8.0, True, None if sel is None else sel.cpu())
+            mid = slice(s[1], s[2])
+            assert ref.worst(out[mid], want[mid], tol[mid]) <= 1
+    finally:
+        c.close()
+
+
 # ------------------------------------------------------------------ statistics of NaN
 
 
