@@ -170,9 +170,11 @@ void pp_cache_destroy(pp_cache* cache) {
 pp_status pp_cache_device_status(const pp_cache* cache, int* device_error) {
   if (!cache || !device_error) return PP_ERR_INVALID_ARG;
   int v = 0;
+  // The word is clear before the call returns: nothing orders a memset on the default stream before the next kernel of
+  // another stream, whose bits it would take away
   if (cudaDeviceSynchronize() != cudaSuccess ||
       cudaMemcpy(&v, cache->status, sizeof(v), cudaMemcpyDeviceToHost) != cudaSuccess ||
-      cudaMemset(cache->status, 0, sizeof(v)) != cudaSuccess)
+      (v && (cudaMemset(cache->status, 0, sizeof(v)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)))
     return PP_ERR_CUDA;
   *device_error = v;
   return PP_OK;

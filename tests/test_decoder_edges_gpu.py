@@ -72,6 +72,25 @@ def test_logits_of_any_size_stay_in_range(pp, dt, tokens):
             c.close()
 
 
+# ------------------------------------------------------------------ the device status word
+
+
+def test_status_reads_lose_no_bit(pp):
+    """What a side stream meets right after the word was read and cleared is there at the next reading."""
+    k = torch.zeros((2, 1, 16, 64), device="cuda")
+    cache = pp.pp_cache_create(k, k.clone(), torch.zeros((2, 1, 2, 64), device="cuda", dtype=torch.int8), torch.zeros((2, 1), device="cuda"))
+    try:
+        bad = torch.tensor([7], device="cuda", dtype=torch.int32)
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for _ in range(3000):
+            pp.pp_cache_summarize(cache, bad, s)
+            assert pp.pp_cache_device_status(cache) == pp.PP_CACHE_BAD_PAGE
+        assert pp.pp_cache_device_status(cache) == 0
+    finally:
+        pp.pp_cache_destroy(cache)
+
+
 # ------------------------------------------------------------------ which kernel runs
 
 
