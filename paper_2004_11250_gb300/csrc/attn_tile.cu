@@ -46,6 +46,7 @@ constexpr int kKeys = 64;              // keys per block
 constexpr int kStages = 2;             // of K and of V
 constexpr int kInfo = 4;               // blocks that the copying warp may be ahead of the softmax, and one
 constexpr int kMaskWords = 2048;       // token bits of the pages in one window
+constexpr int kAhead = 8;              // entries of the tokens' lists in flight per thread
 constexpr int kSplits = 8;             // shares of a tile's blocks at most
 constexpr int kUp = 13;                // f16 weights are up to 2^13 where m is not behind, and 2^2 times that
 template <class T>
@@ -357,7 +358,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       for (int i = tid; i < wn * words; i += kThreadsT) masks[i] = 0;
       __syncthreads();
       const int* lists = p.sel + ((int64_t)t0 * p.H + h) * p.keep;
-      constexpr int U = 8;  // entries in flight per thread
+      constexpr int U = kAhead;
       for (int i0 = tid; i0 < nt * p.keep; i0 += U * kThreadsT) {
         int tk[U], w[U];
 #pragma unroll
@@ -774,6 +775,8 @@ static int64_t most_tiles(const AttnParams& p) { return ((int64_t)p.T / (kRowsT 
 
 bool tile_applicable(const AttnParams& p, int dtype, int sms) {
   if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
+  // a tile's list entries are counted in 32 bits
+  if (p.sel && (int64_t)(kRowsT / p.G.d) * p.keep > INT32_MAX - 2 * kAhead * kThreadsT) return false;
   // Units of rows (attn.cu) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where pages
   // are selected) at about 1 us per 64 keys and CTA; a tile meets it with 128 in about the same, split 8 times at most.
   // Selected pages: neighbouring tokens' together are some four times one token's.

@@ -133,6 +133,22 @@ def test_a_chunk_among_single_tokens_takes_tiles(pp, tmp_path):
         c.close()
 
 
+def test_long_lists_of_pages_take_the_row_kernel(pp, tmp_path):
+    """Lists so long that a tile's entries pass 2^31: only the first ones count, one for each page that a token sees."""
+    keep = 2 ** 24
+    c = Case(pp, BF16, 1, 1, 64, 16, [200], [160], seed=3)
+    try:
+        sel = torch.full((c.T, 1, keep), -1, dtype=torch.int32, device="cuda")
+        sel[:, 0, :3] = torch.tensor([1, 0, 2], dtype=torch.int32)
+        assert not tile_kernel_runs(c, tmp_path, sel)
+        out, _ = c.attend(sel=sel)
+        want, _, tol, _ = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.lens, 1 / 8.0, True, sel[:, :, :3].cpu())
+        assert ref.worst(out, want, tol) <= 1
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
 # ------------------------------------------------------------------ token ranges that do not fit
 
 
