@@ -619,7 +619,7 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  * below 2^-27 of the row's largest have fewer bits, and those below 2^-38 are 0 there.
  * Asynchronous on stream, no allocation; the same inputs give the same bits.
  * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, flags, scale not finite),
- * PP_ERR_UNSUPPORTED (width * page not below 2^31; or T * Hq * width * page above some 2^40 in
+ * PP_ERR_UNSUPPORTED (width * page above 2^31 - 257; or T * Hq * width * page above some 2^40 in
  * fp32 or with D > 128), PP_ERR_CUDA.
  */
 pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,

@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     sums_of(ctas);
 #pragma unroll
     for (int j = 3; j >= 0; --j)
-      if (ctas[j] <= grid) whole = longer[j];
+      if (ctas[j] <= grid && (int64_t)longer[j] * grid <= INT32_MAX) whole = longer[j];  // places are counted in 32 bits
     if (whole) run = whole;
   }
   // a scan places the items in the one order
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
   }
   before -= mine;
   if ((int64_t)blockIdx.x * run >= total) return;
-  const int x0 = blockIdx.x * run, x1 = min(total, x0 + run);
+  const int x0 = blockIdx.x * run, x1 = x0 + min(total - x0, run);
   const bool has = x0 >= before && x0 < before + mine;
   if (has) {
     for (int i = i0;; ++i) {
@@ -932,7 +932,7 @@ extern "C" pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q
                 (reinterpret_cast<uintptr_t>(out) & al) || (reinterpret_cast<uintptr_t>(lse) & 3)))
     return PP_ERR_INVALID_ARG;
   if (T == 0) return PP_OK;
-  if ((int64_t)width * cache->page > INT32_MAX) return PP_ERR_UNSUPPORTED;
+  if ((int64_t)width * cache->page > INT32_MAX - 256) return PP_ERR_UNSUPPORTED;  // the end of a tile is counted in 32 bits, too
   const int sms = device_sms();
   if (sms <= 0) return PP_ERR_CUDA;
   const pp_cache& c = *cache;

@@ -149,6 +149,19 @@ def test_long_lists_of_pages_take_the_row_kernel(pp, tmp_path):
         c.close()
 
 
+def test_tables_near_2_31_keys_are_refused(pp):
+    k = torch.zeros((1, 1, 8, 64), device="cuda", dtype=F16)
+    cache = pp.pp_cache_create(k, k.clone())
+    try:
+        x, n = torch.zeros((1, 1, 64), device="cuda", dtype=F16), torch.zeros(2, dtype=torch.int32, device="cuda")
+        # refused before anything of the table is read
+        got = pp.lib.pp_attn_forward(cache, 1, x.data_ptr(), 64, 64, 1, 1, None, n.data_ptr(), (2 ** 31 - 8) // 8, n.data_ptr(), 1.0, 0,
+                                     None, 0, x.data_ptr(), None, None)
+        assert got == pp.PP_ERR_UNSUPPORTED
+    finally:
+        pp.pp_cache_destroy(cache)
+
+
 # ------------------------------------------------------------------ token ranges that do not fit
 
 
