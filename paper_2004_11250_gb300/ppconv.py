@@ -476,19 +476,19 @@ def _heads(t, dtype, T, D):
         return None, 0, 0, 0
     try:
         (t0, h, d), (ts, hs, ds) = t.shape, t.stride()
-        if t0 == T and d == D and ds == 1 and t.dtype is dtype:
+        if t0 == T and d == D and ds == 1 and t.dtype is dtype and t.is_cuda:
             return t.data_ptr(), ts, hs, h
     except ValueError:  # not three axes
         pass
-    raise PPError(PP_ERR_INVALID_ARG, "a token tensor is [T][heads][D] of the call's type, dense in D")
+    raise PPError(PP_ERR_INVALID_ARG, "a token tensor is [T][heads][D] of the call's type on the GPU, dense in D")
 
 
 def _dense(t, shape, dtype, where):
-    """Pointer of a dense tensor of this shape and torch type; None stays NULL."""
+    """Pointer of a dense tensor of this shape and torch type on the GPU; None stays NULL."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise PPError(PP_ERR_INVALID_ARG, f"{where}: expected a dense {dtype} of {tuple(shape)}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise PPError(PP_ERR_INVALID_ARG, f"{where}: expected a dense {dtype} of {tuple(shape)} on the GPU")
     return t.data_ptr()
 
 
@@ -569,8 +569,8 @@ def pp_qkv_store(rope, cache, pos, slots, eps, q, qw, q_out, k, kw, v, stream=No
     T = shape[0]
     kt, kh, kd = k.stride()
     vt, vh, vd = v.stride()
-    if not (shape == v.shape == (T, H, D) and k.dtype is dt and v.dtype is dt and kd == 1 and vd == 1):
-        raise PPError(PP_ERR_INVALID_ARG, "pp_qkv_store: k and v are [T][the cache's heads][D] of its type, dense in D")
+    if not (shape == v.shape == (T, H, D) and k.dtype is dt and v.dtype is dt and kd == 1 and vd == 1 and k.is_cuda and v.is_cuda):
+        raise PPError(PP_ERR_INVALID_ARG, "pp_qkv_store: k and v are [T][the cache's heads][D] of its type on the GPU, dense in D")
     qp, qt, qh, Hq = _heads(q, dt, T, D)
     _check(lib.pp_qkv_store(rope, cache, T, _dense(pos, (rope.axes, T), y.i32, "pos"), _dense(slots, (T,), y.i32, "slots"),
                             eps, qp, qt, qh, Hq, _dense(qw, (D,), y.f32, "qw"),
