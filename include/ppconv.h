@@ -498,8 +498,9 @@ typedef struct pp_rope pp_rope;
  *   freq   [pairs] host doubles, finite
  *   axes   number of position axes, 1..8
  *   stream copies are enqueued on it; the call waits for them before returning
- * The angle is taken modulo a turn in 64-bit fixed point, so it is as exact at
- * position 2^31 - 1 as at 0.
+ * The angle is taken modulo a turn in fixed point, 2^-64 turn per position (freq
+ * below 2^40), so at any position it errs by less than 2^-31 turn before it is
+ * rounded to fp32.
  * Errors: PP_ERR_INVALID_ARG (null pointer, axes, axis or freq out of range,
  * pairs < 0 or 2 * pairs > D), PP_ERR_UNSUPPORTED (D odd or not in 2..256),
  * PP_ERR_CUDA, PP_ERR_OOM.

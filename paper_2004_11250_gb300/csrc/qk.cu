@@ -4,7 +4,7 @@
 // y = x w / sqrt(mean x^2 + eps) over the D values of a head, then for each pair
 // (a, b) -> (a cos - b sin, b cos + a sin).  The angle is position * frequency
 // modulo a turn: the frequency in turns is a 64-bit fraction, so the wrapping
-// product keeps the exact fraction of a turn whatever the position, and sincospi
+// product is the fraction of a turn to 2^-33 whatever the position, and sincospi
 // gets a number in [-1, 1).
 //
 // Bound by device memory (each value read and written once).  A lane holds V pairs
@@ -310,6 +310,21 @@ cudaError_t by_order(const QkParams& p, bool inter, bool wide, cudaStream_t stre
   return inter ? by_group<T, true>(p, wide, stream, sms) : by_group<T, false>(p, wide, stream, sms);
 }
 
+// A frequency in radians per position as a 64-bit fraction of a turn, to its last bit while it is below 2^40: 1 / 2 pi is the
+// sum of two doubles here, and the product with the first is taken with its rounding error.  (One double would leave 2^-53
+// of the frequency, which 2^31 positions make 2^-22 of it.)
+uint64_t turn_of(double freq) {
+  constexpr double hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;
+  const double f = std::fabs(freq), p = f * hi;
+  double whole;
+  const uint64_t first = (uint64_t)std::ldexp(std::modf(p, &whole), 64);
+  double rest = std::fma(f, hi, -p) + f * lo;
+  rest -= std::rint(rest);
+  const uint64_t second = (uint64_t)std::rint(std::ldexp(std::fabs(rest), 64));
+  const uint64_t turn = rest < 0 ? first - second : first + second;
+  return freq < 0 ? 0 - turn : turn;
+}
+
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 pp_status run(const pp_rope* rope, int dtype, QkParams& p, void* stream) {
@@ -359,11 +374,7 @@ pp_status pp_rope_create(int D, int pairs, const uint8_t* axis, const double* fr
   unsigned char host[128 * 9] = {};  // turns, then axes
   for (int j = 0; j < pairs; ++j) {
     if ((axis && axis[j] >= axes) || !std::isfinite(freq[j])) return PP_ERR_INVALID_ARG;
-    double f = std::fmod(freq[j] / 6.283185307179586476925, 1.0);
-    if (f < 0) f += 1.0;
-    if (f >= 1.0) f = 0.0;  // a negative number too small to move 1
-    const double hi = std::floor(std::ldexp(f, 32));  // two steps: 2^64 itself does not fit
-    const uint64_t turn = ((uint64_t)hi << 32) | (uint64_t)std::floor(std::ldexp(std::ldexp(f, 32) - hi, 32));
+    const uint64_t turn = turn_of(freq[j]);
     reinterpret_cast<uint64_t*>(host)[j] = turn;
     host[128 * 8 + j] = axis ? axis[j] : 0;
   }

@@ -1,6 +1,7 @@
 """The decoder operators on the GPU where they can go wrong: weights far below a row's largest, token ranges that do not
 fit, statistics of NaN, mixed batches, turns at large positions, views at odd places, captured chains."""
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -236,3 +237,36 @@ def test_one_nan_logit_among_far_larger_ones(pp, dt):
         assert torch.isnan(out).all() and torch.isnan(lse).all()
     finally:
         c.close()
+
+
+# ------------------------------------------------------------------ turns
+
+
+# pi to 60 places
+PI = Fraction(314159265358979323846264338327950288419716939937510582097494, 10 ** 59)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_turns_at_any_position_and_frequency(pp, inter):
+    """Frequencies that are no simple part of a turn, up to thousands of radians per position: the angle in exact
+    arithmetic.  The turn's fraction is kept to 2^-64 per position and read to 2^-32, then rounded to fp32: 2^-25 of half a
+    turn.  With both values of a pair 1 the sum of a cosine and a sine errs by at most 2 (2^-25 pi + 2^-30 + 2^-23) + 2^-23."""
+    D, freq = 32, [1000.0, 1.0, 0.7300000001, 12345.678, 1e-3, 3.0e-7, 2 * math.pi, 0.1, -0.1, -777.7, 1e6 / 3, 5e9 / 7, 0.0, 1e-12, 31.4, 2.0]
+    at = [0, 1, 12345, 999_999_937, 2 ** 31 - 1, -(2 ** 31), -7, 2 ** 30 + 1]
+    rope = pp.pp_rope_create(D, None, freq, 1, inter)
+    try:
+        x = torch.ones((len(at), 1, D), device="cuda")
+        out = torch.empty_like(x)
+        pp.pp_qk_rotate(rope, torch.tensor([at], dtype=torch.int32, device="cuda"), -1.0, x, None, out, None, None, None)
+        got = out.double().cpu()[:, 0]
+        tol = 2 * (2.0 ** -25 * math.pi + 2.0 ** -30 + 2.0 ** -23) + 2.0 ** -23
+        for t, p in enumerate(at):
+            for j, f in enumerate(freq):
+                turn = Fraction(p) * Fraction(f) / (2 * PI)
+                a = float(turn - round(turn)) * 2 * math.pi
+                lo, hi = (2 * j, 2 * j + 1) if inter else (j, D // 2 + j)
+                assert abs(float(got[t, lo]) - (math.cos(a) - math.sin(a))) <= tol, (p, f)
+                assert abs(float(got[t, hi]) - (math.cos(a) + math.sin(a))) <= tol, (p, f)
+    finally:
+        torch.cuda.synchronize()
+        pp.pp_rope_destroy(rope)
