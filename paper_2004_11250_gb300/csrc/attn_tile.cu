@@ -675,6 +675,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       }
       if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : log_sum<T, kUp>(m, l);
       unsigned again = __ballot_sync(~0u, odd && live_row && (p.sel || p.causal));
+      __syncwarp();  // what the rows' own threads wrote lies before what the warp writes over it
       while (again) {
         const int r = warp * 32 + __ffs(again) - 1, tk = p.G.div(r);
         again &= again - 1;

@@ -239,6 +239,32 @@ def test_one_nan_logit_among_far_larger_ones(pp, dt):
         c.close()
 
 
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("lens,tokens", [([2500], [2400]), ([3000], [150])])
+def test_rows_computed_again_are_the_same_each_time(pp, dt, lens, tokens):
+    """Most rows of each tile meet a NaN that they do not see and are computed again, by the warp over what their own threads
+    wrote: the reference's values, and the same bits twenty times over (one share per tile, and several)."""
+    c = Case(pp, dt, 4, 2, 64, 16, lens, tokens, seed=12)
+    try:
+        for key in range(lens[0] - tokens[0] + 40, lens[0], 64):
+            c.v[int(c.table[0, key // 16]), :, key % 16, 5] = math.nan
+        c.vd.copy_(c.v)
+        first, l1 = c.attend()
+        for _ in range(20):
+            again, l2 = c.attend()
+            assert torch.equal(torch.nan_to_num(first, nan=99.0), torch.nan_to_num(again, nan=99.0)) and torch.equal(l1, l2)
+        some = slice(0, 120)
+        c.starts, n = [0, 120], lens[0] - tokens[0] + 120
+        want, wl, tol, tl = ref.attend(c.q[some], c.k, c.v, c.table, c.starts, [n], 1 / 8.0, True)
+        fine = torch.isfinite(want)
+        got = first[some].double().cpu()
+        assert torch.equal(torch.isfinite(got), fine)
+        assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
+        assert ref.worst(l1[some], wl, tl) <= 1
+    finally:
+        c.close()
+
+
 # ------------------------------------------------------------------ turns
 
 
