@@ -118,7 +118,7 @@ class FrameReader:
             at = max(self.frames, self.rows, self.cols) + i  # beyond every position of the frames
             x = self.step(x, torch.full((3, 1), at, device="cuda", dtype=torch.int32))
             got.append(x)
-        return torch.cat(got)
+        return torch.cat(got) if got else x[:0]
 
     def status(self) -> int:
         """What the calls on the layers' caches met (PP_CACHE_* bits; synchronous)."""
@@ -145,6 +145,8 @@ def main(argv=None):
     a.add_argument("--tokens", type=int, default=16)
     a.add_argument("--keep", type=int, default=16, help="pages that a token reads at most; 0: all")
     o = a.parse_args(argv)
+    if o.frames < 1 or o.tokens < 0 or not (o.keep == 0 or o.keep >= 3):
+        a.error("at least 1 frame, 0 tokens, and 3 pages (the first and the last two)")
     r = FrameReader(max_tokens=196 * o.frames + o.tokens, keep=o.keep or None)  # maps of 14 x 14
     gen = torch.Generator(device="cuda")
     gen.manual_seed(1)
@@ -158,8 +160,9 @@ def main(argv=None):
         y = r.answer(o.tokens)
         ev[2].record()
         torch.cuda.current_stream().synchronize()
-    print(f"{r.frames} frames, {r.seen} tokens in the cache: {ev[0].elapsed_time(ev[1]) / max(1, o.frames - 1):.3f} ms a frame, "
-          f"{ev[1].elapsed_time(ev[2]) / o.tokens:.3f} ms an answer token, mean |output| {float(y.float().abs().mean()):.4f}, "
+    answer = "" if not o.tokens else (f", {ev[1].elapsed_time(ev[2]) / o.tokens:.3f} ms an answer token, "
+                                      f"mean |output| {float(y.float().abs().mean()):.4f}")
+    print(f"{r.frames} frames, {r.seen} tokens in the cache: {ev[0].elapsed_time(ev[1]) / max(1, o.frames - 1):.3f} ms a frame{answer}, "
           f"status {r.status()}")
     r.close()
 
