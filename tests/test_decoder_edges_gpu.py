@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import decoder_ref as ref
-from test_decoder_gpu import BF16, Case, F16, F32, pp, tile_kernel_runs  # noqa: F401
+from test_decoder_gpu import BF16, Case, F16, F32, freqs, pp, tile_kernel_runs  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -295,4 +295,146 @@ def test_turns_at_any_position_and_frequency(pp, inter):
                 assert abs(float(got[t, hi]) - (math.cos(a) + math.sin(a))) <= tol, (p, f)
     finally:
         torch.cuda.synchronize()
+        pp.pp_rope_destroy(rope)
+
+
+# ------------------------------------------------------------------ views, fp32 sums, captured chains
+
+
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotations_and_stores_at_16_byte_offsets(pp, dt, inter):
+    """Rows that begin 16 bytes, or one value, into a wider boundary, from a fused product: outputs and the cache."""
+    T, Hq, H, D, page = 21, 4, 2, 64, 16
+    step = 16 // torch.empty(0, dtype=dt).element_size()
+    g = torch.Generator().manual_seed(8)
+    w = torch.rand(D, generator=g) + 0.5
+    pos = torch.randint(0, 900, (1, T), generator=g, dtype=torch.int32)
+    slots = torch.randperm(3 * page, generator=g)[:T].to(torch.int32)
+    rope = pp.pp_rope_create(D, None, freqs(D // 2), 1, inter)
+    try:
+        for off in (step, 2 * step, 1):
+            fused = torch.randn((T, (Hq + 2 * H) * D + 2 * step), generator=g).to(dt)
+            q, k, v = (fused[:, off + a * D: off + (a + n) * D].unflatten(1, (n, D)) for a, n in ((0, Hq), (Hq, H), (Hq + H, H)))
+            fd = fused.cuda()
+            qd, kd, vd = (fd[:, off + a * D: off + (a + n) * D].unflatten(1, (n, D)) for a, n in ((0, Hq), (Hq, H), (Hq + H, H)))
+            want = [ref.rotate(x, w, 1e-6, pos, [0] * (D // 2), freqs(D // 2), inter) for x in (q, k)]
+            # outputs that begin at such places too
+            qo, ko = (torch.zeros(T * n * D + off, device="cuda", dtype=dt)[off:].view(T, n, D) for n in (Hq, H))
+            pp.pp_qk_rotate(rope, pos.cuda(), 1e-6, qd, w.cuda(), qo, kd, w.cuda(), ko)
+            for got, (y, tol) in zip((qo, ko), want):
+                assert ref.worst(got, y, tol) <= 1
+            kp, vp = (torch.zeros((3, H, page, D), device="cuda", dtype=dt) for _ in range(2))
+            cache = pp.pp_cache_create(kp, vp)
+            try:
+                pp.pp_qkv_store(rope, cache, pos.cuda(), slots.cuda(), 1e-6, qd, w.cuda(), qo, kd, w.cuda(), vd)
+                at = slots.long()
+                assert ref.worst(qo, *want[0]) <= 1
+                assert ref.worst(kp.cpu()[at // page, :, at % page], *want[1]) <= 1
+                assert torch.equal(vp.cpu()[at // page, :, at % page], v)
+                rest = torch.ones(3 * page, dtype=torch.bool)
+                rest[at] = False
+                rest = rest.nonzero()[:, 0]
+                assert not kp.cpu()[rest // page, :, rest % page].any() and not vp.cpu()[rest // page, :, rest % page].any()
+                assert pp.pp_cache_device_status(cache) == 0
+            finally:
+                pp.pp_cache_destroy(cache)
+    finally:
+        torch.cuda.synchronize()
+        pp.pp_rope_destroy(rope)
+
+
+@pytest.mark.parametrize("D,G,n", [(64, 1, 500), (96, 2, 700), (128, 4, 300), (256, 8, 200)])
+def test_fp32_sums_are_fp32(pp, D, G, n):
+    """fp32 products and sums throughout: a logit errs by d = (D + 8) 2^-24 scale sum |q k|, a weight by 2 d + 2^-19 (the
+    exponential and its argument, of up to 16), n terms add n 2^-24.  No term for products of fewer bits."""
+    c = Case(pp, F32, G, 1, D, 16, [n], None, seed=D, trash=False)
+    try:
+        out, lse = c.attend()
+        ids = c.table[0, : -(-n // 16)].long()
+        k, v = (x[ids, 0].reshape(-1, D)[:n].double() for x in (c.k, c.v))
+        q = c.q[0].double()
+        s, most = q @ k.T / math.sqrt(D), q.abs() @ k.abs().T / math.sqrt(D)
+        assert float(s.abs().max()) < 16
+        d = most.amax(1, keepdim=True) * (D + 8) * 2.0 ** -24
+        p = torch.softmax(s, 1)
+        tol = (2 * d + 2.0 ** -19 + n * 2.0 ** -24) * (p @ v.abs()) + 2.0 ** -23 * (p @ v).abs()
+        assert ref.worst(out[0], p @ v, tol) <= 1
+        assert ref.worst(lse[0], torch.logsumexp(s, 1), d[:, 0] + 2.0 ** -19 + n * 2.0 ** -24) <= 1
+    finally:
+        c.close()
+
+
+def test_a_captured_chain(pp):
+    """Store, summaries, selection and attention by split tiles as one graph, replayed on other tokens, positions, slots and
+    lengths: the bits of the same calls one by one, and the reference's values."""
+    T, G, H, D, page, W, keep = 260, 4, 2, 64, 16, 60, 12
+    P = D // 2
+    rope = pp.pp_rope_create(D, None, freqs(P))
+    g = torch.Generator().manual_seed(5)
+    pool = [torch.randn((W, H, page, D), generator=g).to(BF16) for _ in range(2)]
+
+    class Side:
+        def __init__(self):
+            self.k, self.v = (x.cuda() for x in pool)
+            self.codes, self.scales = torch.zeros((W, H, 2, D), dtype=torch.int8, device="cuda"), torch.zeros((W, H), device="cuda")
+            self.cache = pp.pp_cache_create(self.k, self.v, self.codes, self.scales)
+            self.fused = torch.zeros((T, (G + 2) * H, D), device="cuda", dtype=BF16)
+            self.pos, self.slots = (torch.zeros((1, T), dtype=torch.int32, device="cuda") for _ in range(2))
+            self.q, self.out = (torch.zeros((T, G * H, D), device="cuda", dtype=BF16) for _ in range(2))
+            self.sel = torch.zeros((T, H, keep), dtype=torch.int32, device="cuda")
+            self.lse = torch.zeros((T, G * H), device="cuda")
+            self.table = torch.zeros((1, W), dtype=torch.int32, device="cuda")
+            self.lens, self.starts = torch.tensor([T], dtype=torch.int32, device="cuda"), torch.tensor([0, T], dtype=torch.int32, device="cuda")
+
+        def run(self, s):
+            f, flags = self.fused, pp.PP_ATTN_CAUSAL
+            pp.pp_qkv_store(rope, self.cache, self.pos, self.slots[0], 1e-6, f[:, : G * H], None, self.q, f[:, G * H: (G + 1) * H], None,
+                            f[:, (G + 1) * H:], s)
+            pp.pp_cache_summarize(self.cache, self.table[0], s)
+            pp.pp_cache_select(self.cache, self.q, self.starts, self.table, self.lens, flags, 1, 2, self.sel, s)
+            pp.pp_attn_forward(self.cache, self.q, self.starts, self.table, self.lens, 0.125, flags, self.sel, self.out, self.lse, s)
+
+        def load(self, x, pos, slots, table, n):
+            self.fused.copy_(x)
+            self.pos[0].copy_(pos)
+            self.slots[0].copy_(slots)
+            self.table[0].copy_(table)
+            self.lens[0] = n
+
+    a, b = Side(), Side()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    try:
+        for side in (a, b):  # before the capture, every kernel once
+            side.load(torch.zeros((T, (G + 2) * H, D)), torch.zeros(T), torch.arange(T), torch.arange(W), T)
+            side.run(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            a.run(s)
+        for n in (W * page, 700, 301):
+            x = torch.randn((T, (G + 2) * H, D), generator=g).to(BF16)
+            pos = torch.randint(0, 5000, (T,), generator=g, dtype=torch.int32)
+            table = torch.randperm(W, generator=g).to(torch.int32)
+            key = torch.arange(n - T, n)
+            slots = table[key // page] * page + (key % page).to(torch.int32)
+            for side in (a, b):
+                side.load(x, pos, slots, table, n)
+            torch.cuda.synchronize()
+            graph.replay()
+            b.run(torch.cuda.current_stream())
+            torch.cuda.synchronize()
+            for i, j in ((a.k, b.k), (a.v, b.v), (a.codes, b.codes), (a.scales, b.scales), (a.sel, b.sel), (a.q, b.q), (a.out, b.out), (a.lse, b.lse)):
+                assert torch.equal(i, j)
+            codes, scales = ref.summarize(a.k.cpu())
+            assert torch.equal(a.codes.cpu(), codes) and torch.equal(a.scales.cpu(), scales)
+            sel = ref.select(a.q.cpu(), codes, scales, table[None], [0, T], [n], True, page, 1, 2, keep)
+            assert torch.equal(a.sel.cpu(), sel)
+            want, wl, tol, tl = ref.attend(a.q.cpu(), a.k.cpu(), a.v.cpu(), table[None], [0, T], [n], 0.125, True, sel)
+            assert ref.worst(a.out, want, tol) <= 1 and ref.worst(a.lse, wl, tl) <= 1
+        assert pp.pp_cache_device_status(a.cache) == 0 and pp.pp_cache_device_status(b.cache) == 0
+    finally:
+        torch.cuda.synchronize()
+        for side in (a, b):
+            pp.pp_cache_destroy(side.cache)
         pp.pp_rope_destroy(rope)
