@@ -96,6 +96,16 @@ __device__ __forceinline__ void mma16<__nv_bfloat16>(float (&c)[4], const uint32
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Two numbers as the type's largest ones that are no larger (of numbers from 0 on).
+template <class T>
+__device__ __forceinline__ uint32_t pack_down(float x, float y) {
+  uint32_t r;
+  if constexpr (std::is_same<T, __half>::value) asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  else asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
+}
+template <class T>
+constexpr float kLeast = std::is_same<T, __half>::value ? 0x1p-24f : 0x1p-126f;  // its smallest number (bf16: normal one)
 // An 8 x 8 matrix of 16-bit values over the warp, two per lane, transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
@@ -555,21 +565,22 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[rb][i][e] *= f[2 * rb + (e & 1)];
         }
-        // ---- their product with V.  The weights as two halves of the inputs' type, so that they keep 16 bits in bf16 and 22
-        // in f16 (fewer below 2^-14, of up to 2^15, and none below 2^-25): bound by the copies, the kernel has the time, and
-        // the output's own rounding stays the largest error
+        // ---- their product with V.  The weights as two halves of the inputs' type, so that they keep 16 bits in bf16 and 21
+        // in f16 (fewer below 2^-14, of up to 2^15, and some 2^-24 at the least): bound by the copies, the kernel has the time,
+        // and the output's own rounding stays the largest error.  The first half is rounded down and the second above 0, so
+        // that neither is 0 or negative beside an infinite value
         uint32_t bh[RB][2], bl[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const float a = sc[rb][2 * i], b = sc[rb][2 * i + 1];
-            const uint32_t hi = pack<T>(a, b);
+            const uint32_t hi = pack_down<T>(a, b);
             Vec<T, 2> two;
             memcpy(&two, &hi, 4);
             const float2 back = get2(two, 0);
             bh[rb][i] = transpose8(hi);  // keys x rows to rows x keys
-            bl[rb][i] = transpose8(pack<T>(a - back.x, b - back.y));
+            bl[rb][i] = transpose8(pack<T>(a > 0.f ? fmaxf(a - back.x, kLeast<T>) : 0.f, b > 0.f ? fmaxf(b - back.y, kLeast<T>) : 0.f));
           }
         const int key = warp * KW + (lane / 16) * 8 + lane % 8;
 #pragma unroll

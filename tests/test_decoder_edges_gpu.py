@@ -242,8 +242,8 @@ def test_one_nan_logit_among_far_larger_ones(pp, dt):
 @pytest.mark.parametrize("dt", [F16, BF16])
 @pytest.mark.parametrize("lens,tokens", [([2500], [2400]), ([3000], [150])])
 def test_rows_computed_again_are_the_same_each_time(pp, dt, lens, tokens):
-    """Most rows of each tile meet a NaN that they do not see and are computed again, by the warp over what their own threads
-    wrote: the reference's values, and the same bits twenty times over (one share per tile, and several)."""
+    """Most rows of each tile meet a NaN that they do not see, or see and get by the warp over what their own threads wrote:
+    the reference's values, and the same bits twenty times over (one share per tile, and several)."""
     c = Case(pp, dt, 4, 2, 64, 16, lens, tokens, seed=12)
     try:
         for key in range(lens[0] - tokens[0] + 40, lens[0], 64):
@@ -261,6 +261,29 @@ def test_rows_computed_again_are_the_same_each_time(pp, dt, lens, tokens):
         assert torch.equal(torch.isfinite(got), fine)
         assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
         assert ref.worst(l1[some], wl, tl) <= 1
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("tokens", [None, [5, 3]])
+def test_infinite_values_stay_infinite(pp, dt, tokens):
+    """A value that is infinite gives outputs that are, of its sign, whatever its key's weight (also the row's largest)."""
+    c = Case(pp, dt, 4, 2, 64, 16, [700, 40], tokens, seed=22)
+    try:
+        for key, d, x in ((3, 1, math.inf), (100, 2, -math.inf), (333, 3, math.inf), (333, 4, -math.inf)):
+            c.v[int(c.table[0, key // 16]), :, key % 16, d] = x
+        # key 333 is the largest of the first head's logits by far, and key 5 far below them
+        c.k[int(c.table[0, 333 // 16]), 0, 333 % 16] = c.q[0, 0] * 2
+        c.k[int(c.table[0, 0]), 0, 5] = -c.q[0, 0]
+        c.v[int(c.table[0, 0]), 0, 5, 6] = math.inf
+        c.kd.copy_(c.k)
+        c.vd.copy_(c.v)
+        out, _ = c.attend()
+        want, _, tol, _ = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.lens, 1 / 8.0, True)
+        got, fine = out.double().cpu(), torch.isfinite(want)
+        assert torch.equal(torch.where(fine, torch.zeros_like(got), got), torch.where(fine, torch.zeros_like(want), want))
+        assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
     finally:
         c.close()
 
