@@ -151,38 +151,6 @@ __device__ __forceinline__ void load_item(const AttnParams& p, int TK, int R, in
   w.places = w.units * w.span;
 }
 
-// One row's attention over keys j0 .. j1 - 1 of a sequence by one warp, one key after the other.
-template <class T, int DP>
-__device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int* row, int h, int j0, int j1, float sl,
-                                      float* acc, float* rm, float* rl) {
-  const int lane = threadIdx.x % 32;
-  float o[DP / 32], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int i = 0; i < DP / 32; ++i) o[i] = 0.f;
-  for (int j = j0; j < j1; ++j) {
-    const int id = row[j >> p.log_page];
-    if (id < 0 || id >= p.pages) continue;
-    const int64_t at = (((int64_t)id * p.H + h) * p.page + (j & (p.page - 1))) * p.D;
-    float x = 0.f;
-    for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-    x = __fmul_rn(x, sl);  // rounded before the maximum is taken from it, here and below
-    const float mx = fmaxf(m, x), ref = mx == -INFINITY ? 0.f : mx, f = ex2(m - ref), e = ex2(x - ref);
-    m = mx;
-    l = l * f + e;
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-      if (lane + 32 * i < p.D) o[i] = o[i] * f + e * to_f32(static_cast<const T*>(p.v)[at + lane + 32 * i]);
-  }
-#pragma unroll
-  for (int i = 0; i < DP / 32; ++i) acc[lane + 32 * i] = o[i];
-  if (lane == 0) {
-    *rm = m;
-    *rl = l;
-  }
-}
-
 template <class T, int DP, int RB>
 __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
     attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
@@ -198,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], rm[kRows], rl[kRows];
   __shared__ float wts[kRows][kJoin + 1], sums[kRows][kJoin + 1];
   __shared__ int scan[4][kThreads / 32], last_flag, dead;
+  __shared__ unsigned unfit;  // keys from lim_min on with values that are not finite, a bit each
   __shared__ Walk found;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int NI = p.sel ? p.T : p.B;
@@ -436,6 +405,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       return q + (w.t0 + p.G.div(r0 + r)) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r0 + r)) * p.q_hs;
     };
     [[maybe_unused]] uint32_t qf[S::E == 2 ? RB : 1][S::E == 2 ? DP / 16 : 1][2];
+    if (tid == 0) unfit = 0;
     if constexpr (S::E == 2) {
       // through the joining buffer, free here, so that each value is read once and 16 bytes at a time where they lie so
       T* stage_q = reinterpret_cast<T*>(acc);
@@ -498,14 +468,20 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       const bool clean = sg.full && (listed || (k + 1) * TK <= lim_min);
       // a key of the tile that row r of the lane's may not use; keys whose values have to be 0, as no row uses them
       auto hidden = [&](int j, int r) { return (j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim[r]); };
-      if (!clean) {  // 0 x the values that no row sees has to be 0
+      if (!clean) {  // 0 x the values that a row does not see has to be 0
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
           const int j = warp * KW + i;
-          if ((j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim_max))
+          unsigned char* v = smem + s * 2 * S::TILE + S::TILE + j * 128;
+          bool zero = (j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && k * TK + j >= lim_max);
+          if (!zero && !listed && k * TK + j >= lim_min) {  // some rows see it
             for (int c = lane; c < S::NCH * 8; c += 32)
-              *reinterpret_cast<uint4*>(smem + s * 2 * S::TILE + S::TILE + c / 8 * TK * 128 + j * 128 + c % 8 * 16) =
-                  make_uint4(0, 0, 0, 0);
+              zero = zero || not_finite<T>(*reinterpret_cast<const uint4*>(v + c / 8 * TK * 128 + c % 8 * 16));
+            zero = __any_sync(~0u, zero);
+            if (zero && lane == 0) atomicOr(&unfit, 1u << (k * TK + j - lim_min));
+          }
+          if (zero)
+            for (int c = lane; c < S::NCH * 8; c += 32) *reinterpret_cast<uint4*>(v + c / 8 * TK * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
         }
         __syncwarp();
       }
@@ -731,16 +707,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, RB>::CTAS)
       }
       group_sync<kWarps * 32>();
     }
-    // a product with 0 of a value that is not finite, at a key that this row does not see and another does: such rows again
-    if (lim_min != lim_max) {
-      bool bad = false;
-      for (int i = tid; i < nrows * p.D; i += kWarps * 32) bad = bad || !isfinite(acc[i / p.D * S::AS + i % p.D]);
-      if (group_any<kWarps * 32>(bad)) {
-        for (int r = warp; r < nrows; r += kWarps)
-          redo_row<T, DP>(p, qrow(r), p.table + (int64_t)w.item * p.width, h, k0 * TK, min(k1 * TK, limit(r)), sl,
-                          acc + r * S::AS, rm + r, rl + r);
-        group_sync<kWarps * 32>();
-      }
+    if (unfit) {
+      for (int r = warp; r < nrows; r += kWarps)
+        add_keys<T, DP>(p, qrow(r), p.table + (int64_t)w.item * p.width, h, lim_min, unfit & ((1u << (limit(r) - lim_min)) - 1), sl, rm[r],
+                        acc + r * S::AS);
+      group_sync<kWarps * 32>();
     }
 
     // ---- out, or joined with the unit's other parts

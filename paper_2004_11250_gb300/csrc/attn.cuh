@@ -66,6 +66,37 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Whether some of 16 bytes of values are not finite.
+template <class T>
+__device__ __forceinline__ bool not_finite(uint4 v) {
+  if constexpr (sizeof(T) == 4) {
+    const float* f = reinterpret_cast<const float*>(&v);
+    return !(isfinite(f[0]) && isfinite(f[1]) && isfinite(f[2]) && isfinite(f[3]));
+  } else {  // an exponent of ones carries into the sign's place
+    constexpr uint32_t e = std::is_same<T, __half>::value ? 0x7C007C00u : 0x7F807F80u, one = e & ~(e << 1) & 0x7FFF7FFFu;
+    return (((v.x & e) + one) | ((v.y & e) + one) | ((v.z & e) + one) | ((v.w & e) + one)) & 0x80008000u;
+  }
+}
+
+// Values that are not finite, at a key that some rows of a unit or tile see and others do not, would reach the others as 0 x
+// NaN.  Such a key's values are zeroed in shared memory, and its weight times them is added to each row that sees it when the
+// row is done: those of the keys first + i with bit i set to sums of a row of queries q and its m, by one warp.
+template <class T, int DP>
+__device__ __noinline__ void add_keys(const AttnParams& p, const T* q, const int* table, int h, int first, uint64_t keys, float sl,
+                                      float m, float* sums) {
+  const int lane = threadIdx.x % 32;
+  for (; keys; keys &= keys - 1) {
+    const int key = first + __ffsll(keys) - 1;
+    const int64_t at = (((int64_t)table[key >> p.log_page] * p.H + h) * p.page + (key & (p.page - 1))) * p.D;
+    float x = 0.f;
+    for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+    const float w = ex2(__fmul_rn(x, sl) - (m == -INFINITY ? 0.f : m));
+    for (int d = lane; d < p.D; d += 32) sums[d] += w * to_f32(static_cast<const T*>(p.v)[at + d]);
+  }
+}
+
 // attn_tile.cu: tiles of 128 query rows on the tensor cores, for 16-bit types and heads of up to 128.
 bool tile_applicable(const AttnParams& p, int dtype, int sms);
 cudaError_t tile_prepare();

@@ -24,11 +24,11 @@
 // along their blocks, and a second kernel joins the shares.
 //
 // Measured: 2048 tokens, 32 heads of 128 over 8, 32 of 512 pages of 64 each (bf16):
-// 291 us, 920 TFLOP/s of the products over the unions (125 pages per 32 tokens);
-// 296 us in f16, whose rows are rescaled more often.
+// 296 us, 905 TFLOP/s of the products over the unions (125 pages per 32 tokens);
+// 303 us in f16, whose rows are rescaled more often.
 // Bound by the softmax: two warps per scheduler, some 400 instructions per block
 // each; the tensor pipe is busy 38 % of the time.  3 chunks of 333 tokens, 8 heads
-// of 64, 20 pages of 32 each (f16): 36 us, split in four (71 us whole).
+// of 64, 20 pages of 32 each (f16): 37 us, split in four (71 us whole).
 #include <algorithm>
 #include <type_traits>
 
@@ -44,6 +44,7 @@ constexpr int kSoft = 128;             // threads of the softmax; then a copying
 constexpr int kThreadsT = kSoft + 64;
 constexpr int kKeys = 64;              // keys per block
 constexpr int kStages = 2;             // of K and of V
+constexpr int kEnds = 3;               // blocks with keys that some tokens of a tile see and others do not, at most: 127 keys
 constexpr int kInfo = 4;               // blocks that the copying warp may be ahead of the softmax, and one
 constexpr int kMaskWords = 2048;       // token bits of the pages in one window
 constexpr int kAhead = 8;              // entries of the tokens' lists in flight per thread
@@ -61,7 +62,8 @@ struct TileShape {
 
 struct Block {          // what the copying warp says of a block
   int have[kPieces];
-  int full;
+  int full;  // every row sees all of it (or may, of selected pages)
+  int end;   // 1 + which of the last blocks, with keys that some tokens see and others do not; 0: none of them
 };
 
 // Shared-memory descriptors of 128-byte swizzled operands.  K-major (Q, K): rows of 128 bytes, groups of 8 rows 1024
@@ -141,40 +143,91 @@ __device__ __forceinline__ void tm_st32(uint32_t a, const uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// One row's attention by one warp, a key after the other: of a row whose product met a value that is not finite at a key
-// that another row of the tile sees and it does not.
-template <class T, int DP>
+// One row's attention over its selected pages, by one warp, 4 keys at a time: of a row whose product met a value that is not
+// finite, on a page of the tile's union that may not be its own.  A lane has 4 of the row's values.
+template <class T>
 __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int* table, const int* list, int h, int keys,
                                       float sl, T* out, float* lse) {
-  const int lane = threadIdx.x % 32, P = (keys + p.page - 1) >> p.log_page;
-  float o[DP / 32], m = -INFINITY, l = 0.f;
+  constexpr int U = 4;
+  const int lane = threadIdx.x % 32, P = (keys + p.page - 1) >> p.log_page, d = lane * 4;
+  const bool in = d < p.D;
+  float qv[4], o[4] = {}, m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i) o[i] = 0.f;
-  for (int e = 0; e < (list ? min(p.keep, P) : P); ++e) {
-    const int w = list ? list[e] : e;
+  for (int i = 0; i < 4; ++i) qv[i] = in ? to_f32(q[d + i]) : 0.f;
+  for (int e = 0; e < min(p.keep, P); ++e) {
+    const int w = list[e];
     if (w < 0 || w >= P) continue;
     const int id = table[w];
     if (id < 0 || id >= p.pages) continue;
-    for (int j = 0; j < min(p.page, keys - w * p.page); ++j) {
-      const int64_t at = (((int64_t)id * p.H + h) * p.page + j) * p.D;
-      float x = 0.f;
-      for (int d = lane; d < p.D; d += 32) x += to_f32(q[d]) * to_f32(static_cast<const T*>(p.k)[at + d]);
+    const int n = min(p.page, keys - w * p.page);
+    for (int j = 0; j < n; j += U) {
+      Vec<T, 4> k[U], v[U];
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-      x = __fmul_rn(x, sl);  // rounded before the maximum is taken from it
-      const float mx = fmaxf(m, x), ref = mx == -INFINITY ? 0.f : mx, f = ex2(m - ref), c = ex2(x - ref);
+      for (int u = 0; u < U; ++u) {  // beyond the last key, the last once more
+        const int64_t at = (((int64_t)id * p.H + h) * p.page + min(j + u, n - 1)) * p.D + (in ? d : 0);
+        k[u] = *reinterpret_cast<const Vec<T, 4>*>(static_cast<const T*>(p.k) + at);
+        v[u] = *reinterpret_cast<const Vec<T, 4>*>(static_cast<const T*>(p.v) + at);
+      }
+      float x[U], mx = m;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        x[u] = 0.f;
+        if (in)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[u] += qv[i] * to_f32(k[u].v[i]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) x[u] += __shfl_xor_sync(~0u, x[u], s);
+        x[u] = j + u < n ? __fmul_rn(x[u], sl) : -INFINITY;  // rounded before the maximum is taken from it
+        mx = fmaxf(mx, x[u]);
+      }
+      const float ref = mx == -INFINITY ? 0.f : mx, f = ex2(m - ref);
       m = mx;
-      l = l * f + c;
+      l *= f;
 #pragma unroll
-      for (int i = 0; i < DP / 32; ++i)
-        if (lane + 32 * i < p.D) o[i] = o[i] * f + c * to_f32(static_cast<const T*>(p.v)[at + lane + 32 * i]);
+      for (int i = 0; i < 4; ++i) o[i] *= f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float c = ex2(x[u] - ref);
+        l += c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += c * to_f32(v[u].v[i]);
+      }
     }
   }
   const float n = l == 0.f ? 0.f : 1.f / l;
+  if (in)
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i)
-    if (lane + 32 * i < p.D) out[lane + 32 * i] = from_f32<T>(o[i] * n);
+    for (int i = 0; i < 4; ++i) out[d + i] = from_f32<T>(o[i] * n);
   if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : m * 0.693147181f + logf(l);  // m is the largest here
+}
+
+// Values of a block that meet a weight of 0 for being out of sight have to be 0: of keys that no row sees, and where `unfit`
+// is not null (some rows see keys that others do not) of those that hold a value that is not finite, which are noted there, a
+// bit each.  Two threads per key, a warp per 16 keys.
+template <class T, int DP>
+__device__ __noinline__ void zero_values(unsigned char* v, const Block& bl, int log_br, uint16_t* unfit) {
+  constexpr int C = DP / 16;  // 16-byte pieces of a thread
+  const int tid = threadIdx.x, key = tid / 2, c0 = tid % 2 * C;
+  const bool there = (key & (1 << log_br) - 1) < bl.have[key >> log_br];
+  auto piece = [&](int i) { return reinterpret_cast<uint4*>(v + (c0 + i) / 8 * kKeys * 128 + key * 128 + (c0 + i) % 8 * 16); };
+  bool odd = false;
+  if (unfit) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) odd |= not_finite<T>(*piece((i ^ key) & C - 1));  // rows lie in the same banks
+    odd = (__shfl_xor_sync(~0u, odd, 1) || odd) && there;
+    unsigned bits = 0;
+    if (const unsigned every = __ballot_sync(~0u, odd))
+      for (int i = 0; i < 16; ++i) bits |= (every >> 2 * i & 1) << i;
+    if (bits && tid % 32 == 0) unfit[tid / 32] = (uint16_t)bits;
+  }
+  if (odd || !there) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) *piece(i) = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
 }
 
 // what a wait comes to that does not find its phase complete at once
@@ -201,6 +254,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   __shared__ int2 found[32];
   __shared__ uint32_t tmem_s;
   __shared__ int scan[kThreadsT / 32], tile_of[4], dead;
+  __shared__ alignas(8) uint16_t unfit[kEnds][4];  // keys of the last blocks with values that are not finite, a bit each, and 16 a word
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
   // ---- which tile: those of a sequence's last tokens, which see the most keys, come first
@@ -264,7 +318,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   }
   // keys that token i of the tile sees
   auto limit = [&](int i) { return p.causal ? min(len, max(0, len - tile_of[2] + tile_of[3] + i + 1)) : len; };
-  const int lim_max = limit(nt - 1), P = (lim_max + p.page - 1) >> p.log_page;
+  const int lim_min = limit(0), lim_max = limit(nt - 1), P = (lim_max + p.page - 1) >> p.log_page;
   const int* table = p.table + (int64_t)b * p.width;
   const int log_br = min(p.log_page, 6), BR = 1 << log_br, log_pc = 6 - log_br, pieces = 1 << log_pc;
   const int log_pp = p.log_page - log_br;  // pieces per page
@@ -276,6 +330,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&tmem_s)), "n"(S::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
+  if (tid < kEnds * 4) unfit[tid / 4][tid % 4] = 0;
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
@@ -348,6 +403,9 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   float m = -INFINITY, l = 0.f;
   const uint32_t row_tm = tmem + ((uint32_t)(warp * 32) << 16);
 
+  // the first block with keys that some tokens see and others do not (of selected pages each may be one)
+  const bool dense = !p.sel;
+  const int ends = dense && lim_min < lim_max ? lim_min >> 6 : INT32_MAX / 2;
   const int words = (TT + 31) / 32, window = p.sel ? kMaskWords / words : INT32_MAX;
   int done = 0;  // blocks before this window
   for (int w0 = 0; w0 < P; w0 = p.sel ? w0 + window : P) {
@@ -447,7 +505,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
             bytes += some > 0 ? BR * DP * 2 : 0;
           }
           if (lane == 0) {
-            info[g % kInfo].full = full;
+            info[g % kInfo].full = full && first + k < ends;
+            info[g % kInfo].end = max(0, first + k - ends + 1);
             mbar_arrive(su32(&info_full[g % kInfo]));
           }
           if (*(volatile int*)&dead) bytes = 0;
@@ -525,7 +584,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
             if (c > 0) see |= ((1ull << c) - 1) << (j << log_br);
           }
         }
-        const bool part = __any_sync(~0u, see != 0 && see != ~0ull), none = __all_sync(~0u, see == 0);
+        // (with all pages, a row that sees nothing of a block is masked, too, whatever the keys hold)
+        const bool part = __any_sync(~0u, live_row && see != ~0ull && (see != 0 || dense)), none = __all_sync(~0u, see == 0);
         hold(&s_full[g & 1], g >> 1 & 1);
         __syncwarp();
         tm_fence_after();
@@ -597,14 +657,10 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           l += a + c;
         }
         tm_st32(tm, w);
-        if (!bl.full) {  // values that no row sees: 0 x them has to be 0
+        if (!bl.full) {
           hold(&v_full[st], g / kStages & 1);
-          for (int i = tid; i < kKeys * (DP / 8); i += kSoft) {
-            const int key = i / (DP / 8), c = i % (DP / 8);
-            if ((key & BR - 1) >= bl.have[key >> log_br])
-              *reinterpret_cast<uint4*>(vbuf + st * S::KV + c / 8 * CHUNK_KV + key * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          zero_values<T, DP>(vbuf + st * S::KV, bl, log_br, bl.end ? unfit[bl.end - 1] : nullptr);
         }
         tm_wait_st();
         // each block's products with V are waited for, and in order, so that a parity names one of two phases; those of the
@@ -620,8 +676,21 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   // ---- out
   if (warp < 4) {
     if (done > 0) hold(&pv_done, (done - 1) & 1);
-    __syncwarp();
+    group_sync<kSoft>();  // what was said of the last blocks' keys
     tm_fence_after();
+    // the keys of end block e that row r's token sees and whose values are still missing
+    auto missing = [&](int e, int limit_of) -> uint64_t {
+      const int c = limit_of - (ends + e) * 64;
+      const uint64_t bits = *reinterpret_cast<const uint64_t*>(unfit[e]);
+      return c >= 64 ? bits : c > 0 ? bits & ((1ull << c) - 1) : 0;
+    };
+    uint64_t some = 0;
+    if (dense)
+#pragma unroll
+      for (int e = 0; e < kEnds; ++e) some |= missing(e, lim);
+    const unsigned lacking = __ballot_sync(~0u, live_row && some != 0);
+    auto cell_of = [&](int r, int tk) { return (int64_t)(t0 + tk) * p.H * p.G.d + h * p.G.d + p.G.mod(r); };
+    auto queries_of = [&](int r, int tk) { return q + (t0 + tk) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs; };
     const int64_t cell = (int64_t)(t0 + p.G.div(live_row ? tid : 0)) * p.H * p.G.d + h * p.G.d + p.G.mod(live_row ? tid : 0);
     if (p.splits > 1) {  // sums as they are, for the joining kernel
       const int64_t at = (int64_t)z * p.T * p.H * p.G.d + cell;
@@ -674,15 +743,28 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         }
       }
       if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : log_sum<T, kUp>(m, l);
-      unsigned again = __ballot_sync(~0u, odd && live_row && (p.sel || p.causal));
+      unsigned again = __ballot_sync(~0u, odd && live_row && p.sel);
       __syncwarp();  // what the rows' own threads wrote lies before what the warp writes over it
-      while (again) {
+      for (; again; again &= again - 1) {
         const int r = warp * 32 + __ffs(again) - 1, tk = p.G.div(r);
-        again &= again - 1;
-        const int64_t at = (int64_t)(t0 + tk) * p.H * p.G.d + h * p.G.d + p.G.mod(r);
-        redo_row<T, DP>(p, q + (t0 + tk) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs, table,
-                        p.sel ? p.sel + ((int64_t)(t0 + tk) * p.H + h) * p.keep : nullptr, h, limit(tk), p.scale * 1.44269504f,
-                        static_cast<T*>(p.out) + at * p.D, p.lse ? p.lse + at : nullptr);
+        redo_row<T>(p, queries_of(r, tk), table, p.sel + ((int64_t)(t0 + tk) * p.H + h) * p.keep, h, limit(tk), p.scale * 1.44269504f,
+                    static_cast<T*>(p.out) + cell_of(r, tk) * p.D, p.lse ? p.lse + cell_of(r, tk) : nullptr);
+      }
+    }
+    __syncwarp();
+    for (unsigned left = lacking; left; left &= left - 1) {
+      const int from = __ffs(left) - 1, r = warp * 32 + from, tk = p.G.div(r);
+      const float mr = __shfl_sync(~0u, m, from), n = 1.f / __shfl_sync(~0u, l, from);
+      const int64_t at = cell_of(r, tk);
+      // into the row's sums for the joining kernel, or beside (where the queries were, whose products are done)
+      float* sums = p.splits > 1 ? p.split_sums + ((int64_t)z * p.T * p.H * p.G.d + at) * DP : reinterpret_cast<float*>(smem) + warp * DP;
+      if (p.splits == 1)
+        for (int d = lane; d < p.D; d += 32) sums[d] = 0.f;
+      for (int e = 0; e < kEnds; ++e)
+        add_keys<T, DP>(p, queries_of(r, tk), table, h, (ends + e) * 64, missing(e, limit(tk)), p.scale * 1.44269504f, mr, sums);
+      if (p.splits == 1) {
+        T* dst = static_cast<T*>(p.out) + at * p.D;
+        for (int d = lane; d < p.D; d += 32) dst[d] = from_f32<T>(to_f32(dst[d]) + sums[d] * n);
       }
     }
     tm_fence_before();
@@ -733,11 +815,11 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
   const int t = (int)(cell / Hq), hq = (int)(cell - (int64_t)t * Hq);
   T* out = static_cast<T*>(p.out) + cell * p.D;
   float* lse = p.lse ? p.lse + cell : nullptr;
-  if (__any_sync(~0u, odd) && (p.sel || p.causal)) {
+  if (p.sel && __any_sync(~0u, odd)) {
     const Seen s = seen_keys(t, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status);
     const int h = p.G.div(hq);
-    redo_row<T, DP>(p, static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)hq * p.q_hs, p.table + (int64_t)s.b * p.width,
-                    p.sel ? p.sel + ((int64_t)t * p.H + h) * p.keep : nullptr, h, s.keys, p.scale * 1.44269504f, out, lse);
+    redo_row<T>(p, static_cast<const T*>(p.q) + t * p.q_ts + (int64_t)hq * p.q_hs, p.table + (int64_t)s.b * p.width,
+                p.sel + ((int64_t)t * p.H + h) * p.keep, h, s.keys, p.scale * 1.44269504f, out, lse);
     return;
   }
   const float n = l == 0.f ? 0.f : 1.f / l;

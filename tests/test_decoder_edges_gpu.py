@@ -288,6 +288,67 @@ def test_infinite_values_stay_infinite(pp, dt, tokens):
         c.close()
 
 
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("G,D,page,lens,tokens", [(2, 64, 16, [300], [100]), (1, 128, 64, [500], [300]), (4, 96, 8, [450, 100], [420, 100]),
+                                                  (8, 64, 128, [4000], [140]), (1, 64, 16, [90, 40], [3, 16]), (3, 256, 32, [120], [80])])
+def test_what_is_not_finite_reaches_the_rows_that_see_it(pp, dt, G, D, page, lens, tokens):
+    """NaN and infinities all over a chunk: single values, a key's whole values, the same value twice with both signs, a key
+    that is NaN near the end.  Each value of each row is finite where the reference's is, and then within its bound."""
+    c = Case(pp, dt, G, 2, D, page, lens, tokens, seed=21)
+    try:
+        def put(pool, key, d, x):
+            pool[int(c.table[0, key // page]), :, key % page, d] = x
+
+        first, n = lens[0] - tokens[0], tokens[0]
+        put(c.v, first + n // 3, 5, math.nan)
+        put(c.v, first + n // 3 + 1, 7, math.inf)
+        put(c.v, first + n // 2, 9, -math.inf)
+        put(c.v, first + n - n // 4, 9, math.inf)
+        put(c.v, first + n - n // 5, slice(8, 16), math.inf)
+        put(c.v, first // 2, 3, -math.inf)  # every row sees this one
+        put(c.k, first + n - 1 - n // 9, 2, math.nan)
+        put(c.v, first + n - 1, slice(None), math.nan)
+        c.kd.copy_(c.k)
+        c.vd.copy_(c.v)
+        out, lse = c.attend()
+        want, wl, tol, tl = ref.attend(c.q, c.k, c.v, c.table, c.starts, lens, 1 / math.sqrt(D), True)
+        got, fine = out.double().cpu(), torch.isfinite(want)
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got == math.inf, want == math.inf)
+        assert ref.worst(torch.where(fine, got, 0.0), torch.where(fine, want, 0.0), tol) <= 1
+        sums = ~torch.isnan(wl)
+        assert torch.equal(~torch.isnan(lse.cpu()), sums)
+        assert ref.worst(torch.where(sums, lse.double().cpu(), 0.0), torch.where(sums, wl, 0.0), tl) <= 1
+        assert c.status() == 0
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dt,T", [(BF16, 512), (F32, 64)])
+@pytest.mark.parametrize("where", ["all rows see it", "half of them do"])
+def test_a_value_that_is_not_finite_costs_little(pp, dt, T, where):
+    """One NaN in a cache of 8192 keys: the call takes no more than ten times as long, and a millisecond (computing the rows
+    again, each alone, took a thousand times as long)."""
+    c = Case(pp, dt, 4, 4, 64, 64, [8192], [T], seed=21, trash=False)
+    try:
+        def best():
+            ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            times = []
+            for _ in range(4):
+                ev[0].record()
+                c.attend(lse=False)
+                ev[1].record()
+                torch.cuda.synchronize()
+                times.append(ev[0].elapsed_time(ev[1]))
+            return min(times)
+
+        before = best()
+        key = 100 if where == "all rows see it" else 8192 - T // 2
+        c.vd[int(c.table[0, key // 64]), :, key % 64, 5] = math.nan
+        assert best() <= 10 * before + 1
+    finally:
+        c.close()
+
+
 # ------------------------------------------------------------------ turns
 
 
