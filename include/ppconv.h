@@ -533,7 +533,7 @@ typedef struct pp_cache pp_cache;
  *   page    tokens per page: 8, 16, 32, 64, 128 or 256
  *   codes   [pages][H][2][D] int8 and scales [pages][H] fp32 device memory of the
  *           page summaries (pp_cache_summarize), or both NULL: no page selection
- * The handle owns a workspace (5 to 25 MB) for attention split over the cache's length, so
+ * The handle owns a workspace (2.5 to 26 MB) for attention split over the cache's length, so
  * its calls must be ordered with each other (one stream, or events); callers that
  * attend on several streams at once make a handle for each over the same memory.
  * Synchronous, allocates: not during stream capture.
@@ -599,6 +599,8 @@ pp_status pp_cache_summarize(const pp_cache* cache, const int32_t* ids, int n, v
  * Up to rounding it bounds the sum over the group of the largest q.k of the page.  The sum is an
  * exact integer and the score one fp32 product, so a selection depends on nothing but its inputs.
  * A NaN score ranks lowest.  Queries that are all 0 or not finite count as 0.
+ * Chunks (4 tokens and more per sequence) are scored 16 tokens at a time where width is at most
+ * 2048, else each token alone: a table no wider than its pages in use is up to 8 times as fast.
  * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, last < 1, first < 0, first + last >
  * keep, a cache without summaries), PP_ERR_UNSUPPORTED (width > 32768, keep > 1024,
  * Q < 1), PP_ERR_CUDA.
@@ -620,8 +622,9 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  * below 2^-27 of the row's largest have fewer bits, and those below 2^-38 are 0 there.
  * Asynchronous on stream, no allocation; the same inputs give the same bits.
  * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, flags, scale not finite),
- * PP_ERR_UNSUPPORTED (width * page above 2^31 - 257; or T * Hq * width * page above some 2^40 in
- * fp32 or with D > 128), PP_ERR_CUDA.
+ * PP_ERR_UNSUPPORTED (width * page above 2^31 - 257; or pieces of work beyond 2^31, which takes a
+ * max(T, B) * Hq * width * page, or min(width, keep) for width, of 2^36 in fp32 and 2^37 in 16 bits
+ * at the least), PP_ERR_CUDA.
  */
 pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
                           const int32_t* starts, const int32_t* table, int width, const int32_t* lens, float scale,
