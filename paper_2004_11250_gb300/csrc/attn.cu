@@ -19,12 +19,12 @@
 // transposed (m16n8k16: keys x rows, then values x rows), so that groups of up to
 // 8 rows fill an instruction.  fp32 takes plain fp32 multiply-adds, for 2, 4 or 8
 // rows: mma.sync in tf32 runs no faster on this GPU, and needs three products and
-// 16 rows (48 us against 21 in the fp32 case below).
+// 16 rows (48 us against 22 in the fp32 case below).
 //
 // Measured, of a copy rate of 6.8 TB/s: 8 sequences of 65536 keys, 32 heads of 128
-// over 8 (f16) 306 us, 7.0 TB/s; 48 of up to 8192 (bf16) 152 us, 5.7 TB/s; 32 tokens
+// over 8 (f16) 308 us, 7.0 TB/s; 48 of up to 8192 (bf16) 151 us, 5.7 TB/s; 32 tokens
 // over 32 selected pages of 64 each (bf16) 45 us, 5.9 TB/s; fp32, 16 of up to 2500, 8
-// heads of 96 over 4: 21 us, 3.4 TB/s.  One sequence of 777 keys: 10.4 us, a chain of
+// heads of 96 over 4: 22 us, 3.2 TB/s.  One sequence of 777 keys: 11 us, a chain of
 // launch, lengths, page table, copy, tile and join.
 #include <algorithm>
 #include <cmath>

@@ -10,12 +10,12 @@
 // The score product of a block runs while the softmax of the one before it does
 // (two S buffers), and two CTAs share an SM, so one's softmax hides behind the
 // other's products.  m is only raised, and O rescaled in TMEM, when a row's
-// maximum has grown by more than 2^8 (bf16; 2^2 in f16): the weights then stay
-// below 2^8, and their sums are what they would be, since both are divided in the
-// end.  P is rounded to the inputs' type, as the tensor cores want it (a second
-// half would double the products): 11 bits in f16, 8 in bf16, where the plain sums
-// have 24.  f16 weights are taken 2^13 times as large, so that all down to 2^-27
-// of the row's largest have their 11 bits, and those above 2^-38 some.
+// maximum has grown by more than 2^8 (2^2 in f16): the weights stay below a bound,
+// and both they and their sums are divided in the end.  P is rounded to the inputs'
+// type, as the tensor cores want it: 11 bits in f16, 8 in bf16, where the sums have
+// 24 (a second half would double the products).  f16 weights are taken 2^13 times as
+// large, so that all down to 2^-27 of the row's largest have their 11 bits, and
+// those above 2^-38 some.
 //
 // Where pages are selected for each token, the tile reads the union of its tokens'
 // pages once, and a bit per (page, token) says which rows use it: neighbouring
@@ -26,8 +26,9 @@
 // Measured: 2048 tokens, 32 heads of 128 over 8, 32 of 512 pages of 64 each (bf16):
 // 296 us, 905 TFLOP/s of the products over the unions (125 pages per 32 tokens);
 // 303 us in f16, whose rows are rescaled more often.
-// Bound by the softmax: two warps per scheduler, some 400 instructions per block
-// each; the tensor pipe is busy 38 % of the time.  3 chunks of 333 tokens, 8 heads
+// Bound by latency in the softmax: 2.7 warps per scheduler wait for their loads from
+// tensor memory, at 1.5 instructions per cycle and SM; the tensor pipe is busy 36 %
+// of the time.  All 32768 keys: 998 us, 1060 TFLOP/s.  3 chunks of 333 tokens, 8 heads
 // of 64, 20 pages of 32 each (f16): 37 us, split in four (71 us whole).
 #include <algorithm>
 #include <type_traits>

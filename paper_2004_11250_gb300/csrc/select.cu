@@ -13,7 +13,8 @@
 // (in 8-bit products, m16n8k32 with the integers as 128 hi + lo: 96 us against 71).
 //
 // Measured, 32 heads over 8, D = 128: one token over 625 pages 7.7 us, 32 tokens over up
-// to 512 pages 12.4 us (chains of latencies), 2048 tokens over 512 pages 71 us.
+// to 512 pages 12.4 us (chains of latencies), 2048 tokens over 512 pages 71 us (132 in a
+// table of 2048, whose scores leave an SM one block; 600 in a wider one, token by token).
 #include <algorithm>
 
 #include "cache.h"
