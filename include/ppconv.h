@@ -545,6 +545,18 @@ pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k,
                           pp_cache** out);
 void pp_cache_destroy(pp_cache* cache);
 
+/*
+ * A paged cache that holds keys and values in 8 bits: k and v are codes [pages][H][page][D] (whole numbers of
+ * -127 .. 127), and code c of a page and head stands for c * scale, with scales [pages][H] fp32 of keys and of
+ * values apart.  Caller-owned device memory, 16-byte aligned, which must outlive the handle.
+ *   dtype   of the queries, keys, values and outputs of its calls
+ * It takes pp_cache_append, pp_cache_read, pp_attn_forward (sel NULL), pp_attn_window, pp_cache_device_status and
+ * pp_cache_destroy; pp_qkv_store is refused (PP_ERR_UNSUPPORTED), and it has no page summaries.
+ * Workspace, order of calls and errors: as pp_cache_create, and PP_ERR_UNSUPPORTED for D not a multiple of 16.
+ */
+pp_status pp_cache8_create(int dtype, int pages, int page, int H, int D, int8_t* k, int8_t* v, float* k_scales,
+                           float* v_scales, pp_cache** out);
+
 /* Synchronous: bits of what the calls on this cache met since the last read (0:
  * nothing); the word is cleared.  A call that sets a bit skips the entry. */
 #define PP_CACHE_BAD_PAGE 1    /* a page id outside 0..pages-1, or a selected index outside the table */
@@ -552,6 +564,7 @@ void pp_cache_destroy(pp_cache* cache);
                                 * (the call's output is then not defined) */
 #define PP_CACHE_BAD_SLOT 4    /* a slot outside -1..pages*page-1 */
 #define PP_CACHE_TIMEOUT 8     /* a bounded wait gave up: the call's output is invalid */
+#define PP_CACHE_NOT_FINITE 16 /* a value that is not finite came to a cache in 8 bits: stored as 0 */
 pp_status pp_cache_device_status(const pp_cache* cache, int* device_error);
 
 /*
@@ -589,6 +602,34 @@ pp_status pp_cache_summarize(const pp_cache* cache, const int32_t* ids, int n, v
 #define PP_ATTN_CAUSAL 1
 
 /*
+ * New tokens of the sequences below into a cache in 8 bits: of the n tokens that k and v [T][H][D] (views, as q is)
+ * hold of sequence b, the i-th is key lens[b] - n + i of it (those below 0 are not stored: an idle slot's).
+ * Per page and head that take new values, of keys and of values alike, with a the largest |x| of the call's new
+ * values there (0 where that is below 2^-100):
+ *   s = a * fl(1 / 127), or the page's scale where that is larger and the page has older tokens;
+ *   its older codes c become rint(c * fl(scale / s)) where s is larger, and scale = s;
+ *   new codes are rint(x * fl(1 / s)), cut to -127 .. 127 (0 where s is 0),
+ * each step one fp32 operation.  A page is begun, and its older scale and codes are forgotten, by the token at its
+ * offset 0: pages need no clearing.  What lies behind a page's new tokens stays as it was.  Values that are not finite
+ * are stored as 0 and recorded.  A page is written by one sequence of a call; a length below 0 or beyond the table
+ * stores nothing.  Keys come rotated (pp_qk_rotate).  Asynchronous on stream, no allocation.
+ * Errors: PP_ERR_INVALID_ARG (null pointer, sizes, strides, alignment), PP_ERR_UNSUPPORTED (a cache that is not in
+ * 8 bits, width * page above 2^31 - 257, T / page + 2 B not below 2^31), PP_ERR_CUDA.
+ */
+pp_status pp_cache_append(const pp_cache* cache, int T, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts,
+                          int64_t v_hs, int B, const int32_t* starts, const int32_t* table, int width, const int32_t* lens,
+                          void* stream);
+
+/*
+ * Keys and values of a cache in 8 bits read back: token i of the n of sequence b is key lens[b] - n + i, as
+ * pp_cache_append counts them (starts that sum up the lengths read everything).  k_out, v_out [T][H][D] dense, of the
+ * cache's dtype, or NULL: code * scale in fp32, rounded once; 0 for keys below 0 or on a page that is not there.
+ * Errors: as pp_cache_append.
+ */
+pp_status pp_cache_read(const pp_cache* cache, int T, int B, const int32_t* starts, const int32_t* table, int width,
+                        const int32_t* lens, void* k_out, void* v_out, void* stream);
+
+/*
  * Pages worth reading, for every token and cache head: sel [T][H][keep], ascending
  * indices into the token's row of the table, -1 after the last.  Of the P pages that
  * hold the token's visible keys, the first `first` and the last `last` are always
@@ -617,6 +658,8 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  *           order, the ones that the token sees before others (of a token that sees P pages the first
  *           min(keep, P) entries count; those below 0 are skipped); NULL (keep 0): all pages
  * What the cache holds outside the visible keys is never used, NaN and infinities included.
+ * A cache in 8 bits has its codes used as they are, exact, with the scales of their pages in fp32; queries count with
+ * all their bits, weights as f16's below.
  * A weight's product with v takes the weight in fp32 (fp32), as two 16-bit halves (16 bits, few rows
  * per key), or rounded to the type (16 bits, many tokens: 11 bits in f16, 8 in bf16).  f16 weights
  * below 2^-27 of the row's largest have fewer bits, and those below 2^-38 are 0 there.
@@ -629,6 +672,17 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
 pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
                           const int32_t* starts, const int32_t* table, int width, const int32_t* lens, float scale,
                           int flags, const int32_t* sel, int keep, void* out, float* lse, void* stream);
+
+/*
+ * pp_attn_forward with a sliding window: of the keys 0 .. n - 1 that a token sees without one, it sees the last
+ * `window` (its own among them) and the first `sinks`.  Over either kind of cache.  Pages between the first keys and
+ * the windows of a call's tokens are not read, and their entries of the table not looked at (they may be -1, and
+ * the pages in use elsewhere); a window that holds all keys gives pp_attn_forward's bits.
+ * Errors: as pp_attn_forward; also window < 1, sinks < 0.
+ */
+pp_status pp_attn_window(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,
+                         const int32_t* starts, const int32_t* table, int width, const int32_t* lens, float scale,
+                         int flags, int window, int sinks, void* out, float* lse, void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,6 +31,9 @@ struct AttnParams {
   int splits;
   float* split_sums;
   float2* split_stats;
+  // with a window (else all keys and 0): a token sees the last `window` keys before its limit, and the first `sinks`
+  int window, sinks;
+  const float *ks, *vs;  // scales [pages][H] of codes
 };
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
@@ -96,6 +99,13 @@ __device__ __noinline__ void add_keys(const AttnParams& p, const T* q, const int
     for (int d = lane; d < p.D; d += 32) sums[d] += w * to_f32(static_cast<const T*>(p.v)[at + d]);
   }
 }
+
+// The row kernel (attn_row.cuh) by what is in the cache, without and with a window; their launch attributes.
+cudaError_t rows_launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream);
+cudaError_t rows_window_launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream);
+cudaError_t rows8_launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream);
+cudaError_t rows_window_prepare();
+cudaError_t rows8_prepare();
 
 // attn_tile.cu: tiles of 128 query rows on the tensor cores, for 16-bit types and heads of up to 128.
 bool tile_applicable(const AttnParams& p, int dtype, int sms);

@@ -1,5 +1,5 @@
 // The paged cache: its handle and page summaries (pp_cache_create,
-// pp_cache_summarize).
+// pp_cache8_create, pp_cache_summarize).
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -88,57 +88,46 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// A pool as [pages * H * page][D]: boxes of 128 bytes by up to a tile of one page's rows, zeros beyond D.
+// A pool as [pages * H * page][D]: boxes of 128 bytes (of 64 where rows of codes are no longer) by up to a tile of one page's
+// rows, zeros beyond D.
 bool pool_map(CUtensorMap* m, const pp_cache& c, void* pool) {
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult q;
   if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
       q != cudaDriverEntryPointSuccess)
     return false;
-  const int e = dtype_size(c.dtype);
+  const bool codes = c.scales8[0] != nullptr;
+  const int e = codes ? 1 : dtype_size(c.dtype), bytes = codes && c.D <= 64 ? 64 : 128;
   const cuuint64_t dims[2] = {(cuuint64_t)c.D, (cuuint64_t)c.pages * c.H * c.page};
   const cuuint64_t strides[1] = {(cuuint64_t)c.D * e};
-  const cuuint32_t box[2] = {(cuuint32_t)(128 / e), (cuuint32_t)std::min(c.page, tile_keys(c.dtype))};
+  const cuuint32_t box[2] = {(cuuint32_t)(bytes / e), (cuuint32_t)std::min(c.page, codes ? kTileKeys8 : tile_keys(c.dtype))};
   const cuuint32_t estr[2] = {1, 1};
-  const CUtensorMapDataType t = c.dtype == PP_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+  const CUtensorMapDataType t = codes               ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                : c.dtype == PP_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                 : c.dtype == PP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                     : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   return reinterpret_cast<EncodeTiledFn>(fn)(m, t, 2, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                             bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
+// Sizes that both kinds of cache refuse.
+bool sizes_ok(int pages, int page, int H, int D) {
+  return page >= 8 && page <= 256 && !(page & (page - 1)) && D % 8 == 0 && D >= 16 && D <= 256 && H <= 65535 &&
+         (int64_t)pages * page < (int64_t)INT32_MAX / H;
+}
+uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 
-extern "C" {
-
-pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k, void* v, int8_t* codes, float* scales,
-                          pp_cache** out) {
-  if (!out || !k || !v || !dtype_ok(dtype) || pages < 1 || H < 1 || D < 1 || page < 1 || !codes != !scales)
-    return PP_ERR_INVALID_ARG;
-  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(codes) |
-       reinterpret_cast<uintptr_t>(scales)) & 15)
-    return PP_ERR_INVALID_ARG;
-  if (page < 8 || page > 256 || (page & (page - 1)) || D % 8 || D < 16 || D > 256 || H > 65535 ||
-      (int64_t)pages * page >= (int64_t)INT32_MAX / H)
-    return PP_ERR_UNSUPPORTED;
-  pp_cache* c = new (std::nothrow) pp_cache;
+// A handle over checked memory: tensor maps, workspace.
+pp_status make_cache(const pp_cache& of, pp_cache** out) {
+  pp_cache* c = new (std::nothrow) pp_cache(of);
   if (!c) return PP_ERR_OOM;
-  c->dtype = dtype;
-  c->pages = pages;
-  c->page = page;
-  c->H = H;
-  c->D = D;
-  c->k = k;
-  c->v = v;
-  c->codes = codes;
-  c->scales = scales;
   const int sms = device_sms();
-  if (sms <= 0 || attn_prepare() != cudaSuccess || select_prepare() != cudaSuccess || !pool_map(&c->mk, *c, k) || !pool_map(&c->mv, *c, v)) {
+  if (sms <= 0 || attn_prepare() != cudaSuccess || select_prepare() != cudaSuccess || !pool_map(&c->mk, *c, c->k) || !pool_map(&c->mv, *c, c->v)) {
     delete c;
     return PP_ERR_CUDA;
   }
-  const AttnSpace space = attn_space(dtype, D, sms);
+  const AttnSpace space = attn_space(c->dtype, c->D, sms);
   const size_t head = 256 + (space.counters + 255) / 256 * 256;
   const size_t partial = (space.partial + 255) / 256 * 256;
   cudaError_t e = cudaMalloc(&c->dmem, head + partial + space.tiles);
@@ -159,6 +148,48 @@ pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k,
   c->tiles = reinterpret_cast<float*>(static_cast<char*>(c->dmem) + head + partial);
   *out = c;
   return PP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+pp_status pp_cache_create(int dtype, int pages, int page, int H, int D, void* k, void* v, int8_t* codes, float* scales,
+                          pp_cache** out) {
+  if (!out || !k || !v || !dtype_ok(dtype) || pages < 1 || H < 1 || D < 1 || page < 1 || !codes != !scales)
+    return PP_ERR_INVALID_ARG;
+  if ((bits(k) | bits(v) | bits(codes) | bits(scales)) & 15) return PP_ERR_INVALID_ARG;
+  if (!sizes_ok(pages, page, H, D)) return PP_ERR_UNSUPPORTED;
+  pp_cache c;
+  c.dtype = dtype;
+  c.pages = pages;
+  c.page = page;
+  c.H = H;
+  c.D = D;
+  c.k = k;
+  c.v = v;
+  c.codes = codes;
+  c.scales = scales;
+  return make_cache(c, out);
+}
+
+pp_status pp_cache8_create(int dtype, int pages, int page, int H, int D, int8_t* k, int8_t* v, float* k_scales,
+                           float* v_scales, pp_cache** out) {
+  if (!out || !k || !v || !k_scales || !v_scales || !dtype_ok(dtype) || pages < 1 || H < 1 || D < 1 || page < 1)
+    return PP_ERR_INVALID_ARG;
+  if ((bits(k) | bits(v) | bits(k_scales) | bits(v_scales)) & 15) return PP_ERR_INVALID_ARG;
+  if (!sizes_ok(pages, page, H, D) || D % 16) return PP_ERR_UNSUPPORTED;
+  pp_cache c;
+  c.dtype = dtype;
+  c.pages = pages;
+  c.page = page;
+  c.H = H;
+  c.D = D;
+  c.k = k;
+  c.v = v;
+  c.scales8[0] = k_scales;
+  c.scales8[1] = v_scales;
+  return make_cache(c, out);
 }
 
 void pp_cache_destroy(pp_cache* cache) {

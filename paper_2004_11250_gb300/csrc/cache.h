@@ -26,6 +26,7 @@ struct pp_cache {
   void* v = nullptr;
   int8_t* codes = nullptr;
   float* scales = nullptr;
+  float* scales8[2] = {nullptr, nullptr};  // of k and v where they are codes in 8 bits
   void* dmem = nullptr;   // status word, counters and partial results
   int* status = nullptr;
   int* counters = nullptr;   // zero between calls
@@ -38,6 +39,7 @@ namespace ppc {
 
 // The row kernel's keys per tile (attn.cu): 64 rows of 16-bit values, 32 of fp32.
 inline int tile_keys(int dtype) { return dtype == PP_F32 ? 32 : 64; }
+constexpr int kTileKeys8 = 64;  // over codes of 8 bits
 // Device bytes that attention needs beside the status word: counters, partial results, shares of tiles.
 struct AttnSpace {
   size_t counters, partial, tiles;

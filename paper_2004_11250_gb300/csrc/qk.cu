@@ -436,6 +436,7 @@ pp_status pp_qkv_store(const pp_rope* rope, const pp_cache* cache, int T, const 
                        int64_t v_hs, void* stream) {
   if (!rope || !cache || T < 0 || Hq < 0 || eps != eps || rope->D != cache->D || (T > 0 && !slots))
     return PP_ERR_INVALID_ARG;
+  if (cache->scales8[0]) return PP_ERR_UNSUPPORTED;
   QkParams p = {};
   p.x[0] = {q, q_ts, q_hs};
   p.x[1] = {k, k_ts, k_hs};

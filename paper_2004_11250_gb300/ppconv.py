@@ -67,6 +67,7 @@ PP_CACHE_BAD_PAGE = 1
 PP_CACHE_BAD_LENGTH = 2
 PP_CACHE_BAD_SLOT = 4
 PP_CACHE_TIMEOUT = 8
+PP_CACHE_NOT_FINITE = 16
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -118,11 +119,15 @@ _SIGS = {
     "pp_rope_destroy": ([_P], None),
     "pp_qk_rotate": ([_P, _I, _I, _P, _F, _P, _I64, _I64, _I, _P, _P, _P, _I64, _I64, _I, _P, _P, _P], _I),
     "pp_cache_create": ([_I, _I, _I, _I, _I, _P, _P, _P, _P, _PP], _I),
+    "pp_cache8_create": ([_I, _I, _I, _I, _I, _P, _P, _P, _P, _PP], _I),
     "pp_cache_destroy": ([_P], None),
     "pp_cache_device_status": ([_P, _P], _I),
     "pp_qkv_store": ([_P, _P, _I, _P, _P, _F, _P, _I64, _I64, _I, _P, _P, _P, _I64, _I64, _P, _P, _I64, _I64, _P], _I),
     "pp_cache_summarize": ([_P, _P, _I, _P], _I),
     "pp_cache_select": ([_P, _I, _P, _I64, _I64, _I, _I, _P, _P, _I, _P, _I, _I, _I, _I, _P, _P], _I),
+    "pp_cache_append": ([_P, _I, _P, _I64, _I64, _P, _I64, _I64, _I, _P, _P, _I, _P, _P], _I),
+    "pp_cache_read": ([_P, _I, _I, _P, _P, _I, _P, _P, _P, _P], _I),
+    "pp_attn_window": ([_P, _I, _P, _I64, _I64, _I, _I, _P, _P, _I, _P, _F, _I, _I, _I, _P, _P, _P], _I),
     "pp_attn_forward": ([_P, _I, _P, _I64, _I64, _I, _I, _P, _P, _I, _P, _F, _I, _P, _I, _P, _P, _P], _I),
 }
 for _name, (_args, _res) in _SIGS.items():
@@ -551,6 +556,21 @@ def pp_cache_create(k, v, codes=None, scales=None) -> Cache:
     return c
 
 
+def pp_cache8_create(k, v, k_scales, v_scales, dtype) -> Cache:
+    """A cache in 8 bits: codes k, v [pages][H][page][D] int8, scales [pages][H] fp32; dtype: torch type of its tokens."""
+    y = _torch_types()
+    if k.dim() != 4 or dtype not in y.code:
+        raise PPError(PP_ERR_INVALID_ARG, "pp_cache8_create shapes and dtype")
+    pages, H, page, D = k.shape
+    out = ctypes.c_void_p()
+    _check(lib.pp_cache8_create(y.code[dtype], pages, page, H, D, _dense(k, k.shape, y.i8, "k"), _dense(v, k.shape, y.i8, "v"),
+                                _dense(k_scales, (pages, H), y.f32, "k_scales"), _dense(v_scales, (pages, H), y.f32, "v_scales"),
+                                ctypes.byref(out)), "pp_cache8_create")
+    c = Cache(out.value)
+    c.dtype, c.shape, c.pools = dtype, (pages, H, page, D), (k, v, k_scales, v_scales)
+    return c
+
+
 def pp_cache_destroy(cache):
     lib.pp_cache_destroy(cache)
 
@@ -610,3 +630,35 @@ def pp_attn_forward(cache, q, starts, table, lens, scale, flags, sel, out, lse=N
                                _dense(sel, (T, cache.shape[1], keep), y.i32, "sel"), keep,
                                _dense(out, q.shape, q.dtype, "out"), _dense(lse, (T, Hq), y.f32, "lse"),
                                _stream(stream)), "pp_attn_forward")
+
+
+def pp_attn_window(cache, q, starts, table, lens, scale, flags, window, sinks, out, lse=None, stream=None):
+    """pp_attn_forward where a token sees its last `window` keys and the first `sinks` ones."""
+    (T, Hq, _), y = q.shape, _torch_types()
+    _check(lib.pp_attn_window(*_sequences(q, cache, starts, table, lens, y), scale, flags, window, sinks,
+                              _dense(out, q.shape, q.dtype, "out"), _dense(lse, (T, Hq), y.f32, "lse"), _stream(stream)),
+           "pp_attn_window")
+
+
+def pp_cache_append(cache, k, v, starts, table, lens, stream=None):
+    """New tokens k, v [T][H][D] of the sequences into a cache in 8 bits: the last ones of lens[b] keys each."""
+    (T, H, D), (B, width), y = k.shape, table.shape, _torch_types()
+    kp, kt, kh, _ = _heads(k, cache.dtype, T, cache.shape[3])
+    vp, vt, vh, Hv = _heads(v, cache.dtype, T, D)
+    if H != cache.shape[1] or Hv != H:
+        raise PPError(PP_ERR_INVALID_ARG, "pp_cache_append: k and v have the cache's heads")
+    _check(lib.pp_cache_append(cache, T, kp, kt, kh, vp, vt, vh, B, _dense(starts, (B + 1,), y.i32, "starts"),
+                               _dense(table, (B, width), y.i32, "table"), width, _dense(lens, (B,), y.i32, "lens"),
+                               _stream(stream)), "pp_cache_append")
+
+
+def pp_cache_read(cache, starts, table, lens, k_out, v_out, stream=None):
+    """The sequences' last keys and values of a cache in 8 bits into k_out, v_out [T][H][D] (either may be None)."""
+    y, (_, H, _, D), (B, width) = _torch_types(), cache.shape, table.shape
+    x = k_out if k_out is not None else v_out
+    if x is None:
+        raise PPError(PP_ERR_INVALID_ARG, "pp_cache_read: nothing to read into")
+    T = x.shape[0]
+    _check(lib.pp_cache_read(cache, T, B, _dense(starts, (B + 1,), y.i32, "starts"), _dense(table, (B, width), y.i32, "table"),
+                             width, _dense(lens, (B,), y.i32, "lens"), _dense(k_out, (T, H, D), cache.dtype, "k_out"),
+                             _dense(v_out, (T, H, D), cache.dtype, "v_out"), _stream(stream)), "pp_cache_read")
