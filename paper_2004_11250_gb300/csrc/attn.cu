@@ -36,9 +36,9 @@ pp_status attend(const pp_cache* cache, int T, const void* q, int64_t q_ts, int6
                   windowed ? window : most, windowed ? std::min(sinks, most) : 0, c.scales8[0], c.scales8[1]};
   const cudaStream_t s = (cudaStream_t)stream;
   const cudaError_t e = eight ? rows8_launch(p, c, sms, s)
-                        : windowed ? rows_window_launch(p, c, sms, s)
                         : tile_applicable(p, c.dtype, sms) ? tile_launch(p, c, sms, s)
-                                                           : rows_launch(p, c, sms, s);
+                        : windowed ? rows_window_launch(p, c, sms, s)
+                                   : rows_launch(p, c, sms, s);
   return e == cudaSuccess ? PP_OK : e == cudaErrorNotSupported ? PP_ERR_UNSUPPORTED : PP_ERR_CUDA;
 }
 

@@ -46,6 +46,7 @@ constexpr int kThreadsT = kSoft + 64;
 constexpr int kKeys = 64;              // keys per block
 constexpr int kStages = 2;             // of K and of V
 constexpr int kEnds = 3;               // blocks with keys that some tokens of a tile see and others do not, at most: 127 keys
+                                       // (with a window as many again, where the tokens' windows begin)
 constexpr int kInfo = 4;               // blocks that the copying warp may be ahead of the softmax, and one
 constexpr int kMaskWords = 2048;       // token bits of the pages in one window
 constexpr int kAhead = 8;              // entries of the tokens' lists in flight per thread
@@ -64,7 +65,8 @@ struct TileShape {
 struct Block {          // what the copying warp says of a block
   int have[kPieces];
   int full;  // every row sees all of it (or may, of selected pages)
-  int end;   // 1 + which of the last blocks, with keys that some tokens see and others do not; 0: none of them
+  int end;   // 1 + which of the last blocks, with keys that some tokens see and others do not (from 1 + kEnds on: of those where
+             // the windows begin); 0: none of them
 };
 
 // Shared-memory descriptors of 128-byte swizzled operands.  K-major (Q, K): rows of 128 bytes, groups of 8 rows 1024
@@ -207,12 +209,12 @@ __device__ __noinline__ void redo_row(const AttnParams& p, const T* q, const int
 
 // Values of a block that meet a weight of 0 for being out of sight have to be 0: of keys that no row sees, and where `unfit`
 // is not null (some rows see keys that others do not) of those that hold a value that is not finite, which are noted there, a
-// bit each.  Two threads per key, a warp per 16 keys.
-template <class T, int DP>
-__device__ __noinline__ void zero_values(unsigned char* v, const Block& bl, int log_br, uint16_t* unfit) {
+// bit each.  Keys from `after` to `before` (of the block) are before every window.  Two threads per key, a warp per 16 keys.
+template <class T, int DP, bool WIN>
+__device__ __noinline__ void zero_values(unsigned char* v, const Block& bl, int log_br, uint16_t* unfit, int after, int before) {
   constexpr int C = DP / 16;  // 16-byte pieces of a thread
   const int tid = threadIdx.x, key = tid / 2, c0 = tid % 2 * C;
-  const bool there = (key & (1 << log_br) - 1) < bl.have[key >> log_br];
+  const bool there = (key & (1 << log_br) - 1) < bl.have[key >> log_br] && (!WIN || key < after || key >= before);
   auto piece = [&](int i) { return reinterpret_cast<uint4*>(v + (c0 + i) / 8 * kKeys * 128 + key * 128 + (c0 + i) % 8 * 16); };
   bool odd = false;
   if (unfit) {
@@ -231,12 +233,15 @@ __device__ __noinline__ void zero_values(unsigned char* v, const Block& bl, int 
   }
 }
 
+// the lowest c bits
+__device__ __forceinline__ uint64_t below(int c) { return c >= 64 ? ~0ull : c > 0 ? (1ull << c) - 1 : 0; }
+
 // what a wait comes to that does not find its phase complete at once
 __device__ __noinline__ void hold_on(uint32_t bar, uint32_t parity, volatile int* dead) {
   if (!*dead && !wait(bar, parity)) *dead = 1;
 }
 
-template <class T, int DP>
+template <class T, int DP, bool WIN>
 __global__ void __launch_bounds__(kThreadsT, 2)
     attn_tile_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
                      const __grid_constant__ CUtensorMap mv) {
@@ -255,7 +260,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   __shared__ int2 found[32];
   __shared__ uint32_t tmem_s;
   __shared__ int scan[kThreadsT / 32], tile_of[4], dead;
-  __shared__ alignas(8) uint16_t unfit[kEnds][4];  // keys of the last blocks with values that are not finite, a bit each, and 16 a word
+  constexpr int NE = WIN ? 2 * kEnds : kEnds;
+  __shared__ alignas(8) uint16_t unfit[NE][4];  // keys of the last blocks with values that are not finite, a bit each, and 16 a word
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
   // ---- which tile: those of a sequence's last tokens, which see the most keys, come first
@@ -331,7 +337,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&tmem_s)), "n"(S::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
-  if (tid < kEnds * 4) unfit[tid / 4][tid % 4] = 0;
+  if (tid < NE * 4) unfit[tid / 4][tid % 4] = 0;
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
@@ -407,10 +413,14 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   // the first block with keys that some tokens see and others do not (of selected pages each may be one)
   const bool dense = !p.sel;
   const int ends = dense && lim_min < lim_max ? lim_min >> 6 : INT32_MAX / 2;
+  // With a window: the first key of any, the first keys' blocks, and how many blocks lie between them and the windows'.  Where
+  // the tokens' windows begin, blocks from low >> 6 to last_low >> 6 have keys that some see and others do not.
+  const int low = WIN ? max(0, lim_min - p.window) : 0, last_low = WIN && lim_min < lim_max ? lim_max - p.window - 1 : -1;
+  const int sink_blocks = WIN ? (min(p.sinks, lim_max) + 63) >> 6 : 0, gap = WIN ? max(0, (low >> 6) - sink_blocks) : 0;
   const int words = (TT + 31) / 32, window = p.sel ? kMaskWords / words : INT32_MAX;
   int done = 0;  // blocks before this window
   for (int w0 = 0; w0 < P; w0 = p.sel ? w0 + window : P) {
-    int npieces = (lim_max + BR - 1) >> log_br;  // of the window: all, or those of the listed pages
+    int npieces = ((lim_max + BR - 1) >> log_br) - (gap << log_pc);  // of the window: all, or those of the listed pages
     if (p.sel) {
       const int wn = min(window, P - w0);
       __syncthreads();
@@ -469,6 +479,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     // piece i of the window: its first key, -1 beyond the last
     auto key_of = [&](int i) {
       if (i >= npieces) return -1;
+      if (WIN) return (i + ((i >> log_pc) < sink_blocks ? 0 : gap << log_pc)) << log_br;
       return p.sel ? ((w0 + list[i >> log_pp]) << p.log_page) + ((i & (1 << log_pp) - 1) << log_br) : i << log_br;
     };
 
@@ -479,6 +490,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       for (int k0 = 0; k0 < n; k0 += 32 >> log_pc) {
         const int key = key_of(i0 + (k0 << log_pc) + lane);
         int have = key < 0 ? 0 : max(0, min(BR, lim_max - key)), y = 0;
+        if (WIN && key >= p.sinks && key + BR <= low) have = 0;
         if (have > 0) {
           const int id = table[key >> p.log_page];
           if (id < 0 || id >= p.pages) {
@@ -506,8 +518,15 @@ __global__ void __launch_bounds__(kThreadsT, 2)
             bytes += some > 0 ? BR * DP * 2 : 0;
           }
           if (lane == 0) {
-            info[g % kInfo].full = full && first + k < ends;
-            info[g % kInfo].end = max(0, first + k - ends + 1);
+            if (WIN) {
+              const int kb = first + k < sink_blocks ? first + k : first + k + gap, at = kb << 6;
+              info[g % kInfo].full = full && kb < ends && (at >= lim_max - p.window || at + 64 <= p.sinks);
+              info[g % kInfo].end = kb >= ends ? kb - ends + 1
+                                    : last_low >= 0 && kb >= low >> 6 && kb <= last_low >> 6 ? kEnds + 1 + kb - (low >> 6) : 0;
+            } else {
+              info[g % kInfo].full = full && first + k < ends;
+              info[g % kInfo].end = max(0, first + k - ends + 1);
+            }
             mbar_arrive(su32(&info_full[g % kInfo]));
           }
           if (*(volatile int*)&dead) bytes = 0;
@@ -573,7 +592,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           if (on && p.sel) on = masks[list[i0 + k >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
           hold(&info_full[g % kInfo], g / kInfo & 1);
           const int c = on ? min(bl.have[0], lim - key) : 0;
-          see = c >= 64 ? ~0ull : c > 0 ? (1ull << c) - 1 : 0;
+          see = below(c);
+          if (WIN) see &= ~below(lim - key - p.window) | below(p.sinks - key);
         } else {
           hold(&info_full[g % kInfo], g / kInfo & 1);
 #pragma unroll 1
@@ -582,7 +602,11 @@ __global__ void __launch_bounds__(kThreadsT, 2)
             bool on = live_row && key >= 0;
             if (on && p.sel) on = masks[list[i >> log_pp] * words + tok / 32] >> (tok % 32) & 1;
             const int c = on ? min(bl.have[j], lim - key) : 0;
-            if (c > 0) see |= ((1ull << c) - 1) << (j << log_br);
+            if (WIN) {
+              see |= (below(c) & (~below(lim - key - p.window) | below(p.sinks - key))) << (j << log_br);
+            } else {
+              if (c > 0) see |= ((1ull << c) - 1) << (j << log_br);
+            }
           }
         }
         // (with all pages, a row that sees nothing of a block is masked, too, whatever the keys hold)
@@ -661,7 +685,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         if (!bl.full) {
           hold(&v_full[st], g / kStages & 1);
           __syncwarp();
-          zero_values<T, DP>(vbuf + st * S::KV, bl, log_br, bl.end ? unfit[bl.end - 1] : nullptr);
+          const int at = WIN ? key_of(i0 + (k << log_pc)) : 0;
+          zero_values<T, DP, WIN>(vbuf + st * S::KV, bl, log_br, bl.end ? unfit[bl.end - 1] : nullptr, p.sinks - at, low - at);
         }
         tm_wait_st();
         // each block's products with V are waited for, and in order, so that a parity names one of two phases; those of the
@@ -679,16 +704,18 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     if (done > 0) hold(&pv_done, (done - 1) & 1);
     group_sync<kSoft>();  // what was said of the last blocks' keys
     tm_fence_after();
-    // the keys of end block e that row r's token sees and whose values are still missing
+    // the first key of end block e, and its keys that a token sees and whose values are still missing
+    auto block_of = [&](int e) { return (e < kEnds ? ends + e : (low >> 6) + e - kEnds) * 64; };
     auto missing = [&](int e, int limit_of) -> uint64_t {
-      const int c = limit_of - (ends + e) * 64;
-      const uint64_t bits = *reinterpret_cast<const uint64_t*>(unfit[e]);
-      return c >= 64 ? bits : c > 0 ? bits & ((1ull << c) - 1) : 0;
+      const int at = block_of(e);
+      uint64_t bits = *reinterpret_cast<const uint64_t*>(unfit[e]) & below(limit_of - at);
+      if (WIN) bits &= ~below(limit_of - at - p.window) | below(p.sinks - at);
+      return bits;
     };
     uint64_t some = 0;
     if (dense)
 #pragma unroll
-      for (int e = 0; e < kEnds; ++e) some |= missing(e, lim);
+      for (int e = 0; e < NE; ++e) some |= missing(e, lim);
     const unsigned lacking = __ballot_sync(~0u, live_row && some != 0);
     auto cell_of = [&](int r, int tk) { return (int64_t)(t0 + tk) * p.H * p.G.d + h * p.G.d + p.G.mod(r); };
     auto queries_of = [&](int r, int tk) { return q + (t0 + tk) * p.q_ts + (int64_t)(h * p.G.d + p.G.mod(r)) * p.q_hs; };
@@ -761,8 +788,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
       float* sums = p.splits > 1 ? p.split_sums + ((int64_t)z * p.T * p.H * p.G.d + at) * DP : reinterpret_cast<float*>(smem) + warp * DP;
       if (p.splits == 1)
         for (int d = lane; d < p.D; d += 32) sums[d] = 0.f;
-      for (int e = 0; e < kEnds; ++e)
-        add_keys<T, DP>(p, queries_of(r, tk), table, h, (ends + e) * 64, missing(e, limit(tk)), p.scale * 1.44269504f, mr, sums);
+      for (int e = 0; e < NE; ++e)
+        add_keys<T, DP>(p, queries_of(r, tk), table, h, block_of(e), missing(e, limit(tk)), p.scale * 1.44269504f, mr, sums);
       if (p.splits == 1) {
         T* dst = static_cast<T*>(p.out) + at * p.D;
         for (int d = lane; d < p.D; d += 32) dst[d] = from_f32<T>(to_f32(dst[d]) + sums[d] * n);
@@ -838,13 +865,15 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
 
 template <class T, int DP>
 cudaError_t prepare_one() {
-  return cudaFuncSetAttribute(attn_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
+  const cudaError_t e = cudaFuncSetAttribute(attn_tile_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
+  return e != cudaSuccess ? e
+                          : cudaFuncSetAttribute(attn_tile_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
 }
 
 template <class T, int DP>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int64_t grid, cudaStream_t stream) {
-  const cudaError_t e = launch_after(attn_tile_kernel<T, DP>, dim3((unsigned)grid), kThreadsT, TileShape<DP>::SMEM, stream, 1,
-                                     p, c.mk, c.mv);
+  const cudaError_t e = launch_after(p.window < p.width * p.page ? attn_tile_kernel<T, DP, true> : attn_tile_kernel<T, DP, false>,
+                                     dim3((unsigned)grid), kThreadsT, TileShape<DP>::SMEM, stream, 1, p, c.mk, c.mv);
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t cells = (int64_t)p.T * p.H * p.G.d;
   return launch_after(attn_tile_join_kernel<T, DP>, dim3((unsigned)((cells + 7) / 8)), 256, 0, stream, 1, p);
@@ -892,7 +921,8 @@ cudaError_t tile_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t s
   // about 8 on its queries and masks, but side by side with the others).  3 chunks of 333 tokens, 8 heads of 64: 71 us
   // whole, 35 in four shares; 119 tokens of 2 heads over 1720 keys, with their selection: 50 us whole, 31 in shares.
   const int64_t cells = (int64_t)p.T * p.H * p.G.d, room = (int64_t)2 * sms * kRowsT;
-  const int64_t pages = p.sel ? std::min<int64_t>(p.width, (int64_t)TT * p.keep) : p.width;
+  const int64_t pages = p.sel ? std::min<int64_t>(p.width, (int64_t)TT * p.keep)
+                              : std::min<int64_t>(p.width, ((int64_t)p.window + p.sinks + TT + 2 * kKeys) / p.page + 1);
   const int64_t splits = std::min({(int64_t)kSplits, 2 * sms / tiles, pages * p.page / kKeys / 4, room / cells});
   p.splits = (int)std::max<int64_t>(1, splits);
   p.split_sums = c.tiles;

@@ -365,6 +365,26 @@ def test_codes_scales(pp, dt, scale):
     check(pp, dt, 1, 4, 128, 16, [70], [0, 40], None, 0, scale=scale)
 
 
+# enough rows for tiles of them on the tensor cores
+TILES = [
+    (BF16, 8, 4, 64, 16, [170], [0, 40]),
+    (F16, 8, 1, 128, 8, [300, 40], [0, 150, 190]),
+    (BF16, 4, 3, 80, 64, [200], [0, 130]),
+    (F16, 8, 2, 64, 128, [500], [0, 64]),
+    (BF16, 16, 8, 128, 32, [90, 0, 200], [0, 20, 20, 52]),
+    (F16, 4, 64, 128, 16, [70, 30], [0, 3, 12]),
+    (BF16, 8, 2, 112, 256, [700], [0, 128]),
+    (F16, 8, 4, 48, 16, [30], [0, 50]),      # more tokens than keys
+]
+
+
+@pytest.mark.parametrize("case", TILES)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("strided", [False, True])
+def test_codes_tiles(pp, case, causal, strided):
+    check(pp, *case, None, 0, causal=causal, strided=strided)
+
+
 WINDOWS = [(1, 0), (2, 1), (5, 3), (16, 0), (17, 130), (63, 4), (64, 64), (100, 1), (200, 16), (2 ** 31 - 1, 5), (3, 2 ** 31 - 1)]
 
 
@@ -382,12 +402,20 @@ def test_window_chunk(pp, case, window, sinks, codes):
     check(pp, *case, window, sinks, codes=codes, garbage=True)
 
 
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+@pytest.mark.parametrize("case", TILES)
+@pytest.mark.parametrize("codes", [False, True])
+def test_window_tiles(pp, case, window, sinks, codes):
+    check(pp, *case, window, sinks, codes=codes, garbage=True)
+
+
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("dt", [F32, F16, BF16])
 def test_window_of_all_tokens(pp, dt, codes):
     """Without the causal flag every token sees the sequence's last keys."""
     check(pp, dt, 2, 2, 64, 16, [150, 40], [0, 20, 70], 33, 2, codes=codes, causal=False, garbage=True)
     check(pp, dt, 1, 3, 128, 32, [150, 0], None, 33, 70, codes=codes, causal=False, garbage=True)
+    check(pp, dt, 8, 2, 64, 16, [150, 40], [0, 50, 100], 33, 2, codes=codes, causal=False, garbage=True)
 
 
 @pytest.mark.parametrize("dt", [F32, F16, BF16])
@@ -413,10 +441,11 @@ def broken(values, where):
 
 @pytest.mark.parametrize("dt", [F32, F16, BF16])
 @pytest.mark.parametrize("G,n,window,sinks", [(2, 6, 40, 3), (1, 16, 5, 0), (4, 60, 20, 10), (1, 150, 30, 64), (2, 64, 1, 0), (8, 3, 100, 2)])
-def test_values_not_finite_reach_who_sees_them(pp, dt, G, n, window, sinks):
+@pytest.mark.parametrize("H", [2, 8])
+def test_values_not_finite_reach_who_sees_them(pp, dt, H, G, n, window, sinks):
     """Keys of a chunk, at the ends of the windows and of the first keys: a row that sees one has what the definition gives,
     every other row is as if it was not there."""
-    H, D, page, L = 2, 64, 16, 170
+    D, page, L = 64, 16, 170
     where = sorted({0, sinks, max(0, L - n - window), max(0, L - n - window + 2), L - n, L - n + 1, L - 1, L - window})
     values = [math.inf, math.nan, -math.inf, math.nan, math.inf, math.nan, math.inf, -math.inf][: len(where)]
     g = torch.Generator().manual_seed(3)
@@ -441,34 +470,33 @@ def test_values_not_finite_reach_who_sees_them(pp, dt, G, n, window, sinks):
 
 def test_codes_pages_of_zeros(pp):
     """Pages whose scale is 0 hold zeros: their keys count in the softmax, and beside pages of any size."""
-    H, G, D, page, L = 1, 4, 64, 8, 90
-    for dt in (F32, F16, BF16):
-        for starts, n in ((None, 1), ([0, 40], 40)):
-            h = Held(pp, 14, H, page, D, dt)
-            table = tables([L], page, 14)
+    G, D, page, L = 4, 64, 8, 90
+    for dt, H, starts, n in [(dt, H, *x) for dt in (F32, F16, BF16) for H in (1, 8) for x in ((None, 1), ([0, 40], 40))]:
+        h = Held(pp, 14, H, page, D, dt)
+        table = tables([L], page, 14)
+        for i in range(2):
+            for w in range(0, 12, 3):
+                h.dc[i][int(table[0, w])] = 0
+                h.ds[i][int(table[0, w])] = 0
+            for w in range(1, 12, 4):
+                h.ds[i][int(table[0, w])] *= 2.0 ** -60 if i else 2.0 ** -20
+            h.c[i], h.s[i] = h.dc[i].cpu(), h.ds[i].cpu()
+        q = torch.randn((n, H * G, D), generator=torch.Generator().manual_seed(4)).to(dt)
+        out = torch.empty((n, H * G, D), device="cuda", dtype=dt)
+        try:
+            pp.pp_attn_forward(h.cache, q.cuda(), None if starts is None else ints(starts).cuda(), table.cuda(), ints([L]).cuda(), 0.125,
+                               pp.PP_ATTN_CAUSAL, None, out)
+            k, v = h.values()
+            want, _, tol, _ = ref8.attend(q, k, v, table, starts, [L], 0.125, True, L, 0, True)
+            assert ref.worst(out, want, tol) <= 1 and h.status() == 0
             for i in range(2):
-                for w in range(0, 12, 3):
-                    h.dc[i][int(table[0, w])] = 0
-                    h.ds[i][int(table[0, w])] = 0
-                for w in range(1, 12, 4):
-                    h.ds[i][int(table[0, w])] *= 2.0 ** -60 if i else 2.0 ** -20
-                h.c[i], h.s[i] = h.dc[i].cpu(), h.ds[i].cpu()
-            q = torch.randn((n, H * G, D), generator=torch.Generator().manual_seed(4)).to(dt)
-            out = torch.empty((n, H * G, D), device="cuda", dtype=dt)
-            try:
-                pp.pp_attn_forward(h.cache, q.cuda(), None if starts is None else ints(starts).cuda(), table.cuda(), ints([L]).cuda(), 0.125,
-                                   pp.PP_ATTN_CAUSAL, None, out)
-                k, v = h.values()
-                want, _, tol, _ = ref8.attend(q, k, v, table, starts, [L], 0.125, True, L, 0, True)
-                assert ref.worst(out, want, tol) <= 1 and h.status() == 0
-                for i in range(2):
-                    h.dc[i].zero_()
-                    h.ds[i].zero_()
-                pp.pp_attn_forward(h.cache, q.cuda(), None if starts is None else ints(starts).cuda(), table.cuda(), ints([L]).cuda(), 0.125,
-                                   pp.PP_ATTN_CAUSAL, None, out)
-                assert not out.any()
-            finally:
-                h.close()
+                h.dc[i].zero_()
+                h.ds[i].zero_()
+            pp.pp_attn_forward(h.cache, q.cuda(), None if starts is None else ints(starts).cuda(), table.cuda(), ints([L]).cuda(), 0.125,
+                               pp.PP_ATTN_CAUSAL, None, out)
+            assert not out.any()
+        finally:
+            h.close()
 
 
 def test_codes_queries_of_any_size(pp):
