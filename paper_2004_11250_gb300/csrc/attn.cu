@@ -35,7 +35,7 @@ pp_status attend(const pp_cache* cache, int T, const void* q, int64_t q_ts, int6
                   FastDiv(G), FastDiv(c.H), FastDiv(std::max(keep, 1)), 1, nullptr, nullptr,
                   windowed ? window : most, windowed ? std::min(sinks, most) : 0, c.scales8[0], c.scales8[1]};
   const cudaStream_t s = (cudaStream_t)stream;
-  const cudaError_t e = eight ? rows8_launch(p, c, sms, s)
+  const cudaError_t e = eight ? (tile8_applicable(p, c.dtype, sms) ? tile8_launch(p, c, sms, s) : rows8_launch(p, c, sms, s))
                         : tile_applicable(p, c.dtype, sms) ? tile_launch(p, c, sms, s)
                         : windowed ? rows_window_launch(p, c, sms, s)
                                    : rows_launch(p, c, sms, s);
@@ -70,6 +70,7 @@ cudaError_t attn_prepare() {
     if (e == cudaSuccess) e = prepare_type<__nv_bfloat16, __nv_bfloat16, false>();
     if (e == cudaSuccess) e = rows_window_prepare();
     if (e == cudaSuccess) e = rows8_prepare();
+    if (e == cudaSuccess) e = tile8_prepare();
     return e;
   });
 }
