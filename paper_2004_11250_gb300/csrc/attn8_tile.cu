@@ -3,15 +3,22 @@
 // 128 values.
 //
 // The tensor cores take codes as f16, in which they are exact, so somebody has to
-// turn each byte into two.  Four warps do so once for two tiles: they load a block of
-// 64 keys (the next one's while they write this one's), and write it as the swizzled
-// operands that a copy of f16 would have made.  Per block and tile, as in attn_tile.cu:
-//   S = Q K^T            128 x 64, queries in f16 (bf16 times a power of two per row)
-//   P = 2^(S ks - m) vs  a thread per row; ks, vs are the page's scales, vs over the
-//                        largest of the tile's pages, so that P stays below its bound
-//   O += P V             P from TMEM (over S's own columns), V from shared memory
-// and O is multiplied by the largest vs over the row's sum at the end.  Codes are
-// finite, so a key that a row does not see adds 0 whatever it holds.
+// turn each byte into two.  Four warps do so once for two tiles: blocks of 64 keys are
+// copied as they are, while they write the ones before as the swizzled operands that a copy
+// of f16 would have made.  (Loads into registers instead are waited for as a whole: a warp
+// has few counters for what is on its way.)  Per block and tile
+//   S = Q K^T                 128 x 64, queries in f16 (bf16 times a power of two per row)
+//   P = 2^(S ks + log2 vs - m)   a thread per row; ks, vs are the scales of the key's page, vs
+//                             over the largest of the tile's pages
+//   O += P V                  P from TMEM (over S's own columns), V from shared memory
+// so that O over sum P / vs, times the largest vs, is the output.  A block's scores are there
+// before the softmax of the one before is done (two S buffers).  Codes are finite, so a key that a row does not see adds 0
+// whatever it holds.
+//
+// m stays as it is while the weights fit f16 (they are up to 2^12 when it is set): a block is
+// computed with the last one's m, and only where some 8 weights' sum, which the row's total wants
+// anyway, says that one might not fit, once more, with m raised and the sums so far made smaller.
+// So most blocks read S once, and neither wait for nor look for a maximum.
 #include <algorithm>
 #include <type_traits>
 
@@ -24,34 +31,30 @@ using namespace ppc_attn;
 
 constexpr int kRowsT = 128;                       // query rows of a tile
 constexpr int kSoft = 2 * kRowsT;                 // threads of the softmax
-constexpr int kTurn = 128;                        // that turn codes into f16; then a multiplying warp, and three that idle
-constexpr int kThreads8 = kSoft + kTurn + 128;
-// Registers of a thread at launch, and after they are shared out by warpgroups: a row of 64 scores wants more than 128.
-constexpr int kRegs = 128, kRegsSoft = 176, kRegsTurn = 96, kRegsMul = 64;
-static_assert(2 * kRegsSoft + kRegsTurn + kRegsMul == 4 * kRegs && kThreads8 * kRegs == 65536, "what the block was launched with");
-constexpr int kKeys = 64;                         // keys per block
-constexpr int kStages = 2;                        // of K and of V
-constexpr int kInfo = 8;                          // blocks whose notes are kept: the turning warps are up to 4 ahead of the softmax
+constexpr int kTurn = 128;                        // that turn codes into f16; then a multiplying warp and a copying one
+constexpr int kMulWarp = (kSoft + kTurn) / 32, kCopyWarp = kMulWarp + 1;
+constexpr int kThreads8 = kSoft + kTurn + 64;
+constexpr int kKeys = 64, kLogKeys = 6;           // keys per block
+constexpr int kStages = 3;                        // of K and of V in f16
+constexpr int kCopies = 2;                        // blocks of codes on their way
+constexpr int kInfo = 8;                          // blocks whose notes are kept: those of block g are written when K of g - 2 has been, after the
+                                                  // scores of g - 5, which were asked for when the softmax had done with g - 7
 constexpr int kSplits = 8;                        // shares of a tile's blocks at most
-constexpr int kUp = 13;                           // weights are up to 2^13 where m is not behind, and 2^2 times that
-constexpr float kGrow = 2.f;
+constexpr int kUp = 12;                           // weights are up to 2^12 when m is set
+constexpr float kMost = 65504.f;                  // 8 weights' sum at most: f16's largest number, and twice what they can be then
+constexpr float kLeastScale = -42.f;              // log2 of vs at the least: 2^16 times it is 0 in f16
 
 template <int DP>
 struct Shape8 {
-  static constexpr int Q = kRowsT * DP * 2, KV = kKeys * DP * 2;
-  static constexpr int SMEM = 2 * Q + 2 * kStages * KV + 1024;
+  static constexpr int Q = kRowsT * DP * 2, KV = kKeys * DP * 2, CODES = kKeys * DP;
+  static constexpr int SMEM = 2 * Q + 2 * kStages * KV + 2 * kCopies * CODES + 1024;
   static constexpr int COLS = 512;  // TMEM: O of the tiles at 0 and 128, S at 256, 320 and 384, 448
 };
 
-struct alignas(16) Note {  // of a block
-  float ks[8], vs[8];      // scales of each 8 keys; vs over the largest
-  uint16_t valid[4];       // keys that are there, a bit each
+struct alignas(16) Note {           // of a block
+  float ks[8], lv[8], inv[8];       // of each 8 keys: the keys' scale; log2 of the values' over the largest, and 1 over that
+  uint32_t valid;                   // a bit for each 8 keys that are there
 };
-
-template <int N>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // 16 codes as 16 f16 (attn_row.cuh has the same by bytes' parity)
 __device__ __forceinline__ uint32_t f16_pair(uint32_t biased, uint32_t bytes) {
@@ -73,10 +76,12 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   unsigned char* kbuf = smem + 2 * S::Q;
   unsigned char* vbuf = kbuf + kStages * S::KV;
+  unsigned char* codes = vbuf + kStages * S::KV;  // of K and of V, as they are in the cache
   __shared__ alignas(8) uint64_t q_full[2], k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], s_full[2][2],
-      p_full[2][2], pv_done[2], note_full[kInfo];
+      p_full[2][2], pv_done[2], o_full[2], note_full[kInfo], codes_full[2][kCopies], codes_empty[2][kCopies];
   __shared__ Note notes[kInfo];
-  __shared__ float row_scale[kSoft], most[kThreads8 / 32];
+  __shared__ float most[kThreads8 / 32];
+  __shared__ uint8_t row_power[kSoft];
   __shared__ uint32_t tmem_s;
   __shared__ int scan[kThreads8 / 32], tile_of[4], dead;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -145,34 +150,39 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
   const int lim_min = limit(0), lim_max = limit(nt - 1);
   const int* table = p.table + (int64_t)b * p.width;
   // the first key of a window, and the blocks between the first keys' and the windows'
-  const int low = max(0, lim_min - p.window), sink_blocks = (min(p.sinks, lim_max) + 63) >> 6, gap = max(0, (low >> 6) - sink_blocks);
-  const int blocks = ((lim_max + 63) >> 6) - gap, first = (int)((int64_t)blocks * z / p.splits), n = (int)((int64_t)blocks * (z + 1) / p.splits) - first;
-  auto key_of = [&](int k) { return (first + k < sink_blocks ? first + k : first + k + gap) << 6; };  // of the share's block k
+  const int low = max(0, lim_min - p.window), sink_blocks = (min(p.sinks, lim_max) + kKeys - 1) >> kLogKeys, gap = max(0, (low >> kLogKeys) - sink_blocks);
+  const int blocks = ((lim_max + kKeys - 1) >> kLogKeys) - gap, first = (int)((int64_t)blocks * z / p.splits), n = (int)((int64_t)blocks * (z + 1) / p.splits) - first;
+  auto key_of = [&](int k) { return (first + k < sink_blocks ? first + k : first + k + gap) << kLogKeys; };  // of the share's block k
   const bool two = nt > T1;
   // a negative scale goes into the queries, and so does 0 (with no queries, any scale): sl > 0
   const float sl = p.scale == 0.f ? 1.f : fabsf(p.scale) * 1.44269504f;
 
   // ---- set up
-  if (warp == (kSoft + kTurn) / 32) {
+  if (warp == kMulWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&tmem_s)), "n"(S::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(su32(&q_full[i]), kRowsT);
+      mbar_init(su32(&q_full[i]), 4);  // warps, as below: arrivals of threads come one after another
       mbar_init(su32(&pv_done[i]), 1);
+      mbar_init(su32(&o_full[i]), 1);
       for (int j = 0; j < 2; ++j) {
         mbar_init(su32(&s_full[i][j]), 1);
-        mbar_init(su32(&p_full[i][j]), kRowsT);
+        mbar_init(su32(&p_full[i][j]), 4);
+      }
+      for (int j = 0; j < kCopies; ++j) {
+        mbar_init(su32(&codes_full[i][j]), 1);
+        mbar_init(su32(&codes_empty[i][j]), 4);
       }
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(su32(&k_full[i]), kTurn);
+      mbar_init(su32(&k_full[i]), 4);
       mbar_init(su32(&k_empty[i]), 1);
-      mbar_init(su32(&v_full[i]), kTurn);
+      mbar_init(su32(&v_full[i]), 4);
       mbar_init(su32(&v_empty[i]), 1);
     }
-    for (int i = 0; i < kInfo; ++i) mbar_init(su32(&note_full[i]), kTurn);
+    for (int i = 0; i < kInfo; ++i) mbar_init(su32(&note_full[i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // the largest scale of values among the pages that some token sees
@@ -200,131 +210,159 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
     if (!wait(su32(bar), parity)) dead = 1;
   };
 
-  if (warp >= (kSoft + kTurn) / 32) {
+  // what the warp has done before is there for who waits
+  auto warp_arrive = [&](uint64_t* bar) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(su32(bar));
+  };
+
+  if (warp >= kMulWarp) {
+    if (warp == kCopyWarp) {
+      // ---- copies, and what there is to say of a block.  Lane j < 8 has keys 8 j on; a run of keys on one page is one copy.
+      // Pages are looked up two blocks ahead and scales one, so that neither is waited for
+      const int run = min(p.page, kKeys), runs = run >> 3;
+      auto look = [&](int k) {  // the page's entry of the table; INT32_MIN: none of the run's keys is there
+        const int key = lane < 8 && k < n ? key_of(k) + (lane * 8 & ~(run - 1)) : INT32_MAX;
+        return key < lim_max && (key < p.sinks || key + run > low) ? table[key >> p.log_page] : INT32_MIN;
+      };
+      const float vinv = vtop > 0.f ? 1.f / vtop : 0.f;
+      int64_t cell = -1;
+      float ks = 0.f, vs = 0.f;
+      auto resolve = [&](int id) {
+        const bool there = id >= 0 && id < p.pages;
+        if (!there && id != INT32_MIN) atomicOr(p.status, PP_CACHE_BAD_PAGE);
+        cell = there ? (int64_t)id * p.H + h : -1;
+        ks = vs = 0.f;
+        if (there) {
+          ks = __ldg(p.ks + cell);
+          vs = __ldg(p.vs + cell);
+        }
+      };
+      int ahead = look(1);
+      resolve(look(0));
+      for (int g = 0; g < n; ++g) {
+        Note& note = notes[g % kInfo];
+        const unsigned there = __ballot_sync(~0u, cell >= 0);
+        const int bytes = __popc(there) * 8 * p.D, key = key_of(g) + lane * 8;
+        const int64_t from = (cell * p.page + (key & p.page - 1)) * p.D;
+        const bool lead = cell >= 0 && (lane & runs - 1) == 0;
+        auto copy = [&](int i, const void* pool) {
+          const int at = g % kCopies;
+          hold(&codes_empty[i][at], g / kCopies & 1 ^ 1);
+          const bool go = !*(volatile int*)&dead;
+          if (lane == 0) mbar_arrive_expect_tx(su32(&codes_full[i][at]), go ? bytes : 0);
+          __syncwarp();
+          if (go && lead)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                             su32(codes + (i * kCopies + at) * S::CODES) + lane * 8 * p.D),
+                         "l"(static_cast<const int8_t*>(pool) + from), "r"(run * p.D), "r"(su32(&codes_full[i][at]))
+                         : "memory");
+          __syncwarp();
+        };
+        copy(0, p.k);
+        if (lane < 8) {
+          const float lv = vs > 0.f ? fmaxf(__log2f(vs * vinv), kLeastScale) : kLeastScale;
+          note.ks[lane] = ks;
+          note.lv[lane] = lv;
+          note.inv[lane] = ex2(-lv);
+          if (lane == 0) note.valid = there;
+        }
+        warp_arrive(&note_full[g % kInfo]);
+        copy(1, p.v);
+        resolve(ahead);
+        ahead = look(g + 2);
+      }
+    }
     // ---- products
-    fewer_registers<kRegsMul>();
-    if (warp == (kSoft + kTurn) / 32) {
-    const uint32_t leader = elect();
-    const uint32_t qa = desc_lo(su32(smem), 16), kb = desc_lo(su32(kbuf), 16), vb = desc_lo(su32(vbuf), CHUNK_KV);
-    auto scores = [&](int g) {
-      const int st = g % kStages;
-      hold(&k_full[st], g / kStages & 1);
-      tm_fence_after();
-      const uint32_t kd = kb + st * (S::KV >> 4);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t && !two) break;
-        const uint32_t to = tmem + 256 + t * 128 + (g & 1) * 64;
-#pragma unroll
-        for (int kk = 0; kk < DP / 16; ++kk)
-          mma_ss(to, qa + (t * S::Q + kk / 4 * CHUNK_Q + kk % 4 * 32 >> 4), kd + (kk / 4 * CHUNK_KV + kk % 4 * 32 >> 4),
-                 idesc<__half>(kRowsT, kKeys, false), kk > 0, leader);
-        commit(su32(&s_full[t][g & 1]), leader);
-      }
-      commit(su32(&k_empty[st]), leader);
-    };
-    if (n > 0) {
-      hold(&q_full[0], 0);
-      if (two) hold(&q_full[1], 0);
-      scores(0);
-    }
-    for (int g = 0; g < n; ++g) {
-      const int st = g % kStages;
-      if (g + 1 < n) scores(g + 1);
-      hold(&v_full[st], g / kStages & 1);
-      const uint32_t vd = vb + st * (S::KV >> 4);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t && !two) break;
-        hold(&p_full[t][g & 1], g >> 1 & 1);
+    if (warp == kMulWarp) {
+      const uint32_t leader = elect();
+      const uint32_t qa = desc_lo(su32(smem), 16), kb = desc_lo(su32(kbuf), 16), vb = desc_lo(su32(vbuf), CHUNK_KV);
+      auto scores = [&](int g) {
+        const int st = g % kStages;
+        hold(&k_full[st], g / kStages & 1);
         tm_fence_after();
-        const uint32_t pt = tmem + 256 + t * 128 + (g & 1) * 64;
+        const uint32_t kd = kb + st * (S::KV >> 4);
 #pragma unroll
-        for (int kk = 0; kk < kKeys / 16; ++kk)
-          mma_ts(tmem + t * 128, pt + kk * 8, vd + (kk * 2048 >> 4), idesc<__half>(kRowsT, DP, true), g > 0 || kk > 0, leader);
-        commit(su32(&pv_done[t]), leader);
+        for (int t = 0; t < 2; ++t) {
+          if (t && !two) break;
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk)
+            mma_ss(tmem + 256 + t * 128 + (g & 1) * 64, qa + (t * S::Q + kk / 4 * CHUNK_Q + kk % 4 * 32 >> 4),
+                   kd + (kk / 4 * CHUNK_KV + kk % 4 * 32 >> 4), idesc<__half>(kRowsT, kKeys, false), kk > 0, leader);
+          commit(su32(&s_full[t][g & 1]), leader);
+        }
+        commit(su32(&k_empty[st]), leader);
+      };
+      // Products run in the order in which they are asked for, so the scores that go where a block's P was lie behind its product
+      if (n > 0) {
+        hold(&q_full[0], 0);
+        if (two) hold(&q_full[1], 0);
+        scores(0);
       }
-      commit(su32(&v_empty[st]), leader);
-    }
+      for (int g = 0; g < n; ++g) {
+        if (g + 1 < n) scores(g + 1);
+        const int st = g % kStages;
+        hold(&v_full[st], g / kStages & 1);
+        const uint32_t vd = vb + st * (S::KV >> 4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (t && !two) break;
+          hold(&p_full[t][g & 1], g >> 1 & 1);
+          tm_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < kKeys / 16; ++kk)
+            mma_ts(tmem + t * 128, tmem + 256 + t * 128 + (g & 1) * 64 + kk * 8, vd + (kk * 2048 >> 4), idesc<__half>(kRowsT, DP, true),
+                   g > 0 || kk > 0, leader);
+          commit(su32(&pv_done[t]), leader);
+          if (g + 1 == n) commit(su32(&o_full[t]), leader);
+        }
+        commit(su32(&v_empty[st]), leader);
+      }
     }
   } else if (warp >= kSoft / 32) {
-    fewer_registers<kRegsTurn>();
-    // ---- codes to f16: a warp has 16 keys of a block, which lie on one page, or on two of 8
-    constexpr int CPR = DP / 16, RPL = 32 / CPR, NI = 16 / RPL;  // chunks of 16 codes to a row, rows to a load, loads
-    const int w = warp - kSoft / 32, c = lane % CPR, r = lane / CPR;
+    // ---- codes to f16: a warp has 16 keys of a block, a lane 16 codes of a row at a time, their halves apart: e is the one that
+    // it takes first, so that 16 lanes read from all banks, and the 8 lanes that write at once write to all (rows of 128 or 64)
+    constexpr int CPR = DP / 16, RPL = 32 / CPR, NI = 16 / RPL;  // chunks of 16 codes to a row, rows to a step, steps
+    const int w = warp - kSoft / 32, c = lane % CPR, r = lane / CPR, e = DP == 128 ? c >> 2 ^ r & 1 : r >> 1 & 1;
     const bool in = c * 16 < p.D;
-    struct Place {
-      int64_t cell[2];  // of each 8 keys: (page id * H + h), -1: no key that is there
-    };
-    auto look = [&](int k) {
-      Place at;
+    const int key0 = w * 16 + r, from = key0 * p.D + c * 16 + e * 8, other = 8 - 16 * e;
+    // where the halves go: rows 4 on of 8 are swizzled by 4 more chunks
+    const int to0 = c / 4 * CHUNK_KV + key0 * 128;
+    const int at0 = to0 + ((c % 4 * 2 + e ^ key0 & 7) << 4), at1 = to0 + ((c % 4 * 2 + 1 - e ^ key0 & 7) << 4);
+    auto turn = [&](unsigned char* to, const unsigned char* codes) {
+      uint2 x[NI], y[NI];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        at.cell[j] = -1;
-        const int key = k < n ? key_of(k) + w * 16 + j * 8 : INT32_MAX;
-        if (key < lim_max && (key < p.sinks || key + 8 > low)) {
-          const int id = table[key >> p.log_page];
-          if (id >= 0 && id < p.pages) at.cell[j] = (int64_t)id * p.H + h;
-          else atomicOr(p.status, PP_CACHE_BAD_PAGE);
+      for (int i = 0; i < NI; ++i) {
+        x[i] = y[i] = make_uint2(0, 0);
+        if (in) {
+          x[i] = *reinterpret_cast<const uint2*>(codes + from + i * RPL * p.D);
+          y[i] = *reinterpret_cast<const uint2*>(codes + from + i * RPL * p.D + other);
         }
       }
-      return at;
-    };
-    auto load = [&](const void* pool, const Place& at, int k, uint4 (&x)[NI]) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int row = i * RPL + r;
-        const int64_t cell = at.cell[row >> 3];
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (in && cell >= 0)
-          x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const int8_t*>(pool) + (cell * p.page + (key_of(k) + w * 16 + row & p.page - 1)) * p.D + c * 16));
+        const int flip = i * RPL & 4 ? 64 : 0;
+        *reinterpret_cast<uint4*>(to + (at0 ^ flip) + i * RPL * 128) = f16_of8(x[i].x, x[i].y);
+        *reinterpret_cast<uint4*>(to + (at1 ^ flip) + i * RPL * 128) = f16_of8(y[i].x, y[i].y);
       }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     };
-    auto write = [&](unsigned char* to, const uint4 (&x)[NI]) {
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int key = w * 16 + i * RPL + r;
-        unsigned char* row = to + c / 4 * CHUNK_KV + key * 128;
-        const uint4 lo = f16_of8(x[i].x, x[i].y), hi = f16_of8(x[i].z, x[i].w);
-        // lanes of the second column write their halves the other way round, so that eight lanes meet eight banks
-        const int e = DP == 128 ? c >> 2 : 0;
-        *reinterpret_cast<uint4*>(row + ((c % 4 * 2 + e ^ key & 7) << 4)) = e ? hi : lo;
-        *reinterpret_cast<uint4*>(row + ((c % 4 * 2 + 1 - e ^ key & 7) << 4)) = e ? lo : hi;
-      }
-    };
-    const float vinv = vtop > 0.f ? 1.f / vtop : 0.f;
-    uint4 kx[NI], vx[NI];
-    Place here = look(0), next;
-    if (n > 0) {
-      load(p.k, here, 0, kx);
-      load(p.v, here, 0, vx);
-    }
     for (int g = 0; g < n; ++g) {
-      const int st = g % kStages;
-      const uint32_t ph = (g / kStages + 1) & 1;
-      next = look(g + 1);
+      const int st = g % kStages, at = g % kCopies;
+      const uint32_t ph = (g / kStages + 1) & 1, pc = g / kCopies & 1;
+      hold(&codes_full[0][at], pc);
       hold(&k_empty[st], ph);
-      if (lane < 2) {
-        const int64_t cell = lane ? here.cell[1] : here.cell[0];
-        notes[g % kInfo].ks[w * 2 + lane] = cell >= 0 ? p.ks[cell] : 0.f;
-        notes[g % kInfo].vs[w * 2 + lane] = cell >= 0 ? p.vs[cell] * vinv : 0.f;
-        if (lane == 0) notes[g % kInfo].valid[w] = (here.cell[0] >= 0 ? 0xFFu : 0u) | (here.cell[1] >= 0 ? 0xFF00u : 0u);
-      }
-      mbar_arrive(su32(&note_full[g % kInfo]));
-      write(kbuf + st * S::KV, kx);
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(su32(&k_full[st]));
-      if (g + 1 < n) load(p.k, next, g + 1, kx);
+      turn(kbuf + st * S::KV, codes + at * S::CODES);
+      warp_arrive(&k_full[st]);
+      if (lane == 0) mbar_arrive(su32(&codes_empty[0][at]));
+      hold(&codes_full[1][at], pc);
       hold(&v_empty[st], ph);
-      write(vbuf + st * S::KV, vx);
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(su32(&v_full[st]));
-      if (g + 1 < n) load(p.v, next, g + 1, vx);
-      here = next;
+      turn(vbuf + st * S::KV, codes + (kCopies + at) * S::CODES);
+      warp_arrive(&v_full[st]);
+      if (lane == 0) mbar_arrive(su32(&codes_empty[1][at]));
     }
   } else {
     // ---- queries, then the softmax, a thread per row
-    more_registers<kRegsSoft>();
     const int t = warp / 4, tr = tid % kRowsT, rows = (t ? nt - T1 : min(nt, T1)) * p.G.d;  // the tile, its row, its rows
     const bool some = rows > 0;
     const int base = t0 + t * T1;
@@ -353,7 +391,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         for (int u = 0; u < U; ++u) {
           const int r = (i0 + u * kRowsT) / L, c = (i0 + u * kRowsT) % L;
           const bool used = r < rows && c * 8 < p.D;
-          float f[8], up = 1.f, back = 1.f;
+          float f[8], up = 1.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] = used ? to_f32(v[u].v[e]) : 0.f;
           if constexpr (!std::is_same<T, __half>::value) {
@@ -363,9 +401,8 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
 #pragma unroll
             for (int m = 1; m < L; m <<= 1) top = max(top, __shfl_xor_sync(~0u, top, m));
             up = __int_as_float((268 - top) << 23);
-            back = __int_as_float((top - 14) << 23);
+            if (c == 0) row_power[t * kRowsT + r] = (uint8_t)(top - 14);
           }
-          if (c == 0) row_scale[t * kRowsT + r] = back;
           Vec<__half, 8> y;
 #pragma unroll
           for (int e = 0; e < 8; ++e) y.v[e] = __float2half_rn(sign == 0.f ? 0.f : f[e] * (up * sign));
@@ -373,111 +410,144 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(su32(&q_full[t]));
+      warp_arrive(&q_full[t]);
       // the rows of this tile's four warps
       asm volatile("bar.sync %0, %1;" ::"r"(1 + t), "n"(kRowsT) : "memory");
     }
     const bool live_row = tr < rows;
-    const int tok = live_row ? t * T1 + p.G.div(tr) : 0;
-    const int lim = live_row ? limit(tok) : 0;
-    const float slr = some ? sl * row_scale[t * kRowsT + tr] : 0.f;
-    const uint32_t row_tm = tmem + t * 128 + ((uint32_t)(warp % 4 * 32) << 16), s_tm = row_tm + 256;  // its sums, its scores
+    const int tok = t * T1 + p.G.div(min(tr, max(rows, 1) - 1));  // rows behind the last do as it does
+    const int lim = some ? limit(tok) : 0;
+    const float slr = sl * (std::is_same<T, __half>::value || !some ? 1.f : __int_as_float(row_power[t * kRowsT + tr] << 23));
+    const uint32_t row_tm = tmem + t * 128 + ((uint32_t)(warp % 4 * 32) << 16);  // its sums; its scores lie 256 on
     float m = -INFINITY, l = 0.f;
     for (int g = 0; some && g < n; ++g) {
       const int key = key_of(g);
       const Note& note = notes[g % kInfo];
       hold(&note_full[g % kInfo], g / kInfo & 1);
-      uint64_t see = *reinterpret_cast<const uint64_t*>(note.valid);
-      see &= live_row ? below(lim - key) & (~below(lim - key - p.window) | below(p.sinks - key)) : 0;
-      const bool part = __any_sync(~0u, live_row && see != ~0ull), none = __all_sync(~0u, see == 0);
+      const uint32_t valid = note.valid;
+      const bool part = __any_sync(~0u, valid != 0xFFu || lim - key < kKeys || (key < lim - p.window && key + kKeys > p.sinks));
+      // which of 32 keys the row sees
+      auto see = [&](int c) -> uint32_t {
+        const int at = key + c * 32;
+        const uint32_t v = (valid >> c * 4 & 15u) * 0x00204081u & 0x01010101u;  // a bit to a byte
+        return v * 255u & (uint32_t)(below(lim - at) & (~below(lim - at - p.window) | below(p.sinks - at)));
+      };
+      const uint32_t s_tm = row_tm + 256 + (g & 1) * 64;
       hold(&s_full[t][g & 1], g >> 1 & 1);
       __syncwarp();
       tm_fence_after();
-      const uint32_t tm = s_tm + (g & 1) * 64;
-      uint32_t w[32];
-      bool waited = false;
-      if (none) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = 0;
-      } else {
-        float x[64];
-        tm_ld32(tm, reinterpret_cast<float(&)[32]>(x[0]));
-        tm_ld32(tm + 32, reinterpret_cast<float(&)[32]>(x[32]));
-        float ks[8], vs[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          ks[j] = __fmul_rn(note.ks[j], slr);
-          vs[j] = note.vs[j];
-        }
+      float top = 0.f, sum = 0.f;
+      bool again = __any_sync(~0u, m == -INFINITY);  // m is not set: it has to be where the row sees something
+      if (again) again = __any_sync(~0u, m == -INFINITY && (!part || (see(0) | see(1))));
+      if (!again) {
+        uint32_t w[32];
+        const float at = m == -INFINITY ? 0.f : m;
+        float x[2][32];
+        tm_ld32(s_tm, x[0]);
+        tm_ld32(s_tm + 32, x[1]);
         tm_wait_ld();
-        const uint64_t zero = pack2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 32; ++i)  // a product plus 0, so that it is rounded before the maximum is taken from it
-          unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), pack2(ks[i / 4], ks[i / 4]), zero), x[2 * i], x[2 * i + 1]);
-        if (part) {
+        for (int c = 0; c < 2; ++c) {
+          float(&y)[32] = x[c];
+          const float4 ks = *reinterpret_cast<const float4*>(note.ks + 4 * c), lv = *reinterpret_cast<const float4*>(note.lv + 4 * c),
+                       inv = *reinterpret_cast<const float4*>(note.inv + 4 * c);
+          const float k4[4] = {ks.x, ks.y, ks.z, ks.w}, l4[4] = {lv.x, lv.y, lv.z, lv.w}, i4[4] = {inv.x, inv.y, inv.z, inv.w};
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (!((i < 32 ? (uint32_t)see : (uint32_t)(see >> 32)) >> (i & 31) & 1)) x[i] = -INFINITY;
-        }
-        float top[4];
+          for (int j = 0; j < 4; ++j) {
+            const float kj = k4[j] * slr, oj = l4[j] - at;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          top[c] = fmaxf(x[c], x[c + 4]);
+            for (int i = 0; i < 8; i += 2)
+              unpack2(fma2(pack2(y[8 * j + i], y[8 * j + i + 1]), pack2(kj, kj), pack2(oj, oj)), y[8 * j + i], y[8 * j + i + 1]);
+          }
+          if (part) {
+            const uint32_t bits = see(c);
 #pragma unroll
-          for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
-        }
-        const float mx = lower(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), (float)kUp);
-        const bool grow = mx > __fadd_rd(m, kGrow);  // from -infinity, too
-        if (__any_sync(~0u, grow)) {
-          const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
-          m = to;
-          l *= f;
-          if (g > 0) {  // the sums so far, in TMEM
-            hold(&pv_done[t], (g - 1) & 1);
-            waited = true;
-            __syncwarp();
-            tm_fence_after();
+            for (int i = 0; i < 32; ++i)
+              if (!(bits >> i & 1)) y[i] = -INFINITY;
+          }
 #pragma unroll
-            for (int c = 0; c < DP; c += 32) {
-              float o[32];
-              tm_ld32(row_tm + c, o);
-              tm_wait_ld();
-              uint32_t r[32];
+          for (int j = 0; j < 4; ++j) {
+            uint64_t s2 = 0;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * f);
-              tm_st32(row_tm + c, r);
+            for (int i = 0; i < 8; i += 2) {
+              const float a = ex2(y[8 * j + i]), b = ex2(y[8 * j + i + 1]);
+              s2 = add2(s2, pack2(a, b));
+              w[16 * c + 4 * j + i / 2] = pack<__half>(a, b);
             }
-            tm_wait_st();
+            float a, b;
+            unpack2(s2, a, b);
+            a += b;
+            top = fmaxf(top, a);
+            sum = fmaf(a, i4[j], sum);
+          }
+        }
+        again = __any_sync(~0u, top > kMost);
+        if (!again) {
+          l += sum;
+          tm_st32(s_tm, w);
+        }
+      }
+      if (again) {
+        // once more from the scores, with m above them.  Each step is rounded by itself, as the maximum's are, so that no weight
+        // passes its bound and the largest does not vanish where fp32 numbers lie further than 1 apart
+        auto exponents = [&](int c, float (&y)[32]) {
+          tm_ld32(s_tm + 32 * c, y);
+          tm_wait_ld();
+          const uint32_t bits = part ? see(c) : ~0u;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            y[i] = bits >> i & 1 ? __fadd_rn(__fmul_rn(y[i], note.ks[4 * c + i / 8] * slr), note.lv[4 * c + i / 8]) : -INFINITY;
+        };
+        float most = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          float y[32];
+          exponents(c, y);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) most = fmaxf(most, y[i]);
+        }
+        const float to = fmaxf(m, lower(most, (float)kUp)), f = to == -INFINITY ? 1.f : ex2(m - to);
+        m = to;
+        l *= f;
+        if (g > 0) {  // the sums so far, in TMEM.  (Those of g - 2 are done, as they lie before these scores: a parity names one phase)
+          hold(&pv_done[t], (g - 1) & 1);
+          __syncwarp();
+          tm_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < DP; c += 32) {
+            float o[32];
+            tm_ld32(row_tm + c, o);
+            tm_wait_ld();
+            uint32_t r[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * f);
+            tm_st32(row_tm + c, r);
           }
         }
         const float at = m == -INFINITY ? 0.f : m;
-        const uint64_t at2 = pack2(-at, -at);
-        uint64_t sum[4] = {};
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {  // weights go where scores were that have been read
+          float y[32];
+          exponents(c, y);
+          uint32_t r[16];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float a, c;
-          unpack2(add2(pack2(x[2 * i], x[2 * i + 1]), at2), a, c);
-          a = ex2(a);
-          c = ex2(c);
-          sum[i & 3] = add2(sum[i & 3], pack2(a, c));
-          unpack2(fma2(pack2(a, c), pack2(vs[i / 4], vs[i / 4]), zero), a, c);
-          w[i] = pack<__half>(a, c);
+          for (int i = 0; i < 32; i += 2) {
+            const float a = ex2(__fadd_rn(y[i], -at)), b = ex2(__fadd_rn(y[i + 1], -at));
+            l = fmaf(a + b, note.inv[4 * c + i / 8], l);
+            r[i / 2] = pack<__half>(a, b);
+          }
+          tm_st16(s_tm + 16 * c, r);
         }
-        float a, c;
-        unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, c);
-        l += a + c;
       }
-      tm_st32(tm, w);
       tm_wait_st();
-      // each block's products with V are waited for, and in order, so that a parity names one of two phases
-      if (g > 0 && !waited) hold(&pv_done[t], (g - 1) & 1);
       tm_fence_before();
-      mbar_arrive(su32(&p_full[t][g & 1]));
+      warp_arrive(&p_full[t][g & 1]);
     }
 
     // ---- out
     if (some) {
-      if (n > 0) hold(&pv_done[t], (n - 1) & 1);
+      // (a barrier of its own: of pv_done's last two phases both may be over, and their parities say nothing then)
+      if (n > 0) hold(&o_full[t], 0);
       __syncwarp();
       tm_fence_after();
       const int64_t cell = (int64_t)(base + p.G.div(live_row ? tr : 0)) * p.H * p.G.d + h * p.G.d + p.G.mod(live_row ? tr : 0);
@@ -531,11 +601,14 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
   __syncthreads();
   if (dead && tid == 0) {
     atomicOr(p.status, PP_CACHE_TIMEOUT);
-    // products still in flight end before the CTA does
+    // copies and products still in flight end before the CTA does
     for (int i = 0; i < 2; ++i)
-      for (uint32_t ph = 0; ph < 2; ++ph) wait(su32(&pv_done[i]), ph);
+      for (uint32_t ph = 0; ph < 2; ++ph) {
+        for (int j = 0; j < kCopies; ++j) wait(su32(&codes_full[i][j]), ph);
+        wait(su32(&pv_done[i]), ph);
+      }
   }
-  if (warp == (kSoft + kTurn) / 32) {
+  if (warp == kMulWarp) {
     __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS));
   }
@@ -543,11 +616,6 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
 
 template <class T, int DP>
 cudaError_t prepare_one() {
-  // warps that ask for more registers than the block has would wait for ever: it has to be launched with what they add up to
-  cudaFuncAttributes at;
-  const cudaError_t e = cudaFuncGetAttributes(&at, attn8_tile_kernel<T, DP>);
-  if (e != cudaSuccess) return e;
-  if (at.numRegs != kRegs) return cudaErrorInvalidConfiguration;
   return cudaFuncSetAttribute(attn8_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape8<DP>::SMEM);
 }
 
