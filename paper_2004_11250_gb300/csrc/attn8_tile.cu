@@ -31,9 +31,9 @@ using namespace ppc_attn;
 
 constexpr int kRowsT = 128;                       // query rows of a tile
 constexpr int kSoft = 2 * kRowsT;                 // threads of the softmax
-constexpr int kTurn = 128;                        // that turn codes into f16; then a multiplying warp and a copying one
-constexpr int kMulWarp = (kSoft + kTurn) / 32, kCopyWarp = kMulWarp + 1;
-constexpr int kThreads8 = kSoft + kTurn + 64;
+constexpr int kTurn = 128;                        // that turn codes into f16; then a multiplying warp for each tile and a copying one
+constexpr int kMulWarp = (kSoft + kTurn) / 32, kCopyWarp = kMulWarp + 2;
+constexpr int kThreads8 = kSoft + kTurn + 96;
 constexpr int kKeys = 64, kLogKeys = 6;           // keys per block
 constexpr int kStages = 3;                        // of K and of V in f16
 constexpr int kCopies = 2;                        // blocks of codes on their way
@@ -178,9 +178,9 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
     }
     for (int i = 0; i < kStages; ++i) {
       mbar_init(su32(&k_full[i]), 4);
-      mbar_init(su32(&k_empty[i]), 1);
+      mbar_init(su32(&k_empty[i]), 1 + two);
       mbar_init(su32(&v_full[i]), 4);
-      mbar_init(su32(&v_empty[i]), 1);
+      mbar_init(su32(&v_empty[i]), 1 + two);
     }
     for (int i = 0; i < kInfo; ++i) mbar_init(su32(&note_full[i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -273,51 +273,42 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         ahead = look(g + 2);
       }
     }
-    // ---- products
-    if (warp == kMulWarp) {
+    // ---- products, each tile's by a warp of its own, so that neither waits for the other's softmax
+    if (const int t = warp - kMulWarp; t < 1 + two) {
       const uint32_t leader = elect();
-      const uint32_t qa = desc_lo(su32(smem), 16), kb = desc_lo(su32(kbuf), 16), vb = desc_lo(su32(vbuf), CHUNK_KV);
+      const uint32_t qa = desc_lo(su32(smem) + t * S::Q, 16), kb = desc_lo(su32(kbuf), 16), vb = desc_lo(su32(vbuf), CHUNK_KV);
+      const uint32_t to = tmem + t * 128, scores_at = to + 256;
       auto scores = [&](int g) {
         const int st = g % kStages;
         hold(&k_full[st], g / kStages & 1);
         tm_fence_after();
         const uint32_t kd = kb + st * (S::KV >> 4);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (t && !two) break;
-#pragma unroll
-          for (int kk = 0; kk < DP / 16; ++kk)
-            mma_ss(tmem + 256 + t * 128 + (g & 1) * 64, qa + (t * S::Q + kk / 4 * CHUNK_Q + kk % 4 * 32 >> 4),
-                   kd + (kk / 4 * CHUNK_KV + kk % 4 * 32 >> 4), idesc<__half>(kRowsT, kKeys, false), kk > 0, leader);
-          commit(su32(&s_full[t][g & 1]), leader);
-        }
+        for (int kk = 0; kk < DP / 16; ++kk)
+          mma_ss(scores_at + (g & 1) * 64, qa + (kk / 4 * CHUNK_Q + kk % 4 * 32 >> 4), kd + (kk / 4 * CHUNK_KV + kk % 4 * 32 >> 4),
+                 idesc<__half>(kRowsT, kKeys, false), kk > 0, leader);
+        commit(su32(&s_full[t][g & 1]), leader);
         commit(su32(&k_empty[st]), leader);
       };
       // Products run in the order in which they are asked for, so the scores that go where a block's P was lie behind its product
       if (n > 0) {
-        hold(&q_full[0], 0);
-        if (two) hold(&q_full[1], 0);
+        hold(&q_full[t], 0);
         scores(0);
       }
       for (int g = 0; g < n; ++g) {
         if (g + 1 < n) scores(g + 1);
         const int st = g % kStages;
         hold(&v_full[st], g / kStages & 1);
+        hold(&p_full[t][g & 1], g >> 1 & 1);
+        tm_fence_after();
         const uint32_t vd = vb + st * (S::KV >> 4);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (t && !two) break;
-          hold(&p_full[t][g & 1], g >> 1 & 1);
-          tm_fence_after();
-#pragma unroll
-          for (int kk = 0; kk < kKeys / 16; ++kk)
-            mma_ts(tmem + t * 128, tmem + 256 + t * 128 + (g & 1) * 64 + kk * 8, vd + (kk * 2048 >> 4), idesc<__half>(kRowsT, DP, true),
-                   g > 0 || kk > 0, leader);
-          commit(su32(&pv_done[t]), leader);
-          if (g + 1 == n) commit(su32(&o_full[t]), leader);
-        }
+        for (int kk = 0; kk < kKeys / 16; ++kk)
+          mma_ts(to, scores_at + (g & 1) * 64 + kk * 8, vd + (kk * 2048 >> 4), idesc<__half>(kRowsT, DP, true), g > 0 || kk > 0, leader);
+        commit(su32(&pv_done[t]), leader);
         commit(su32(&v_empty[st]), leader);
       }
+      if (n > 0) commit(su32(&o_full[t]), leader);
     }
   } else if (warp >= kSoft / 32) {
     // ---- codes to f16: a warp has 16 keys of a block, a lane 16 codes of a row at a time, their halves apart: e is the one that
