@@ -58,7 +58,7 @@ namespace ppc {
 
 AttnSpace attn_space(int dtype, int D, int sms) {
   const int DP = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  const size_t ctas = (size_t)std::min(sms * (DP <= 128 ? 2 : 1), kMaxCtas);
+  const size_t ctas = (size_t)std::min(sms * (DP <= 128 ? 3 : 1), kMaxCtas);
   return {ctas * 3 * 4, ctas * 2 * (kRows * DP + 2 * kRows) * 4, tile_space(dtype, D, sms)};
 }
 

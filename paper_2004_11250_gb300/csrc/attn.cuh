@@ -12,7 +12,6 @@ namespace ppc_attn {
 using namespace ppc;
 using namespace ppc_ptx;
 
-constexpr int kPieces = 8;  // boxes down a tile at most (pages of 8)
 
 struct AttnParams {
   const void* q;

@@ -31,7 +31,7 @@ using namespace ppc_attn;
 
 constexpr int kRowsT = 128;                       // query rows of a tile
 constexpr int kSoft = 2 * kRowsT;                 // threads of the softmax
-constexpr int kTurn = 128;                        // that turn codes into f16; then a multiplying warp for each tile and a copying one
+constexpr int kTurn = 128;                        // that turn codes into f16, half of them keys, half values; then a multiplying warp for each tile and a copying one
 constexpr int kMulWarp = (kSoft + kTurn) / 32, kCopyWarp = kMulWarp + 2;
 constexpr int kThreads8 = kSoft + kTurn + 96;
 constexpr int kKeys = 64, kLogKeys = 6;           // keys per block
@@ -173,13 +173,13 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       }
       for (int j = 0; j < kCopies; ++j) {
         mbar_init(su32(&codes_full[i][j]), 1);
-        mbar_init(su32(&codes_empty[i][j]), 4);
+        mbar_init(su32(&codes_empty[i][j]), 2);
       }
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(su32(&k_full[i]), 4);
+      mbar_init(su32(&k_full[i]), 2);
       mbar_init(su32(&k_empty[i]), 1 + two);
-      mbar_init(su32(&v_full[i]), 4);
+      mbar_init(su32(&v_full[i]), 2);
       mbar_init(su32(&v_empty[i]), 1 + two);
     }
     for (int i = 0; i < kInfo; ++i) mbar_init(su32(&note_full[i]), 1);
@@ -311,12 +311,12 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       if (n > 0) commit(su32(&o_full[t]), leader);
     }
   } else if (warp >= kSoft / 32) {
-    // ---- codes to f16: a warp has 16 keys of a block, a lane 16 codes of a row at a time, their halves apart: e is the one that
+    // ---- codes to f16, two warps the keys' and two the values': a warp has 32 rows of a block, a lane 16 codes of a row at a time, their halves apart: e is the one that
     // it takes first, so that 16 lanes read from all banks, and the 8 lanes that write at once write to all (rows of 128 or 64)
-    constexpr int CPR = DP / 16, RPL = 32 / CPR, NI = 16 / RPL;  // chunks of 16 codes to a row, rows to a step, steps
-    const int w = warp - kSoft / 32, c = lane % CPR, r = lane / CPR, e = DP == 128 ? c >> 2 ^ r & 1 : r >> 1 & 1;
+    constexpr int CPR = DP / 16, RPL = 32 / CPR, NI = 32 / RPL;  // chunks of 16 codes to a row, rows to a step, steps
+    const int pool = warp / 2 & 1, w = warp % 2, c = lane % CPR, r = lane / CPR, e = DP == 128 ? c >> 2 ^ r & 1 : r >> 1 & 1;
     const bool in = c * 16 < p.D;
-    const int key0 = w * 16 + r, from = key0 * p.D + c * 16 + e * 8, other = 8 - 16 * e;
+    const int key0 = w * 32 + r, from = key0 * p.D + c * 16 + e * 8, other = 8 - 16 * e;
     // where the halves go: rows 4 on of 8 are swizzled by 4 more chunks
     const int to0 = c / 4 * CHUNK_KV + key0 * 128;
     const int at0 = to0 + ((c % 4 * 2 + e ^ key0 & 7) << 4), at1 = to0 + ((c % 4 * 2 + 1 - e ^ key0 & 7) << 4);
@@ -338,19 +338,15 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     };
+    uint64_t *const full = pool ? v_full : k_full, *const empty = pool ? v_empty : k_empty;
+    unsigned char* const buf = pool ? vbuf : kbuf;
     for (int g = 0; g < n; ++g) {
       const int st = g % kStages, at = g % kCopies;
-      const uint32_t ph = (g / kStages + 1) & 1, pc = g / kCopies & 1;
-      hold(&codes_full[0][at], pc);
-      hold(&k_empty[st], ph);
-      turn(kbuf + st * S::KV, codes + at * S::CODES);
-      warp_arrive(&k_full[st]);
-      if (lane == 0) mbar_arrive(su32(&codes_empty[0][at]));
-      hold(&codes_full[1][at], pc);
-      hold(&v_empty[st], ph);
-      turn(vbuf + st * S::KV, codes + (kCopies + at) * S::CODES);
-      warp_arrive(&v_full[st]);
-      if (lane == 0) mbar_arrive(su32(&codes_empty[1][at]));
+      hold(&codes_full[pool][at], g / kCopies & 1);
+      hold(&empty[st], (g / kStages + 1) & 1);
+      turn(buf + st * S::KV, codes + (pool * kCopies + at) * S::CODES);
+      warp_arrive(&full[st]);
+      if (lane == 0) mbar_arrive(su32(&codes_empty[pool][at]));
     }
   } else {
     // ---- queries, then the softmax, a thread per row

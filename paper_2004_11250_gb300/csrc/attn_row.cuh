@@ -48,12 +48,13 @@ using namespace ppc_ptx;
 using namespace ppc_attn;
 
 constexpr int kRows = 16;      // query rows of a unit at most
-constexpr int kWarps = 4;      // that compute; one more copies
-constexpr int kThreads = kWarps * 32 + 32;
 constexpr int kUp = 15;        // f16 weights are up to 2^15 (a warp's m is never behind its keys)
 constexpr int kGroup = 16;     // parts of a unit joined at once
 constexpr int kMaxCtas = 512;  // kGroup^2 parts and more
 constexpr int kJoin = kMaxCtas / kGroup;
+constexpr float kUp8 = 12.f;      // over codes, weights are up to 2^12 when m is set, and stay
+constexpr float kMost8 = 32768.f; // up to this with it
+constexpr float kNone = -3e38f;   // m before there is one: any weight from it is too large
 
 // Cell: what the cache holds, T or codes of 8 bits
 template <class T, class Cell, int DP, int RB>
@@ -64,28 +65,32 @@ struct Shape {
   static constexpr int NT = EIGHT && sizeof(T) == 4 ? 3 : 1;  // f16 parts of a query
   static constexpr int R = MM ? 8 * RB : RB;    // query rows of a unit
   static constexpr int TK = EIGHT ? kTileKeys8 : MM ? 64 : 32;  // keys per tile
-  static constexpr int LOG_TK = TK == 64 ? 6 : 5;
-  static constexpr int KW = TK / kWarps;        // keys per warp
+  static constexpr int LOG_TK = TK == 128 ? 7 : TK == 64 ? 6 : 5;
+  static constexpr int WARPS = 4;               // that compute; one more copies
+  static constexpr int THREADS = WARPS * 32 + 32;
+  static constexpr int KW = TK / WARPS;         // keys per warp
+  static constexpr int PIECES = TK / 8;         // boxes down a tile at most (pages of 8)
   static constexpr int COL = E * DP < 128 ? 64 : 128;  // bytes of a column
   static constexpr int CH = COL / E;            // values of it
   static constexpr int NCH = DP / CH;
   static constexpr int TILE = TK * DP * E;      // bytes of a K or V tile
-  static constexpr int CTAS = DP <= 128 ? 2 : 1;
+  static constexpr int CTAS = EIGHT && RB == 1 && NT == 1 && DP <= 128 ? 3 : DP <= 128 ? 2 : 1;
   static constexpr int QS = MM ? 0 : R * DP * 4;  // fp32 queries stay in shared memory
   static constexpr int AS = DP + 4;             // row stride of the joining buffers, free of bank conflicts
-  static constexpr int NB = R <= 8 ? 2 : 1;     // joining buffers
+  static constexpr int NB = R <= 8 && CTAS < 3 ? 2 : 1;  // joining buffers
   static constexpr int ACC = NB * R * AS * 4;
   // as many stages as fit: with 228 KB per SM, 1 KB of it taken and 6 KB static per CTA, 190 KB are in flight (16 bits)
-  static constexpr int STAGES = (233472 / CTAS - 1024 - 6144 - 1024 - ACC - QS) / (2 * TILE);
+  static constexpr int STAGES = (233472 / CTAS - 1024 - (EIGHT ? 4096 : 6144) - 1024 - ACC - QS) / (2 * TILE);
   static constexpr int SMEM = STAGES * 2 * TILE + ACC + QS + 1024;
   static constexpr int PART = kRows * DP + 2 * kRows;  // floats of a partial result
   static_assert(!MM || NT * R * (DP + 8) * 2 <= ACC, "queries pass through the joining buffers");
 };
 
+template <int PIECES>
 struct Stage {          // what the producer says of a tile
-  int have[kPieces];    // keys of each piece that the call may use
+  int have[PIECES];     // keys of each piece that the call may use
   int full;             // all of them
-  float ks[kPieces], vs[kPieces];  // their scales, of codes
+  float ks[PIECES], vs[PIECES];  // their scales, of codes
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t a, uint32_t (&r)[4]) {
@@ -201,20 +206,20 @@ __device__ __forceinline__ void load_item(const AttnParams& p, int TK, int R, in
 }
 
 template <class T, class Cell, int DP, int RB, bool WIN>
-__global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
+__global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell, DP, RB>::CTAS)
     attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv) {
   using S = Shape<T, Cell, DP, RB>;
   using W = std::conditional_t<S::EIGHT, __half, T>;  // of the weights
-  constexpr int TK = S::TK, KW = S::KW, ST = S::STAGES, R = S::R;
+  constexpr int TK = S::TK, KW = S::KW, ST = S::STAGES, R = S::R, kWarps = S::WARPS, kThreads = S::THREADS;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* acc = reinterpret_cast<float*>(smem + ST * 2 * S::TILE);
   [[maybe_unused]] float* qs = acc + S::NB * R * S::AS;
   __shared__ alignas(8) uint64_t full_bar[ST], empty_bar[ST];
-  __shared__ Stage stage[ST];
+  __shared__ Stage<S::PIECES> stage[ST];
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], rm[kRows], rl[kRows];
-  __shared__ float wts[kRows][kJoin + 1], sums[kRows][kJoin + 1];
+  __shared__ float wts[R][kJoin + 1], sums[R][kJoin + 1];
   __shared__ int scan[4][kThreads / 32], last_flag, dead;
   // keys with values that are not finite, a bit each: 16 from lim_min on, and 16 from the first row's window on
   __shared__ unsigned unfit;
@@ -273,10 +278,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
     if (tid == 0) atomicOr(p.status, PP_CACHE_BAD_LENGTH);
     return;
   }
-  // Equal runs; one of a single tile would spend more on joining than on its keys.  Where every unit can have CTAs of its
+  // Equal runs; one of a single tile (but of 128 keys) would spend more on joining than on its keys.  Where every unit can have CTAs of its
   // own with runs not much longer (up to 1.4 times, which the copies of the other CTAs make up for), runs end with
   // their unit: a CTA that changes units waits some 3 us for queries, joining and stores.
-  int run = max((all[0] + grid - 1) / grid, 2), whole = 0;
+  int run = max((all[0] + grid - 1) / grid, TK == 128 ? 1 : 2), whole = 0;
   if (all[1] <= grid) {
     const int longer[4] = {run, run + run / 10 + 1, run + run / 4 + 1, run + run * 2 / 5 + 2};
     int ctas[4] = {};
@@ -610,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
     float m[NR], l[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      m[r] = -INFINITY;
+      m[r] = S::EIGHT ? kNone : -INFINITY;
       l[r] = 0.f;
     }
 
@@ -619,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
       __syncwarp();
       timed_out = timed_out || *(volatile int*)&dead;
       const uint32_t kt = su32(smem + s * 2 * S::TILE), vt = kt + S::TILE;
-      const Stage& sg = stage[s];
+      const Stage<S::PIECES>& sg = stage[s];
       const int from = (WIN && k >= w.st ? k + gap : k) * TK;  // the tile's first key
       const bool clean = sg.full && (listed || (from + TK <= lim_min && (!WIN || from >= lim_max - p.window || from + TK <= p.sinks)));
       // a key of the tile that row r of the lane's may not use; keys whose values have to be 0, as no row uses them
@@ -657,7 +662,132 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
         m[r] = mx;
         return at;
       };
-      if constexpr (S::MM) {
+      if constexpr (S::EIGHT) {
+        // ---- scores of this warp's keys, 16 at a time: sc[.][rb] is keys g (0, 1) and g + 8 (2, 3) by the lane's two rows
+        constexpr int SL = KW / 16;
+        float sc[SL][RB][4] = {}, x[SL][RB][4];
+        float ks[SL][2], vs[SL][2];  // scales of keys g and g + 8
+#pragma unroll
+        for (int z = 0; z < SL; ++z) {
+          const int slab = warp * KW + 16 * z, key = slab + lane % 16;
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; kk += 2) {  // 16 values of a key are a chunk of 16 bytes: two at a time
+            uint32_t c[4], a[4];
+            ldsm4(kt + place8<S>(key, kk + lane / 16), c);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              f16_in_order(c[2 * i], a[0], a[2]);
+              f16_in_order(c[2 * i + 1], a[1], a[3]);
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int n = S::NT - 1; n >= 0; --n) mma16<W>(sc[z][rb], a, qf[n][rb][kk + i][0], qf[n][rb][kk + i][1]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            ks[z][i] = sg.ks[slab + 8 * i >> log_br];
+            vs[z][i] = sg.vs[slab + 8 * i >> log_br];
+          }
+        }
+        auto masked = [&](int z, int rb, int e) { return !clean && hidden(warp * KW + 16 * z + g + 8 * (e >> 1), 2 * rb + (e & 1)); };
+        // ---- softmax over what this warp has seen: with m as it is, and only where a weight would leave f16 once more with the
+        // scores' maximum looked for and m 2^12 below it (each step rounded by itself there, as the maximum's are)
+        float top = 0.f;
+#pragma unroll
+        for (int z = 0; z < SL; ++z)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = 2 * rb + (e & 1);
+              float y = fmaf(sc[z][rb][e], ks[z][e >> 1] * slr[r], -m[r]);
+              if (masked(z, rb, e)) y = -INFINITY;
+              x[z][rb][e] = ex2(y);
+              top = fmaxf(top, x[z][rb][e]);
+            }
+        if (__any_sync(~0u, top > kMost8)) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int z = 0; z < SL; ++z)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                float& y = sc[z][r >> 1][2 * i + (r & 1)];
+                y = masked(z, r >> 1, 2 * i + (r & 1)) ? -INFINITY : __fmul_rn(__fmul_rn(y, ks[z][i]), slr[r]);
+                mx = fmaxf(mx, y);
+              }
+            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+            const float to = fmaxf(m[r], lower(mx, kUp8)), f = ex2(m[r] - to);
+            m[r] = to;
+            l[r] *= f;
+#pragma unroll
+            for (int z = 0; z < SL; ++z)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) x[z][r >> 1][2 * i + (r & 1)] = ex2(__fadd_rn(sc[z][r >> 1][2 * i + (r & 1)], -to));
+#pragma unroll
+            for (int i = 0; i < NO; ++i) {
+              o[r >> 1][i][r & 1] *= f;
+              o[r >> 1][i][2 + (r & 1)] *= f;
+            }
+          }
+        }
+        // ---- their product with V.  A weight as two halves in f16, the first rounded down, so that it keeps 21 bits (some 2^-24 of
+        // up to 2^15 at the least); of several pages' scales the largest, and the others' weights less
+        float vmax = 0.f;
+#pragma unroll
+        for (int z = 0; z < SL; ++z) vmax = fmaxf(vmax, fmaxf(vs[z][0], vs[z][1]));
+        const bool differ = 8 << log_br - 3 < KW && vmax > 0.f;
+        uint32_t bh[SL][RB][2], bl[SL][RB][2];
+#pragma unroll
+        for (int z = 0; z < SL; ++z)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float a = x[z][rb][2 * i], b = x[z][rb][2 * i + 1];
+              l[2 * rb] += a;
+              l[2 * rb + 1] += b;
+              if (differ) {
+                a *= vs[z][i] / vmax;
+                b *= vs[z][i] / vmax;
+              }
+              const uint32_t hi = pack_down<W>(a, b);
+              Vec<W, 2> two;
+              memcpy(&two, &hi, 4);
+              const float2 back = get2(two, 0);
+              bh[z][rb][i] = transpose8(hi);  // keys x rows to rows x keys
+              bl[z][rb][i] = transpose8(pack<W>(a - back.x, b - back.y));
+            }
+#pragma unroll
+        for (int i0 = 0; i0 < NO; i0 += 2) {
+          float sum[2][RB][4] = {};
+#pragma unroll
+          for (int z = 0; z < SL; ++z) {
+            uint32_t c[4], a[4];
+            ldsm4t(vt + place8<S>(warp * KW + 16 * z + lane % 16, i0 + lane / 16), c);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              f16_by_parity(c[2 * i], a[0], a[1]);
+              f16_by_parity(c[2 * i + 1], a[2], a[3]);
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb) {
+                mma16<W>(sum[i][rb], a, bl[z][rb][0], bl[z][rb][1]);
+                mma16<W>(sum[i][rb], a, bh[z][rb][0], bh[z][rb][1]);
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[rb][i0 + i][e] = fmaf(sum[i][rb][e], vmax, o[rb][i0 + i][e]);
+        }
+      } else if constexpr (S::MM) {
         // ---- scores of this warp's keys: sc[rb] is keys g (0, 1) and g + 8 (2, 3) by the lane's two rows
         float sc[RB][4], odd[RB][4];  // every other step apart: two chains of products instead of one
 #pragma unroll
@@ -666,45 +796,19 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
           for (int e = 0; e < 4; ++e) sc[rb][e] = odd[rb][e] = 0.f;
         {
           const int key = warp * KW + lane % 16;
-          if constexpr (S::EIGHT) {
-#pragma unroll
-            for (int kk = 0; kk < DP / 16; kk += 2) {  // 16 values of a key are a chunk of 16 bytes: two at a time
-              uint32_t c[4], a[4];
-              ldsm4(kt + place8<S>(key, kk + lane / 16), c);
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                f16_in_order(c[2 * i], a[0], a[2]);
-                f16_in_order(c[2 * i + 1], a[1], a[3]);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                  for (int n = S::NT - 1; n >= 0; --n) mma16<W>(i ? odd[rb] : sc[rb], a, qf[n][rb][kk + i][0], qf[n][rb][kk + i][1]);
-              }
-            }
-          } else {
 #pragma unroll
           for (int kk = 0; kk < DP / 16; ++kk) {
             uint32_t a[4];
             ldsm4(kt + kk / 4 * TK * 128 + key * 128 + ((((kk % 4) * 2 + lane / 16) ^ (key & 7)) << 4), a);
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) mma16<W>(kk % 2 ? odd[rb] : sc[rb], a, qf[0][rb][kk][0], qf[0][rb][kk][1]);
-          }
-          }
-        }
-        [[maybe_unused]] float ks[2], vs[2];  // scales of keys g and g + 8
-        if constexpr (S::EIGHT) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            ks[i] = sg.ks[warp * KW + 8 * i >> log_br];
-            vs[i] = sg.vs[warp * KW + 8 * i >> log_br];
+            for (int rb = 0; rb < RB; ++rb) mma16<T>(kk % 2 ? odd[rb] : sc[rb], a, qf[0][rb][kk][0], qf[0][rb][kk][1]);
           }
         }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if constexpr (S::EIGHT) sc[rb][e] = __fmul_rn(__fmul_rn(sc[rb][e] + odd[rb][e], ks[e >> 1]), slr[2 * rb + (e & 1)]);
-            else sc[rb][e] = __fmul_rn(sc[rb][e] + odd[rb][e], sl);
+            sc[rb][e] = __fmul_rn(sc[rb][e] + odd[rb][e], sl);
             if (!clean && hidden(warp * KW + g + 8 * (e >> 1), 2 * rb + (e & 1))) sc[rb][e] = -INFINITY;
           }
         // ---- softmax over what this warp has seen
@@ -733,50 +837,18 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
         // and the output's own rounding stays the largest error.  The first half is rounded down and the second above 0, so
         // that neither is 0 or negative beside an infinite value
         uint32_t bh[RB][2], bl[RB][2];
-        [[maybe_unused]] float vmax = 0.f;
-        if constexpr (S::EIGHT) {  // of two pages' scales the larger, and the other's weights less
-          vmax = fmaxf(vs[0], vs[1]);
-          if (log_br == 3 && vs[0] != vs[1]) {
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) sc[rb][e] *= vs[e >> 1] / vmax;
-          }
-        }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const float a = sc[rb][2 * i], b = sc[rb][2 * i + 1];
-            const uint32_t hi = pack_down<W>(a, b);
-            Vec<W, 2> two;
+            const uint32_t hi = pack_down<T>(a, b);
+            Vec<T, 2> two;
             memcpy(&two, &hi, 4);
             const float2 back = get2(two, 0);
             bh[rb][i] = transpose8(hi);  // keys x rows to rows x keys
-            if constexpr (S::EIGHT) bl[rb][i] = transpose8(pack<W>(a - back.x, b - back.y));  // codes are finite
-            else bl[rb][i] = transpose8(pack<W>(a > 0.f ? fmaxf(a - back.x, kLeast<W>) : 0.f, b > 0.f ? fmaxf(b - back.y, kLeast<W>) : 0.f));
+            bl[rb][i] = transpose8(pack<T>(a > 0.f ? fmaxf(a - back.x, kLeast<T>) : 0.f, b > 0.f ? fmaxf(b - back.y, kLeast<T>) : 0.f));
           }
-        if constexpr (S::EIGHT) {
-          const int key = warp * KW + lane % 16;
-#pragma unroll
-          for (int i0 = 0; i0 < NO; i0 += 2) {
-            uint32_t c[4], a[4];
-            ldsm4t(vt + place8<S>(key, i0 + lane / 16), c);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              f16_by_parity(c[2 * i], a[0], a[1]);
-              f16_by_parity(c[2 * i + 1], a[2], a[3]);
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb) {
-                float sum[4] = {};
-                mma16<W>(sum, a, bl[rb][0], bl[rb][1]);
-                mma16<W>(sum, a, bh[rb][0], bh[rb][1]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[rb][i0 + i][e] = fmaf(sum[e], vmax, o[rb][i0 + i][e]);
-              }
-            }
-          }
-        } else {
         const int key = warp * KW + (lane / 16) * 8 + lane % 8;
 #pragma unroll
         for (int i = 0; i < NO; ++i) {
@@ -784,10 +856,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
           ldsm4t(vt + i / 4 * TK * 128 + key * 128 + (((i % 4 * 2 + (lane / 8 & 1)) ^ (key & 7)) << 4), a);
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
-            mma16<W>(o[rb][i], a, bl[rb][0], bl[rb][1]);
-            mma16<W>(o[rb][i], a, bh[rb][0], bh[rb][1]);
+            mma16<T>(o[rb][i], a, bl[rb][0], bl[rb][1]);
+            mma16<T>(o[rb][i], a, bh[rb][0], bh[rb][1]);
           }
-        }
         }
       } else {
         // ---- scores: lane (g, t) has a quarter of key g, 16 bytes at a time.  Which ones goes by where they lie: of each
@@ -867,6 +938,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, Cell, DP, RB>::CTAS)
       l[r] += __shfl_xor_sync(~0u, l[r], 4);
       l[r] += __shfl_xor_sync(~0u, l[r], 8);
       l[r] += __shfl_xor_sync(~0u, l[r], 16);
+      if (S::EIGHT && l[r] == 0.f) m[r] = -INFINITY;
       if (S::MM ? g == 0 : lane == 0) {
         wm[warp][row_of(r)] = m[r];
         wl[warp][row_of(r)] = l[r];
@@ -1070,7 +1142,7 @@ cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t
   const int64_t deep = ((int64_t)(p.sel ? std::min(p.width, p.keep) : p.width) * p.page + TK - 1) / TK;
   if (units >= INT32_MAX / deep) return cudaErrorNotSupported;
   const int grid = std::min(sms * S::CTAS, kMaxCtas);
-  return launch_after(attn_kernel<T, Cell, DP, RB, WIN>, dim3(grid), kThreads, S::SMEM, stream, 1, p, c.mk, c.mv);
+  return launch_after(attn_kernel<T, Cell, DP, RB, WIN>, dim3(grid), S::THREADS, S::SMEM, stream, 1, p, c.mk, c.mv);
 }
 
 // Units of as many rows as a sequence (or, with selected pages, a token) has, up to 8 or 16; in fp32 up to 8.

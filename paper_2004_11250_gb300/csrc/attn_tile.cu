@@ -44,6 +44,7 @@ constexpr int kRowsT = 128;            // query rows of a tile
 constexpr int kSoft = 128;             // threads of the softmax; then a copying and a multiplying warp
 constexpr int kThreadsT = kSoft + 64;
 constexpr int kKeys = 64;              // keys per block
+constexpr int kPieces = kKeys / 8;     // boxes down a block at most (pages of 8)
 constexpr int kStages = 2;             // of K and of V
 constexpr int kEnds = 3;               // blocks with keys that some tokens of a tile see and others do not, at most: 127 keys
                                        // (with a window as many again, where the tokens' windows begin)

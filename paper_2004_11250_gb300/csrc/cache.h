@@ -39,7 +39,7 @@ namespace ppc {
 
 // The row kernel's keys per tile (attn.cu): 64 rows of 16-bit values, 32 of fp32.
 inline int tile_keys(int dtype) { return dtype == PP_F32 ? 32 : 64; }
-constexpr int kTileKeys8 = 64;  // over codes of 8 bits
+constexpr int kTileKeys8 = 128;  // over codes of 8 bits
 // Device bytes that attention needs beside the status word: counters, partial results, shares of tiles.
 struct AttnSpace {
   size_t counters, partial, tiles;
