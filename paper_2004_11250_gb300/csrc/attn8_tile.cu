@@ -234,8 +234,8 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         cell = there ? (int64_t)id * p.H + h : -1;
         ks = vs = 0.f;
         if (there) {
-          ks = __ldg(p.ks + cell);
-          vs = __ldg(p.vs + cell);
+          ks = p.ks[cell];
+          vs = p.vs[cell];
         }
       };
       int ahead = look(1);
