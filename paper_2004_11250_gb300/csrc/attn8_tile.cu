@@ -615,14 +615,28 @@ cudaError_t launch(const AttnParams& p, int64_t grid, cudaStream_t stream) {
 // Pairs of tiles of a call at most: each sequence adds at most one that is not full.
 int64_t most_pairs(const AttnParams& p) { return ((int64_t)p.T / (2 * (kRowsT / p.G.d)) + std::min(p.T, p.B)) * p.H; }
 
+// Few tiles are split along their blocks, up to one CTA per SM, while a share can have 4 blocks; the shares' sums have room for
+// two tiles per SM.
+int64_t splits_of(const AttnParams& p, int sms) {
+  const int TT = 2 * (kRowsT / p.G.d);
+  const int64_t cells = (int64_t)p.T * p.H * p.G.d, room = (int64_t)2 * sms * kRowsT;
+  const int64_t keys = std::min<int64_t>((int64_t)p.width * p.page, (int64_t)p.window + p.sinks + TT + 2 * kKeys);
+  return std::max<int64_t>(1, std::min({(int64_t)kSplits, sms / most_pairs(p), keys / kKeys / 4, room / cells}));
+}
+
 }  // namespace
 
 namespace ppc_attn {
 
 bool tile8_applicable(const AttnParams& p, int dtype, int sms) {
   if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
-  const int64_t few = 2 * sms / kSplits, pairs = most_pairs(p), units = ((int64_t)p.T * p.G.d + 15) / 16 * p.H;
-  return few < units && pairs * 8 <= units * 9;
+  // By what 64 keys of every sequence take.  The row kernel has three CTAs per SM, each of which meets them with 8 rows in about
+  // 0.95 us; a CTA here meets them with a tile in as much, with two in 1.5 times that, and the CTAs come in rounds.  32 heads of
+  // 128 over 8, bf16, rows and tiles: 16 rows of each of 32 sequences of up to 8192 keys 168 and 197 us, 32 rows 324 and 197; 20
+  // rows of one of 30000 43 and 70, 64 rows of one of 32768 95 and 76, 1024 rows 1144 and 227.
+  const int64_t units = ((int64_t)p.T * p.G.d + 7) / 8 * p.H, pairs = most_pairs(p), s = splits_of(p, sms);
+  const bool two = (int64_t)p.T * p.G.d > (int64_t)kRowsT * p.B;
+  return units * s * 2 > 3 * (int64_t)sms * ((pairs * s + sms - 1) / sms) * (two ? 3 : 2);
 }
 
 cudaError_t tile8_prepare() {
@@ -634,14 +648,9 @@ cudaError_t tile8_prepare() {
 }
 
 cudaError_t tile8_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t stream) {
-  const int TT = 2 * (kRowsT / p.G.d), DP = p.D <= 64 ? 64 : 128;
-  const int64_t pairs = most_pairs(p);  // CTAs beyond the last tile leave
-  // Few tiles are split along their blocks, up to one CTA per SM, while a share can have 4 blocks; the shares' sums have room for
-  // two tiles per SM.
-  const int64_t cells = (int64_t)p.T * p.H * p.G.d, room = (int64_t)2 * sms * kRowsT;
-  const int64_t keys = std::min<int64_t>((int64_t)p.width * p.page, (int64_t)p.window + p.sinks + TT + 2 * kKeys);
-  const int64_t splits = std::min({(int64_t)kSplits, sms / pairs, keys / kKeys / 4, room / cells});
-  p.splits = (int)std::max<int64_t>(1, splits);
+  const int DP = p.D <= 64 ? 64 : 128;
+  const int64_t pairs = most_pairs(p), room = (int64_t)2 * sms * kRowsT;  // CTAs beyond the last tile leave
+  p.splits = (int)splits_of(p, sms);
   p.split_sums = c.tiles;
   p.split_stats = reinterpret_cast<float2*>(c.tiles + room * DP);
   const int64_t grid = pairs * p.splits;

@@ -1145,14 +1145,14 @@ cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t
   return launch_after(attn_kernel<T, Cell, DP, RB, WIN>, dim3(grid), S::THREADS, S::SMEM, stream, 1, p, c.mk, c.mv);
 }
 
-// Units of as many rows as a sequence (or, with selected pages, a token) has, up to 8 or 16; in fp32 up to 8.
+// Units of as many rows as a sequence (or, with selected pages, a token) has, up to 8 or 16; in fp32 and over codes up to 8.
 template <class T, class Cell, int DP, bool WIN>
 cudaError_t by_rows(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t stream) {
   const int64_t rows = p.sel || !p.starts ? p.G.d : ((int64_t)p.T * p.G.d + p.B - 1) / p.B;
-  if constexpr (sizeof(T) == 2) {
-    return rows <= 8 ? launch<T, Cell, DP, 1, WIN>(p, c, sms, stream) : launch<T, Cell, DP, 2, WIN>(p, c, sms, stream);
-  } else if constexpr (sizeof(Cell) == 1) {
+  if constexpr (sizeof(Cell) == 1) {
     return launch<T, Cell, DP, 1, WIN>(p, c, sms, stream);
+  } else if constexpr (sizeof(T) == 2) {
+    return rows <= 8 ? launch<T, Cell, DP, 1, WIN>(p, c, sms, stream) : launch<T, Cell, DP, 2, WIN>(p, c, sms, stream);
   } else {
     return rows <= 2   ? launch<T, Cell, DP, 2, WIN>(p, c, sms, stream)
            : rows <= 4 ? launch<T, Cell, DP, 4, WIN>(p, c, sms, stream)
@@ -1178,11 +1178,11 @@ cudaError_t prepare_rows() {
 template <class T, class Cell, bool WIN>
 cudaError_t prepare_type() {
   cudaError_t e;
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(Cell) == 1) {
+    e = prepare_rows<T, Cell, 1, WIN>();
+  } else if constexpr (sizeof(T) == 2) {
     e = prepare_rows<T, Cell, 1, WIN>();
     if (e == cudaSuccess) e = prepare_rows<T, Cell, 2, WIN>();
-  } else if constexpr (sizeof(Cell) == 1) {
-    e = prepare_rows<T, Cell, 1, WIN>();
   } else {
     e = prepare_rows<T, Cell, 2, WIN>();
     if (e == cudaSuccess) e = prepare_rows<T, Cell, 4, WIN>();
