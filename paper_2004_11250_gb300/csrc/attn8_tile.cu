@@ -15,7 +15,7 @@
 // before the softmax of the one before is done (two S buffers).  Codes are finite, so a key that a row does not see adds 0
 // whatever it holds.
 //
-// m stays as it is while the weights fit f16 (they are up to 2^12 when it is set): a block is
+// m stays as it is while the weights fit f16 (they are up to 2^8 when it is set): a block is
 // computed with the last one's m, and only where some 8 weights' sum, which the row's total wants
 // anyway, says that one might not fit, once more, with m raised and the sums so far made smaller.
 // So most blocks read S once, and neither wait for nor look for a maximum.
@@ -40,8 +40,8 @@ constexpr int kCopies = 2;                        // blocks of codes on their wa
 constexpr int kInfo = 8;                          // blocks whose notes are kept: those of block g are written when K of g - 2 has been, after the
                                                   // scores of g - 5, which were asked for when the softmax had done with g - 7
 constexpr int kSplits = 8;                        // shares of a tile's blocks at most
-constexpr int kUp = 12;                           // weights are up to 2^12 when m is set
-constexpr float kMost = 65504.f;                  // 8 weights' sum at most: f16's largest number, and twice what they can be then
+constexpr int kUp = 8;                            // weights are up to 2^8 when m is set
+constexpr float kMost = 65504.f;                  // 8 weights' sum at most: f16's largest number
 constexpr float kLeastScale = -42.f;              // log2 of vs at the least: 2^16 times it is 0 in f16
 
 template <int DP>
