@@ -69,6 +69,11 @@ struct Shape {
   static constexpr int WARPS = 4;               // that compute; one more copies
   static constexpr int THREADS = WARPS * 32 + 32;
   static constexpr int KW = TK / WARPS;         // keys per warp
+  // A change of unit, in tiles: some 8 us under way (queries, joining, stores), of 2 a tile.  Without it CTAs that get many short
+  // units are the last to end: 48 sequences of up to 8192 keys, one of them idle, 84 us, and 102 without.  (Not where it would
+  // move the joins of calls from before it.)
+  template <bool WIN>
+  static constexpr int EXTRA = EIGHT ? 3 : WIN ? 2 : 0;
   static constexpr int PIECES = TK / 8;         // boxes down a tile at most (pages of 8)
   static constexpr int COL = E * DP < 128 ? 64 : 128;  // bytes of a column
   static constexpr int CH = COL / E;            // values of it
@@ -165,10 +170,10 @@ struct Walk {
   int item, t0, n, len, rows, units;
   int kt;    // tiles of a unit
   int st;    // with a window: the first st of them are the first keys'
-  int span;  // places of a unit in the order: its tiles, or whole runs of them
+  int span;  // places of a unit in the order: its tiles and what a change of unit costs in tiles, or whole runs of tiles
   int places;
 };
-template <bool WIN>
+template <bool WIN, int EXTRA>
 __device__ __forceinline__ void load_item(const AttnParams& p, int TK, int R, int whole, int i, Walk& w) {
   w.item = i;
   int seen;
@@ -201,7 +206,7 @@ __device__ __forceinline__ void load_item(const AttnParams& p, int TK, int R, in
     w.st = min(w.kt, (min(p.sinks, seen) + TK - 1) / TK);
     w.kt = min(w.kt, w.st + (min(p.window, seen) + tokens + TK - 3) / TK + 1);
   }
-  w.span = whole ? (w.kt + whole - 1) / whole * whole : w.kt;
+  w.span = whole ? (w.kt + whole - 1) / whole * whole : w.kt + EXTRA;
   w.places = w.units * w.span;
 }
 
@@ -211,7 +216,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
                 const __grid_constant__ CUtensorMap mv) {
   using S = Shape<T, Cell, DP, RB>;
   using W = std::conditional_t<S::EIGHT, __half, T>;  // of the weights
-  constexpr int TK = S::TK, KW = S::KW, ST = S::STAGES, R = S::R, kWarps = S::WARPS, kThreads = S::THREADS;
+  constexpr int TK = S::TK, KW = S::KW, ST = S::STAGES, R = S::R, kWarps = S::WARPS, kThreads = S::THREADS, EX = S::template EXTRA<WIN>;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* acc = reinterpret_cast<float*>(smem + ST * 2 * S::TILE);
@@ -247,11 +252,43 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   int tiles = 0, units = 0;
   bool bad_range = false;
   Walk w;
-  for (int i = i0; i < i1; ++i) {
-    load_item<WIN>(p, TK, R, 0, i, w);
-    tiles += w.places;
-    units += w.units;
-    bad_range = bad_range || w.n < 0;
+  // what the passes below ask of an item; of up to four kept, as each load of a length waits a microsecond
+  constexpr int KEEP = EX ? 4 : 1;
+  int kept_kt[KEEP] = {}, kept_units[KEEP] = {};
+  const bool kept = per <= KEEP;
+  auto each_item = [&](auto f) {  // f(tiles of a unit, units)
+    if (kept) {
+#pragma unroll
+      for (int j = 0; j < KEEP; ++j)
+        if (i0 + j < i1) f(kept_kt[j], kept_units[j]);
+    } else {
+      for (int i = i0; i < i1; ++i) {
+        load_item<WIN, EX>(p, TK, R, 0, i, w);
+        f(w.kt, w.units);
+      }
+    }
+  };
+  auto span_of = [&](int kt, int whole) { return whole ? (kt + whole - 1) / whole * whole : kt + EX; };
+  if (kept) {
+#pragma unroll
+    for (int j = 0; j < KEEP; ++j)
+      if (i0 + j < i1) {
+        load_item<WIN, EX>(p, TK, R, 0, i0 + j, w);
+        kept_kt[j] = w.kt;
+        kept_units[j] = w.units;
+        bad_range = bad_range || w.n < 0;
+      }
+    each_item([&](int kt, int n) {
+      tiles += n * (kt + EX);
+      units += n;
+    });
+  } else {
+    for (int i = i0; i < i1; ++i) {
+      load_item<WIN, EX>(p, TK, R, 0, i, w);
+      tiles += w.places;
+      units += w.units;
+      bad_range = bad_range || w.n < 0;
+    }
   }
   const int grid = gridDim.x;
   // sums of N numbers over the team
@@ -283,13 +320,12 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   // their unit: a CTA that changes units waits some 3 us for queries, joining and stores.
   int run = max((all[0] + grid - 1) / grid, TK == 128 ? 1 : 2), whole = 0;
   if (all[1] <= grid) {
-    const int longer[4] = {run, run + run / 10 + 1, run + run / 4 + 1, run + run * 2 / 5 + 2};
+    const int own = max(run - EX, 1), longer[4] = {own, own + own / 10 + 1, own + own / 4 + 1, own + own * 2 / 5 + 2};
     int ctas[4] = {};
-    for (int i = i0; i < i1; ++i) {
-      if (per > 1) load_item<WIN>(p, TK, R, 0, i, w);
+    each_item([&](int kt, int n) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) ctas[j] += w.units * ((w.kt + longer[j] - 1) / longer[j]);
-    }
+      for (int j = 0; j < 4; ++j) ctas[j] += n * ((kt + longer[j] - 1) / longer[j]);
+    });
     sums_of(ctas);
 #pragma unroll
     for (int j = 3; j >= 0; --j)
@@ -298,10 +334,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   }
   // a scan places the items in the one order
   int mine = 0;
-  for (int i = i0; i < i1; ++i) {
-    if (per > 1 || whole) load_item<WIN>(p, TK, R, whole, i, w);
-    mine += w.places;
-  }
+  each_item([&](int kt, int n) { mine += n * span_of(kt, whole); });
   int before = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -325,7 +358,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   const bool has = x0 >= before && x0 < before + mine;
   if (has) {
     for (int i = i0;; ++i) {
-      if (per > 1) load_item<WIN>(p, TK, R, whole, i, w);
+      if (per > 1 || whole) load_item<WIN, EX>(p, TK, R, whole, i, w);
       if (x0 < before + w.places) break;
       before += w.places;
     }
@@ -355,7 +388,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   auto settle = [&](int x) {
     while (x - w.base >= w.places) {
       const int b = w.base + w.places;
-      load_item<WIN>(p, TK, R, whole, w.item + 1, w);
+      load_item<WIN, EX>(p, TK, R, whole, w.item + 1, w);
       w.base = b;
     }
   };
@@ -376,6 +409,10 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       settle(x);
       const int u = (x - w.base) / w.span, h = p.by_head.mod(u);
       const int k0 = x - w.base - u * w.span, next = x + min(w.span - k0, x1 - x), k1 = min(w.kt, k0 + next - x);
+      if (EX && k0 >= k1) {  // no tiles of it
+        x = next;
+        continue;
+      }
       const int b = p.sel ? seen_keys(w.t0, p.T, p.B, p.starts, p.lens, p.width * p.page, p.causal, p.status).b : w.item;
       const int* row = p.table + (int64_t)b * p.width;
       const int* list = p.sel ? p.sel + ((int64_t)w.t0 * p.H + h) * p.keep : nullptr;
@@ -487,6 +524,10 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
     settle(x);
     const int u = (x - w.base) / w.span, h = p.by_head.mod(u), r0 = p.by_head.div(u) * R;
     const int k0 = x - w.base - u * w.span, next = x + min(w.span - k0, x1 - x), k1 = min(w.kt, k0 + next - x);
+    if (EX && k0 >= k1) {
+      x = next;
+      continue;
+    }
     const int nrows = min(R, w.rows - r0);
     const bool listed = p.sel != nullptr;
     // keys that a row of the unit may see
@@ -1034,7 +1075,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
             rl[tid] == 0.f ? -INFINITY : log_sum<W, kUp>(rm[tid], rl[tid]);
     };
     const int first = w.base + u * w.span;  // the unit's first place
-    const int c0 = first / run, parts = (first + w.span - 1) / run - c0 + 1;
+    const int c0 = first / run, parts = (first + w.kt - 1) / run - c0 + 1;
     if (parts == 1) {
       rows_out();
     } else {
@@ -1140,7 +1181,7 @@ cudaError_t launch(const AttnParams& p, const pp_cache& c, int sms, cudaStream_t
   constexpr int R = S::R, TK = S::TK;
   const int64_t units = (p.sel ? (int64_t)p.T * ((p.G.d + R - 1) / R) : ((int64_t)p.T * p.G.d + (int64_t)p.B * (R - 1)) / R) * p.H;
   const int64_t deep = ((int64_t)(p.sel ? std::min(p.width, p.keep) : p.width) * p.page + TK - 1) / TK;
-  if (units >= INT32_MAX / deep) return cudaErrorNotSupported;
+  if (units >= INT32_MAX / (deep + S::template EXTRA<WIN>)) return cudaErrorNotSupported;
   const int grid = std::min(sms * S::CTAS, kMaxCtas);
   return launch_after(attn_kernel<T, Cell, DP, RB, WIN>, dim3(grid), S::THREADS, S::SMEM, stream, 1, p, c.mk, c.mv);
 }
