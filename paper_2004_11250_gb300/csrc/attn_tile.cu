@@ -53,6 +53,9 @@ constexpr int kMaskWords = 2048;       // token bits of the pages in one window
 constexpr int kAhead = 8;              // entries of the tokens' lists in flight per thread
 constexpr int kSplits = 8;             // shares of a tile's blocks at most
 constexpr int kUp = 13;                // f16 weights are up to 2^13 where m is not behind, and 2^2 times that
+constexpr int kUpWindow = 10;          // with a window, up to this when m is set, and while 8 of them
+template <class T>
+constexpr float kMostWindow = std::is_same<T, __half>::value ? 65504.f : 0x1p64f;  // sum up to this with it
 template <class T>
 constexpr float kGrow = std::is_same<T, __half>::value ? 2.f : 8.f;  // log2 of how far a row's weights may pass their bound
 
@@ -162,6 +165,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     attn_tile_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
                      const __grid_constant__ CUtensorMap mv) {
   using S = TileShape<DP>;
+  constexpr int UP = WIN ? kUpWindow : kUp, ARRIVALS = WIN ? 4 : kSoft;
   constexpr int CHUNK_Q = kRowsT * 128, CHUNK_KV = kKeys * 128;  // bytes of 64 values of every row
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -268,7 +272,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     for (int i = 0; i < kInfo; ++i) mbar_init(su32(&info_full[i]), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(su32(&s_full[i]), 1);
-      mbar_init(su32(&p_full[i]), kSoft);
+      mbar_init(su32(&p_full[i]), ARRIVALS);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -547,6 +551,37 @@ __global__ void __launch_bounds__(kThreadsT, 2)
             for (int i = 0; i < 64; ++i)
               if (!((i < 32 ? (uint32_t)see : (uint32_t)(see >> 32)) >> (i & 31) & 1)) x[i] = -INFINITY;
           }
+          bool again = true;
+          if constexpr (WIN) {
+            // With m as it is, and only where some 8 weights' sum, which the row's total wants anyway, says that one might not fit the
+            // type once more below: most blocks neither wait for a maximum nor look for one
+            if (!__any_sync(~0u, m == -INFINITY && see != 0)) {
+              const float at = see ? (m == -INFINITY ? 0.f : m) : INFINITY;
+              const uint64_t sl2 = pack2(sl, sl), at2 = pack2(-at, -at);
+              float most = 0.f, sum = 0.f;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                uint64_t s2 = 0;
+#pragma unroll
+                for (int i = 4 * j; i < 4 * j + 4; ++i) {
+                  float a, c;
+                  unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), sl2, at2), a, c);
+                  a = ex2(a);
+                  c = ex2(c);
+                  s2 = add2(s2, pack2(a, c));
+                  w[i] = pack<T>(a, c);
+                }
+                float a, c;
+                unpack2(s2, a, c);
+                a += c;
+                most = fmaxf(most, a);
+                sum += a;
+              }
+              again = __any_sync(~0u, most > kMostWindow<T>);
+              if (!again) l += sum;
+            }
+          }
+          if (again) {
           float top[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -554,7 +589,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
 #pragma unroll
             for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
           }
-          const float mx = see ? lower(__fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl), kLift<T, kUp>) : -INFINITY;
+          const float mx = see ? lower(__fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl), kLift<T, UP>) : -INFINITY;
           const bool grow = mx > __fadd_rd(m, kGrow<T>);  // from -infinity, too
           if (__any_sync(~0u, grow)) {
             const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
@@ -596,6 +631,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           float a, c;
           unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, c);
           l += a + c;
+          }
         }
         tm_st32(tm, w);
         if (!bl.full) {
@@ -609,7 +645,12 @@ __global__ void __launch_bounds__(kThreadsT, 2)
         // block before are done by now
         if (g > 0 && !waited) hold(&pv_done, (g - 1) & 1);
         tm_fence_before();
-        mbar_arrive(su32(&p_full[g & 1]));
+        if constexpr (WIN) {  // (arrivals of threads come one after another)
+          __syncwarp();
+          if (lane == 0) mbar_arrive(su32(&p_full[g & 1]));
+        } else {
+          mbar_arrive(su32(&p_full[g & 1]));
+        }
       }
     }
     done += n;

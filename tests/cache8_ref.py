@@ -7,8 +7,8 @@ Tolerances of attention (u: half a unit in the last place as in decoder_ref), fr
   decoder_ref (2^-20).
   a weight errs by 2 d + 2^-19 relative, by its rounding before its product with v (over codes f16's: 2^-11 of it; else u of
   the type; fp32 queries, which take two halves, and fp32 values: 2^-20), and over codes and in f16 by half a step of f16 where
-  it has left the range that is normal: 2^-25 where the largest weight is 2^13 at the least (f16) or 2^8 (codes), times the
-  largest scale, and twice that for two roundings: 2^-37 or 2^-32 max p max |v| for each key.
+  it has left the range that is normal: 2^-25 where the largest weight is 2^10 at the least (f16) or 2^8 (codes), times the
+  largest scale, and twice that for two roundings: 2^-34 or 2^-32 max p max |v| for each key.
   n terms add n 2^-24.  Together times sum p |v|, plus one rounding to the type.
 """
 import math
@@ -74,7 +74,7 @@ def attend(q, k, v, table, starts, lens, scale, causal, window, sinks, codes):
     G, dt = Hq // H, q.dtype
     wide = dt == torch.float32
     u = 2.0 ** -20 if wide else ref.UNIT[torch.float16] if codes else ref.UNIT[dt]
-    step = 2.0 ** -32 if codes else 2.0 ** -37 if dt == torch.float16 else 0.0
+    step = 2.0 ** -32 if codes else 2.0 ** -34 if dt == torch.float16 else 0.0
     out = torch.zeros((T, Hq, D), dtype=torch.float64)
     lse = torch.full((T, Hq), -math.inf, dtype=torch.float64)
     tol = torch.full((T, Hq, D), ref.TINY[dt], dtype=torch.float64)
