@@ -7,7 +7,12 @@ pages worth reading for each token (``pp_cache_select``) and attends to them (``
 after the frames, a token at a time, on all three axes alike.  The projections are plain matrix products of torch;
 weights are random, as there is no trained model here.
 
+The cache holds the tokens' type, or codes of 8 bits (``pp_cache_append``).  With a window a token reads the last tokens and
+the first few (``pp_attn_window``), and the pages that nobody reads any more take new tokens: memory and time of a step
+do not grow with the video.
+
     python -m paper_2004_11250_gb300.reader --frames 32 --tokens 16
+    python -m paper_2004_11250_gb300.reader --frames 400 --bits 8 --window 2048 --sinks 16
 """
 from __future__ import annotations
 
@@ -23,7 +28,7 @@ from . import runner, synth
 class Layer:
     """One decoder layer's weights and its cache: x + attention(x) Wo."""
 
-    def __init__(self, width: int, Hq: int, H: int, D: int, pages: int, page: int, dtype, gen):
+    def __init__(self, width: int, Hq: int, H: int, D: int, pages: int, page: int, dtype, gen, bits: int = 16):
         def normal(*shape):
             return torch.randn(shape, device="cuda", generator=gen) / math.sqrt(shape[0])
 
@@ -31,8 +36,12 @@ class Layer:
         self.wo = (0.5 * normal(Hq * D, width)).to(dtype)
         self.qw = 1 + 0.1 * torch.randn(D, device="cuda", generator=gen)
         self.kw = 1 + 0.1 * torch.randn(D, device="cuda", generator=gen)
-        self.k = torch.zeros((pages, H, page, D), device="cuda", dtype=dtype)
+        self.k = torch.zeros((pages, H, page, D), device="cuda", dtype=torch.int8 if bits == 8 else dtype)
         self.v = torch.zeros_like(self.k)
+        if bits == 8:
+            self.k_scales, self.v_scales = (torch.zeros((pages, H), device="cuda") for _ in range(2))
+            self.cache = pp.pp_cache8_create(self.k, self.v, self.k_scales, self.v_scales, dtype)
+            return
         self.codes = torch.zeros((pages, H, 2, D), device="cuda", dtype=torch.int8)
         self.scales = torch.zeros((pages, H), device="cuda")
         self.cache = pp.pp_cache_create(self.k, self.v, self.codes, self.scales)
@@ -42,20 +51,33 @@ class FrameReader:
     """Reads frames and answers about them (one sequence).
 
     keep: pages that a token reads at most, the first and the last two among them; None: all, without a selection.
+    bits: 8 for a cache in 8 bits; 16 (or 32, with dtype) for one of the tokens' type.
+    window, sinks: a token reads the last `window` tokens and the first `sinks`; None: no window.  With a window or in 8 bits
+    there is no selection (keep is None).
     """
 
     EPS = 1e-6
 
     def __init__(self, trunk: Optional[synth.Net] = None, layers: int = 2, Hq: int = 8, H: int = 2, D: int = 64,
-                 page: int = 16, max_tokens: int = 4096, keep: Optional[int] = 16, dtype=torch.bfloat16, seed: int = 0):
+                 page: int = 16, max_tokens: int = 4096, keep: Optional[int] = 16, dtype=torch.bfloat16, seed: int = 0,
+                 bits: int = 16, window: Optional[int] = None, sinks: int = 4):
+        if bits not in (8, 16) or (window is not None and window < 1) or sinks < 0:
+            raise ValueError("bits is 8 or 16, a window 1 token or more, sinks 0 or more")
+        if keep is not None and (bits == 8 or window is not None):
+            raise ValueError("pages are selected (keep) from a cache of the tokens' type without a window")
         spec = trunk if trunk is not None else synth.cfg1_vgg16()
         self.net = runner.DeviceNet(spec)
         _, self.C, self.rows, self.cols = self.net.out_shape
         self.Hq, self.H, self.D, self.page, self.keep, self.dtype = Hq, H, D, page, keep, dtype
+        self.bits, self.window, self.sinks = bits, window, sinks
         gen = torch.Generator(device="cuda")
         gen.manual_seed(seed)
-        pages = -(-max_tokens // page)
-        self.layers: List[Layer] = [Layer(self.C, Hq, H, D, pages, page, dtype, gen) for _ in range(layers)]
+        width = pages = -(-max_tokens // page)  # of the table; of the cache
+        first = -(-sinks // page)               # pages that stay
+        if window is not None:  # the others in turn: a frame's windows, the frame, and a page begun at either end
+            turn = -(-(window + self.rows * self.cols) // page) + 2
+            pages = min(pages, first + turn)
+        self.layers: List[Layer] = [Layer(self.C, Hq, H, D, pages, page, dtype, gen, bits) for _ in range(layers)]
         # a quarter of the pairs follows the frame's number, the rest its rows and columns
         P = D // 2
         axis = [0] * (P // 4) + [1] * ((P - P // 4) // 2)
@@ -63,7 +85,11 @@ class FrameReader:
         self.freq = [10000.0 ** (-j / P) for j in range(P)]
         self.axis = axis
         self.rope = pp.pp_rope_create(D, axis, self.freq, 3)
-        self.table = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32)[None].contiguous()
+        order = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32)
+        at = torch.arange(width, device="cuda")
+        if pages < width:
+            at = torch.where(at < first, at, first + (at - first) % (pages - first))
+        self.table = order[at][None].contiguous()
         self.map = torch.empty(self.net.out_shape, device="cuda")
         self.seen = 0    # tokens in the cache
         self.frames = 0
@@ -89,15 +115,25 @@ class FrameReader:
         sel = None if self.keep is None else torch.empty((T, self.H, self.keep), device="cuda", dtype=torch.int32)
         q = torch.empty((T, self.Hq, self.D), device="cuda", dtype=self.dtype)
         out = torch.empty_like(q)
+        if self.bits == 8:
+            k = torch.empty((T, self.H, self.D), device="cuda", dtype=self.dtype)
         for L in self.layers:
             fused = x @ L.wqkv
             heads = fused.view(T, self.Hq + 2 * self.H, self.D)
             new_q, new_k, new_v = heads[:, : self.Hq], heads[:, self.Hq: self.Hq + self.H], heads[:, self.Hq + self.H:]
-            pp.pp_qkv_store(self.rope, L.cache, pos, slots, self.EPS, new_q, L.qw, q, new_k, L.kw, new_v, s)
+            if self.bits == 8:
+                pp.pp_qk_rotate(self.rope, pos, self.EPS, new_q, L.qw, q, new_k, L.kw, k, s)
+                pp.pp_cache_append(L.cache, k, new_v, starts, self.table, lens, s)
+            else:
+                pp.pp_qkv_store(self.rope, L.cache, pos, slots, self.EPS, new_q, L.qw, q, new_k, L.kw, new_v, s)
             if sel is not None:
                 pp.pp_cache_summarize(L.cache, filled, s)
                 pp.pp_cache_select(L.cache, q, starts, self.table, lens, pp.PP_ATTN_CAUSAL, 1, 2, sel, s)
-            pp.pp_attn_forward(L.cache, q, starts, self.table, lens, 1 / math.sqrt(self.D), pp.PP_ATTN_CAUSAL, sel, out, None, s)
+            scale = 1 / math.sqrt(self.D)
+            if self.window is None:
+                pp.pp_attn_forward(L.cache, q, starts, self.table, lens, scale, pp.PP_ATTN_CAUSAL, sel, out, None, s)
+            else:
+                pp.pp_attn_window(L.cache, q, starts, self.table, lens, scale, pp.PP_ATTN_CAUSAL, self.window, self.sinks, out, None, s)
             x = x + out.view(T, -1) @ L.wo
         self.seen = n + T
         return x
@@ -144,10 +180,14 @@ def main(argv=None):
     a.add_argument("--frames", type=int, default=32)
     a.add_argument("--tokens", type=int, default=16)
     a.add_argument("--keep", type=int, default=16, help="pages that a token reads at most; 0: all")
+    a.add_argument("--bits", type=int, default=16, choices=(8, 16), help="of the cache; 8: without a selection of pages")
+    a.add_argument("--window", type=int, default=0, help="last tokens that a token reads, without a selection of pages; 0: no window")
+    a.add_argument("--sinks", type=int, default=4, help="first tokens that stay visible beside a window")
     o = a.parse_args(argv)
-    if o.frames < 1 or o.tokens < 0 or not (o.keep == 0 or o.keep >= 3):
-        a.error("at least 1 frame, 0 tokens, and 3 pages (the first and the last two)")
-    r = FrameReader(max_tokens=196 * o.frames + o.tokens, keep=o.keep or None)  # maps of 14 x 14
+    if o.frames < 1 or o.tokens < 0 or not (o.keep == 0 or o.keep >= 3) or o.window < 0 or o.sinks < 0:
+        a.error("at least 1 frame, 0 tokens, 3 pages (the first and the last two), and 0 of a window's")
+    keep = None if o.bits == 8 or o.window else o.keep or None
+    r = FrameReader(max_tokens=196 * o.frames + o.tokens, keep=keep, bits=o.bits, window=o.window or None, sinks=o.sinks)  # maps of 14 x 14
     gen = torch.Generator(device="cuda")
     gen.manual_seed(1)
     ev = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
