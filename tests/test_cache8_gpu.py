@@ -377,8 +377,21 @@ TILES = [
     (F16, 8, 4, 48, 16, [30], [0, 50]),      # more tokens than keys
 ]
 
+# and over codes, where tiles are taken from more rows on
+TILES8 = [
+    (BF16, 16, 8, 64, 16, [170], [0, 48]),
+    (F16, 16, 8, 128, 8, [300, 40], [0, 30, 52]),
+    (BF16, 16, 4, 80, 64, [200], [0, 100]),
+    (F16, 16, 2, 64, 128, [500], [0, 180]),
+    (BF16, 16, 8, 128, 32, [90, 0, 200], [0, 20, 20, 52]),
+    (F16, 4, 64, 128, 16, [70, 30], [0, 20, 26]),
+    (BF16, 16, 4, 112, 256, [700], [0, 96]),
+    (F16, 16, 8, 48, 16, [30], [0, 50]),      # more tokens than keys
+    (F16, 8, 8, 128, 64, [2100], [0, 40]),    # split along the keys, and joined
+]
 
-@pytest.mark.parametrize("case", TILES)
+
+@pytest.mark.parametrize("case", TILES + TILES8)
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("strided", [False, True])
 def test_codes_tiles(pp, case, causal, strided):
@@ -407,6 +420,99 @@ def test_window_chunk(pp, case, window, sinks, codes):
 @pytest.mark.parametrize("codes", [False, True])
 def test_window_tiles(pp, case, window, sinks, codes):
     check(pp, *case, window, sinks, codes=codes, garbage=True)
+
+
+@pytest.mark.parametrize("window,sinks", [WINDOWS[i] for i in (0, 2, 4, 6, 8, 10)])
+@pytest.mark.parametrize("case", TILES8)
+def test_window_tiles_of_codes(pp, case, window, sinks):
+    check(pp, *case, window, sinks, garbage=True)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B", [33, 150, 900])
+@pytest.mark.parametrize("window", [None, 20])
+def test_many_sequences(pp, dt, B, codes, window):
+    """More sequences than a lane or a thread looks after one of, idle ones among them; as single tokens and as ranges."""
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 40, (B,), generator=g).tolist()
+    check(pp, dt, 1, 2, 64, 16, lens, None, window, 3, codes=codes, garbage=True)
+    if B == 150:
+        n = torch.randint(0, 4, (B,), generator=g).tolist()
+        check(pp, dt, 1, 2, 64, 16, lens, [sum(n[:b]) for b in range(B + 1)], window, 3, codes=codes, garbage=True)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("dt,H,G,D,page,lens,n,window", [
+    (BF16, 1, 8, 128, 64, [40000], 1, None), (F32, 1, 3, 96, 32, [30000, 17], 1, None), (F16, 1, 4, 64, 16, [50000, 20000, 1], 1, 33333),
+    (BF16, 2, 4, 128, 64, [30000], 5, 20000), (F16, 8, 8, 128, 128, [20000], 40, None), (BF16, 8, 4, 64, 16, [20000], 100, 15000)])
+def test_long_sequences(pp, dt, H, G, D, page, lens, n, window, codes):
+    """Split over many CTAs and joined in two levels, or along tiles' keys; against 64 bits on the GPU.  Tolerance as derived for
+    the short ones with the softmax's own sums: 2^-11 of sum p |v| for 16-bit weights (over keys in bf16 2^-8), 2^-17 for the rest (logits err
+    by some 140 x 2^-24 x 10, and 50000 x 2^-24 of the sum), one rounding to the type."""
+    g = torch.Generator(device="cuda").manual_seed(D)
+    need = sum(-(-v // page) for v in lens)
+    table = tables(lens, page, need).cuda()
+    q = torch.randn((n * len(lens), H * G, D), device="cuda", generator=g).to(dt)
+    if codes:
+        k, v = (torch.randint(-127, 128, (need, H, page, D), device="cuda", generator=g, dtype=torch.int8) for _ in range(2))
+        ks, vs = (torch.rand((need, H), device="cuda", generator=g) * 0.01 + 0.005 for _ in range(2))
+        cache = pp.pp_cache8_create(k, v, ks, vs, dt)
+        k64, v64 = k.double() * ks.double()[:, :, None, None], v.double() * vs.double()[:, :, None, None]
+    else:
+        k, v = (torch.randn((need, H, page, D), device="cuda", generator=g).to(dt) for _ in range(2))
+        cache = pp.pp_cache_create(k, v)
+        k64, v64 = k.double(), v.double()
+    out, lse = torch.empty_like(q), torch.empty((q.shape[0], H * G), device="cuda")
+    starts = None if n == 1 else torch.arange(0, n * len(lens) + 1, n, device="cuda", dtype=torch.int32)
+    a = (cache, q, starts, table, ints(lens).cuda(), D ** -0.5, pp.PP_ATTN_CAUSAL)
+    try:
+        pp.pp_attn_forward(*a, None, out, lse) if window is None else pp.pp_attn_window(*a, window, 40, out, lse)
+        assert pp.pp_cache_device_status(cache) == 0
+    finally:
+        pp.pp_cache_destroy(cache)
+    u = 2.0 ** -20 if dt is F32 else 2.0 ** -11 if codes or dt is F16 else 2.0 ** -8
+    for b, L in enumerate(lens):
+        ids = table[b, : -(-L // page)].long()
+        kk, vv = (x[ids].transpose(1, 2).reshape(-1, H, D)[:L] for x in (k64, v64))
+        x = q[b * n: (b + 1) * n].double().view(n, H, G, D)
+        s = torch.einsum("nhgd,shd->nhgs", x, kk) * D ** -0.5
+        seen = torch.arange(L - n + 1, L + 1, device="cuda")[:, None]
+        at = torch.arange(L, device="cuda")[None]
+        hide = at >= seen
+        if window is not None:
+            hide = hide | ((at < seen - window) & (at >= 40))
+        s = s.masked_fill(hide[:, None, None], -math.inf)
+        p = torch.softmax(s, -1)
+        want = torch.einsum("nhgs,shd->nhgd", p, vv).reshape(n, H * G, D)
+        tol = (u + 2.0 ** -17) * torch.einsum("nhgs,shd->nhgd", p, vv.abs()).reshape(n, H * G, D) + ref.UNIT[dt] * want.abs() * 1.01 + ref.TINY[dt]
+        assert ref.worst(out[b * n: (b + 1) * n], want.cpu(), tol.cpu()) <= 1
+        assert float((lse[b * n: (b + 1) * n].double() - torch.logsumexp(s, -1).reshape(n, -1)).abs().max()) < 2.0 ** -14
+
+
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("starts,n", [(None, 3), ([0, 48], 48)])
+def test_codes_queries_not_finite(pp, dt, starts, n):
+    """Rows of queries with NaN have NaN, the others are as if they were not there."""
+    H, G, D, page = 16, 8, 64, 16
+    lens = [50, 70, 20] if starts is None else [90]
+    h = Held(pp, 12, H, page, D, dt)
+    table = tables(lens, page, 12)
+    k, v = h.values()
+    q = torch.randn((n, H * G, D), generator=torch.Generator().manual_seed(8)).to(dt)
+    want, wl, tol, tl = ref8.attend(q, k, v, table, starts, lens, 0.125, True, 10 ** 6, 0, True)
+    bad = torch.zeros((n, H * G), dtype=torch.bool)
+    bad[0, 3] = bad[n - 1, 5] = bad[1, 64:72] = True
+    q[bad] = math.nan
+    out, lse = torch.empty((n, H * G, D), device="cuda", dtype=dt), torch.empty((n, H * G), device="cuda")
+    try:
+        pp.pp_attn_forward(h.cache, q.cuda(), None if starts is None else ints(starts).cuda(), table.cuda(), ints(lens).cuda(), 0.125,
+                           pp.PP_ATTN_CAUSAL, None, out, lse)
+        got, gl = out.cpu(), lse.cpu()
+        assert torch.isnan(got[bad]).all() and torch.isnan(gl[bad]).all()
+        assert ref.worst(got[~bad], want[~bad], tol[~bad]) <= 1 and ref.worst(gl[~bad], wl[~bad], tl[~bad]) <= 1
+    finally:
+        h.close()
 
 
 @pytest.mark.parametrize("codes", [False, True])
