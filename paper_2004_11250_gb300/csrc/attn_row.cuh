@@ -358,7 +358,12 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   const bool has = x0 >= before && x0 < before + mine;
   if (has) {
     for (int i = i0;; ++i) {
-      if (per > 1 || whole) load_item<WIN, EX>(p, TK, R, whole, i, w);
+      if (per > 1) {
+        load_item<WIN, EX>(p, TK, R, whole, i, w);
+      } else {
+        w.span = span_of(w.kt, whole);
+        w.places = w.units * w.span;
+      }
       if (x0 < before + w.places) break;
       before += w.places;
     }
@@ -1093,13 +1098,13 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
         }
       };
       // the last of `of` to come here; what the others stored is then there to read
+      // (one thread's release behind the barrier is every thread's)
       auto last_of = [&](int* counter, int of) {
-        __threadfence();
         group_sync<kWarps * 32>();
         if (tid == 0) {
-          const int was = atomicAdd(counter, 1);
+          int was;
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(was) : "l"(counter) : "memory");
           if (was == of - 1) *counter = 0;
-          __threadfence();
           last_flag = was == of - 1;
         }
         group_sync<kWarps * 32>();
@@ -1107,6 +1112,24 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       };
       // n parts, step apart, into acc, rm and rl: in their order, whoever comes last
       auto join = [&](int part, int n, int step) {
+        if (EX > 0 && R <= 8 && n <= kGroup) {  // 16 lanes to a row, a part each
+          const int r = tid / kGroup, i = tid % kGroup;
+          const bool in = r < nrows && i < n;
+          const float* from = slot(part + (in ? i : 0) * step) + kRows * DP + (in ? r : 0);
+          const float pm = in ? __ldcg(from) : -INFINITY, pl = in ? __ldcg(from + kRows) : 0.f;
+          float mx = pm;
+#pragma unroll
+          for (int d = 1; d < kGroup; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, d));
+          const float c = pm == -INFINITY ? 0.f : ex2(pm - mx);
+          float sum = c * pl;  // NaN stays NaN
+#pragma unroll
+          for (int d = 1; d < kGroup; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+          if (in) wts[r][i] = c;
+          if (i == 0 && r < nrows) {
+            rm[r] = mx;
+            rl[r] = sum;
+          }
+        } else {
         for (int i = tid; i < n * kRows; i += kWarps * 32) {  // row i % 16 of part i / 16
           const float* from = slot(part + i / kRows * step) + kRows * DP + i % kRows;
           if (i % kRows < nrows) {
@@ -1125,6 +1148,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
           }
           rm[tid] = mx;
           rl[tid] = sum;
+        }
         }
         group_sync<kWarps * 32>();
         for (int i = tid; i < nrows * (DP / 4); i += kWarps * 32) {
