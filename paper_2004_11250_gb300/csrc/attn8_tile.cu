@@ -206,8 +206,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
   const uint32_t tmem = tmem_s;
   // a bounded wait; after one gave up none waits any more
   auto hold = [&](uint64_t* bar, uint32_t parity) {
-    if (mbar_try(su32(bar), parity) || *(volatile int*)&dead) return;
-    if (!wait(su32(bar), parity)) dead = 1;
+    if (!mbar_try(su32(bar), parity)) hold_on(su32(bar), parity, &dead);
   };
 
   // what the warp has done before is there for who waits
@@ -425,8 +424,8 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       tm_fence_after();
       float top = 0.f, sum = 0.f;
       bool again = __any_sync(~0u, m == -INFINITY);  // m is not set: it has to be where the row sees something
-      if (again) again = __any_sync(~0u, m == -INFINITY && (!part || (see(0) | see(1))));
-      if (!again) {
+      if (__builtin_expect(again, 0)) again = __any_sync(~0u, m == -INFINITY && (!part || (see(0) | see(1))));
+      if (__builtin_expect(!again, 1)) {
         uint32_t w[32];
         const float at = m == -INFINITY ? 0.f : m;
         float x[2][32];
@@ -446,7 +445,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
             for (int i = 0; i < 8; i += 2)
               unpack2(fma2(pack2(y[8 * j + i], y[8 * j + i + 1]), pack2(kj, kj), pack2(oj, oj)), y[8 * j + i], y[8 * j + i + 1]);
           }
-          if (part) {
+          if (__builtin_expect(part, 0)) {
             const uint32_t bits = see(c);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -474,7 +473,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
           tm_st32(s_tm, w);
         }
       }
-      if (again) {
+      if (__builtin_expect(again, 0)) {
         // once more from the scores, with m above them.  Each step is rounded by itself, as the maximum's are, so that no weight
         // passes its bound and the largest does not vanish where fp32 numbers lie further than 1 apart
         auto exponents = [&](int c, float (&y)[32]) {

@@ -747,12 +747,28 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int r = 2 * rb + (e & 1);
-              float y = fmaf(sc[z][rb][e], ks[z][e >> 1] * slr[r], -m[r]);
-              if (masked(z, rb, e)) y = -INFINITY;
-              x[z][rb][e] = ex2(y);
+              x[z][rb][e] = fmaf(sc[z][rb][e], ks[z][e >> 1] * slr[r], -m[r]);
+            }
+        // (what is rare is kept out of the way: the loop is long for the instruction cache)
+        if (__builtin_expect(!clean, 0)) {
+#pragma unroll
+          for (int z = 0; z < SL; ++z)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (masked(z, rb, e)) x[z][rb][e] = -INFINITY;
+        }
+#pragma unroll
+        for (int z = 0; z < SL; ++z)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[z][rb][e] = ex2(x[z][rb][e]);
               top = fmaxf(top, x[z][rb][e]);
             }
-        if (__any_sync(~0u, top > kMost8)) {
+        if (__builtin_expect(__any_sync(~0u, top > kMost8), 0)) {
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
             float mx = -INFINITY;
@@ -787,6 +803,22 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
 #pragma unroll
         for (int z = 0; z < SL; ++z) vmax = fmaxf(vmax, fmaxf(vs[z][0], vs[z][1]));
         const bool differ = 8 << log_br - 3 < KW && vmax > 0.f;
+#pragma unroll
+        for (int z = 0; z < SL; ++z)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) l[2 * rb + (e & 1)] += x[z][rb][e];
+        if (__builtin_expect(differ, 0)) {
+#pragma unroll
+          for (int z = 0; z < SL; ++z)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float f = vs[z][e >> 1] / vmax;
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb) x[z][rb][e] *= f;
+            }
+        }
         uint32_t bh[SL][RB][2], bl[SL][RB][2];
 #pragma unroll
         for (int z = 0; z < SL; ++z)
@@ -794,13 +826,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
           for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              float a = x[z][rb][2 * i], b = x[z][rb][2 * i + 1];
-              l[2 * rb] += a;
-              l[2 * rb + 1] += b;
-              if (differ) {
-                a *= vs[z][i] / vmax;
-                b *= vs[z][i] / vmax;
-              }
+              const float a = x[z][rb][2 * i], b = x[z][rb][2 * i + 1];
               const uint32_t hi = pack_down<W>(a, b);
               Vec<W, 2> two;
               memcpy(&two, &hi, 4);
