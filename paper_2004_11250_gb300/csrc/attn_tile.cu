@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           tm_ld32(tm + 32, reinterpret_cast<float(&)[32]>(x[32]));
           tm_wait_ld();
           // rows that see all or nothing need no mask: the latter's exponents are taken from infinity below
-          if (part) {
+          if (WIN ? __builtin_expect(part, 0) : part) {
 #pragma unroll
             for (int i = 0; i < 64; ++i)
               if (!((i < 32 ? (uint32_t)see : (uint32_t)(see >> 32)) >> (i & 31) & 1)) x[i] = -INFINITY;
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           if constexpr (WIN) {
             // With m as it is, and only where some 8 weights' sum, which the row's total wants anyway, says that one might not fit the
             // type once more below: most blocks neither wait for a maximum nor look for one
-            if (!__any_sync(~0u, m == -INFINITY && see != 0)) {
+            if (__builtin_expect(!__any_sync(~0u, m == -INFINITY && see != 0), 1)) {
               const float at = see ? (m == -INFINITY ? 0.f : m) : INFINITY;
               const uint64_t sl2 = pack2(sl, sl), at2 = pack2(-at, -at);
               float most = 0.f, sum = 0.f;
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
               if (!again) l += sum;
             }
           }
-          if (again) {
+          if (WIN ? __builtin_expect(again, 0) : again) {
           float top[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           }
         }
         tm_st32(tm, w);
-        if (!bl.full) {
+        if (WIN ? __builtin_expect(!bl.full, 0) : !bl.full) {
           hold(&v_full[st], g / kStages & 1);
           __syncwarp();
           const int at = WIN ? key_of(i0 + (k << log_pc)) : 0;
