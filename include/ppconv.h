@@ -658,8 +658,10 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  *           order, the ones that the token sees before others (of a token that sees P pages the first
  *           min(keep, P) entries count; those below 0 are skipped); NULL (keep 0): all pages
  * What the cache holds outside the visible keys is never used, NaN and infinities included.
- * A cache in 8 bits has its codes used as they are, exact, with the scales of their pages in fp32; queries count with
- * all their bits, weights as f16's below.
+ * A cache in 8 bits has its codes used as they are, exact, with the scales of their pages in fp32, and queries count with
+ * all their bits.  A weight, times its page's value scale over that of the largest near by, is two f16 halves (few rows
+ * per key: down to 2^-14 of the row's largest; those below 2^-36 are 0) or one of 11 bits (many tokens in 16 bits: down
+ * to 2^-22, below 2^-33 0).  Scales are finite.
  * A weight's product with v takes the weight in fp32 (fp32), as two 16-bit halves (16 bits, few rows
  * per key), or rounded to the type (16 bits, many tokens: 11 bits in f16, 8 in bf16).  f16 weights
  * below 2^-27 of the row's largest have fewer bits, and those below 2^-38 are 0 there.
@@ -677,7 +679,8 @@ pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q
  * pp_attn_forward with a sliding window: of the keys 0 .. n - 1 that a token sees without one, it sees the last
  * `window` (its own among them) and the first `sinks`.  Over either kind of cache.  Pages between the first keys and
  * the windows of a call's tokens are not read, and their entries of the table not looked at (they may be -1, and
- * the pages in use elsewhere); a window that holds all keys gives pp_attn_forward's bits.
+ * the pages in use elsewhere); a window that holds all keys gives pp_attn_forward's bits.  f16 weights of many tokens
+ * have 11 bits down to 2^-24 of the row's largest, and are 0 below 2^-35.
  * Errors: as pp_attn_forward; also window < 1, sinks < 0.
  */
 pp_status pp_attn_window(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,

@@ -605,6 +605,28 @@ def test_codes_pages_of_zeros(pp):
             h.close()
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("H,G,n", [(1, 4, 48), (16, 8, 48)])
+@pytest.mark.parametrize("power", [-20, -50, 40])
+def test_codes_rows_that_see_small_pages_alone(pp, dt, H, G, n, power):
+    """The values' scales change by a large factor from one page to the next, which the first tokens of a chunk still see."""
+    D, page, L, window = 64, 32, 170, 20
+    h = Held(pp, 8, H, page, D, dt)
+    table = tables([L], page, 8)
+    for w in range(4, 6):
+        h.ds[1][int(table[0, w])] *= 2.0 ** power
+    h.s[1] = h.ds[1].cpu()
+    k, v = h.values()
+    q = torch.randn((n, H * G, D), generator=torch.Generator().manual_seed(4)).to(dt)
+    out = torch.empty((n, H * G, D), device="cuda", dtype=dt)
+    try:
+        pp.pp_attn_window(h.cache, q.cuda(), ints([0, n]).cuda(), table.cuda(), ints([L]).cuda(), 0.125, pp.PP_ATTN_CAUSAL, window, 0, out)
+        want, _, tol, _ = ref8.attend(q, k, v, table, [0, n], [L], 0.125, True, window, 0, True)
+        assert ref.worst(out, want, tol) <= 1 and h.status() == 0
+    finally:
+        h.close()
+
+
 def test_codes_queries_of_any_size(pp):
     """Rows of queries from the smallest to the largest: each has its own power of two."""
     H, G, D, page, L = 1, 8, 64, 16, 40
