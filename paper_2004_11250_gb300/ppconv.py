@@ -606,12 +606,20 @@ def pp_cache_summarize(cache, ids, stream=None):
 
 
 def _sequences(q, cache, starts, table, lens, y):
-    """The arguments that pp_cache_select and pp_attn_forward share: tokens, queries, sequences."""
+    """The arguments that pp_cache_select and the attention calls share: tokens, queries, sequences."""
     T = q.shape[0]
     qp, qt, qh, Hq = _heads(q, cache.dtype, T, cache.shape[3])
+    return (cache, T, qp, qt, qh, Hq, *_tables(starts, table, lens, y.i32))
+
+
+def _tables(starts, table, lens, i32):
+    """(sequences, starts, table, width, lens) as the calls take them.  A small call is the host's, so its checks are in one place."""
     B, width = table.shape
-    return (cache, T, qp, qt, qh, Hq, B, _dense(starts, (B + 1,), y.i32, "starts"),
-            _dense(table, (B, width), y.i32, "table"), width, _dense(lens, (B,), y.i32, "lens"))
+    if not (table.dtype is i32 and lens.dtype is i32 and lens.shape == (B,) and table.is_cuda and lens.is_cuda and
+            table.is_contiguous() and lens.is_contiguous()):
+        _dense(table, (B, width), i32, "table")
+        _dense(lens, (B,), i32, "lens")
+    return B, None if starts is None else _dense(starts, (B + 1,), i32, "starts"), table.data_ptr(), width, lens.data_ptr()
 
 
 def pp_cache_select(cache, q, starts, table, lens, flags, first, last, sel, stream=None):
@@ -642,23 +650,22 @@ def pp_attn_window(cache, q, starts, table, lens, scale, flags, window, sinks, o
 
 def pp_cache_append(cache, k, v, starts, table, lens, stream=None):
     """New tokens k, v [T][H][D] of the sequences into a cache in 8 bits: the last ones of lens[b] keys each."""
-    (T, H, D), (B, width), y = k.shape, table.shape, _torch_types()
-    kp, kt, kh, _ = _heads(k, cache.dtype, T, cache.shape[3])
-    vp, vt, vh, Hv = _heads(v, cache.dtype, T, D)
-    if H != cache.shape[1] or Hv != H:
-        raise PPError(PP_ERR_INVALID_ARG, "pp_cache_append: k and v have the cache's heads")
-    _check(lib.pp_cache_append(cache, T, kp, kt, kh, vp, vt, vh, B, _dense(starts, (B + 1,), y.i32, "starts"),
-                               _dense(table, (B, width), y.i32, "table"), width, _dense(lens, (B,), y.i32, "lens"),
-                               _stream(stream)), "pp_cache_append")
+    shape, dt, (_, H, _, D) = k.shape, cache.dtype, cache.shape
+    kt, kh, kd = k.stride()
+    vt, vh, vd = v.stride()
+    T = shape[0]
+    if not (shape == v.shape == (T, H, D) and k.dtype is dt and v.dtype is dt and kd == 1 and vd == 1 and k.is_cuda and v.is_cuda):
+        raise PPError(PP_ERR_INVALID_ARG, "pp_cache_append: k and v are [T][the cache's heads][D] of its type on the GPU, dense in D")
+    _check(lib.pp_cache_append(cache, T, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
+                               *_tables(starts, table, lens, (_types or _torch_types()).i32), _stream(stream)), "pp_cache_append")
 
 
 def pp_cache_read(cache, starts, table, lens, k_out, v_out, stream=None):
     """The sequences' last keys and values of a cache in 8 bits into k_out, v_out [T][H][D] (either may be None)."""
-    y, (_, H, _, D), (B, width) = _torch_types(), cache.shape, table.shape
     x = k_out if k_out is not None else v_out
     if x is None:
         raise PPError(PP_ERR_INVALID_ARG, "pp_cache_read: nothing to read into")
-    T = x.shape[0]
-    _check(lib.pp_cache_read(cache, T, B, _dense(starts, (B + 1,), y.i32, "starts"), _dense(table, (B, width), y.i32, "table"),
-                             width, _dense(lens, (B,), y.i32, "lens"), _dense(k_out, (T, H, D), cache.dtype, "k_out"),
-                             _dense(v_out, (T, H, D), cache.dtype, "v_out"), _stream(stream)), "pp_cache_read")
+    T, dt, (_, H, _, D) = x.shape[0], cache.dtype, cache.shape
+    B, s, t, width, n = _tables(starts, table, lens, (_types or _torch_types()).i32)
+    _check(lib.pp_cache_read(cache, T, B, s, t, width, n, _dense(k_out, (T, H, D), dt, "k_out"),
+                             _dense(v_out, (T, H, D), dt, "v_out"), _stream(stream)), "pp_cache_read")
