@@ -224,7 +224,7 @@ struct ReadParams {
 };
 
 template <class T, bool WIDE>
-__global__ void __launch_bounds__(kReadThreads) read_kernel(const __grid_constant__ ReadParams p) {
+__global__ void __launch_bounds__(kReadThreads, 6) read_kernel(const __grid_constant__ ReadParams p) {
   __shared__ int place[kMostTokens];  // page id * page + offset; -1: no such key
   after_previous();
   const int t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0), tid = threadIdx.x;
