@@ -615,11 +615,11 @@ def _sequences(q, cache, starts, table, lens, y):
 def _tables(starts, table, lens, i32):
     """(sequences, starts, table, width, lens) as the calls take them.  A small call is the host's, so its checks are in one place."""
     B, width = table.shape
-    if not (table.dtype is i32 and lens.dtype is i32 and lens.shape == (B,) and table.is_cuda and lens.is_cuda and
+    first = None if starts is None else _dense(starts, (B + 1,), i32, "starts")
+    if (lens is not None and table.dtype is i32 and lens.dtype is i32 and lens.shape == (B,) and table.is_cuda and lens.is_cuda and
             table.is_contiguous() and lens.is_contiguous()):
-        _dense(table, (B, width), i32, "table")
-        _dense(lens, (B,), i32, "lens")
-    return B, None if starts is None else _dense(starts, (B + 1,), i32, "starts"), table.data_ptr(), width, lens.data_ptr()
+        return B, first, table.data_ptr(), width, lens.data_ptr()
+    return B, first, _dense(table, (B, width), i32, "table"), width, _dense(lens, (B,), i32, "lens")
 
 
 def pp_cache_select(cache, q, starts, table, lens, flags, first, last, sel, stream=None):
