@@ -35,7 +35,7 @@
 // are left out, and m is not looked for in each block: sums of 8 weights say when one
 // might not fit, and the block is computed again.  2048 tokens over windows of 4096
 // keys and 64 first ones (f16): 168 us, 830 TFLOP/s; each tile's start and end take a
-// quarter of it, and 512 tiles come in two rounds of 304.
+// sixth of it, and 512 tiles come in two rounds of 304.
 #include <algorithm>
 #include <type_traits>
 
