@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
   int8_t* codes = p.codes[pool] + cell * p.page * p.D;
   const float had = at ? p.scales[pool][cell] : 0.f;
   const int64_t ts = p.ts[pool];
-  const T* x = static_cast<const T*>(p.x[pool]) + (s0 + lo - from) * ts + h * p.hs[pool];
+  const T* x = static_cast<const T*>(p.x[pool]) + (s0 + (lo - from)) * ts + h * p.hs[pool];
   const int row = p.row.d, chunks = (hi - lo) * row;
   auto chunk = [&](int c) {
     const int r = p.row.div(c);
@@ -362,7 +362,7 @@ pp_status pp_cache_read(const pp_cache* cache, int T, int B, const int32_t* star
                   FastDiv(c.H)};
   const cudaError_t e = by_type(c.dtype, (at & 31) == 0, [&](auto* t, auto wide) {
     using E = std::remove_pointer_t<decltype(t)>;
-    return launch_after(read_kernel<E, decltype(wide)::value>, dim3((unsigned)((T + tokens - 1) / tokens)), kReadThreads, 0,
+    return launch_after(read_kernel<E, decltype(wide)::value>, dim3((unsigned)((T - 1) / tokens + 1)), kReadThreads, 0,
                         (cudaStream_t)stream, 1, p);
   });
   return e == cudaSuccess ? PP_OK : PP_ERR_CUDA;
