@@ -30,8 +30,10 @@
 // Over a cache in 8 bits a tile is 128 keys.  Codes are whole numbers, exact in f16, so
 // all products are f16's: queries of other types are scaled by a power of two per row (bf16
 // has fewer bits than f16, and fp32 comes as three f16 parts), a page's key scale goes into
-// its scores, and its value scale to the 32 keys' products that a warp adds up.  A byte
-// becomes f16 by two instructions for two: placed below the exponent of 1024, and 1152 taken
+// its scores, and its value scale to the 32 keys' products that a warp adds up (where pages
+// are smaller the largest of their scales, and the weights of the others are less, down to
+// 2^-6; pages beyond that come again as a tile of their own).  A byte becomes f16 by two
+// instructions for two: placed below the exponent of 1024, and 1152 taken
 // off.  At half the bytes a key the instructions count: weights are taken from the last
 // maximum while they fit, 8 rows to a unit leave registers for three CTAs per SM, and what is
 // rare lies behind the loop.  8 sequences of 65536 keys (f16) 169 us, 6.4 TB/s (260 at
@@ -63,6 +65,7 @@ constexpr int kJoin = kMaxCtas / kGroup;
 constexpr float kUp8 = 12.f;      // over codes, weights are up to 2^12 when m is set, and stay
 constexpr float kMost8 = 32768.f; // up to this with it
 constexpr float kNone = -3e38f;   // m before there is one: any weight from it is too large
+constexpr float kNear = 64.f;     // pages whose value scales lie within this share a product: they have 2^-6 of f16's range at the least
 
 // Cell: what the cache holds, T or codes of 8 bits
 template <class T, class Cell, int DP, int RB>
@@ -99,10 +102,11 @@ struct Shape {
   static_assert(!MM || NT * R * (DP + 8) * 2 <= ACC, "queries pass through the joining buffers");
 };
 
+constexpr int kMore = 2;
 template <int PIECES>
 struct Stage {          // what the producer says of a tile
   int have[PIECES];     // keys of each piece that the call may use
-  int full;             // all of them
+  int full;             // all of them (1); of codes also: the tile comes once more, with its other pieces (kMore)
   float ks[PIECES], vs[PIECES];  // their scales, of codes
 };
 
@@ -479,41 +483,55 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
         }
         const int have = __shfl_sync(~0u, have32, in32 + (lane & pieces - 1));
         const int y = __shfl_sync(~0u, y32, in32 + (lane & pieces - 1));
-        const unsigned live = __ballot_sync(~0u, lane < pieces && have > 0);
-        const bool whole = __all_sync(~0u, have == BR);
-        if (!*(volatile int*)&dead && !wait(su32(&empty_bar[s]), ph)) dead = 1;
-        __syncwarp();
-        const bool go = !*(volatile int*)&dead;
-        if constexpr (!S::EIGHT) {
-          if (lane < pieces) stage[s].have[lane] = have;
-          if (lane == 0) stage[s].full = whole;
+        // The pieces that the stage has: all that are there; over codes those of similar value scales (as their products share one,
+        // and a row may not see, or hardly, the page that has the largest), and the others in stages of their own behind it
+        unsigned live = __ballot_sync(~0u, lane < pieces && have > 0);
+        bool whole = __all_sync(~0u, have == BR), again;
+        do {
+          again = false;
+          if (!*(volatile int*)&dead && !wait(su32(&empty_bar[s]), ph)) dead = 1;
           __syncwarp();
-        }
-        if (lane == 0) mbar_arrive_expect_tx(su32(&full_bar[s]), go ? __popc(live) * 2 * BR * DP * S::E : 0);
-        __syncwarp();
-        const uint32_t dst = su32(smem + s * 2 * S::TILE);
-        const int boxes = pieces * S::NCH * 2, j = lane & pieces - 1;  // box i: piece i % pieces, column and pool i / pieces
-        for (int i = lane; i < boxes; i += 32) {
-          const int c = (i >> log_pc) % S::NCH, v = (i >> log_pc) / S::NCH;
-          if (go && (live >> j & 1))
-            copy_box(dst + v * S::TILE + c * TK * S::COL + j * BR * S::COL, v ? &mv : &mk, c * S::CH, y, su32(&full_bar[s]));
-        }
-        if constexpr (S::EIGHT) {
-          const float ks = __shfl_sync(~0u, ks32, in32 + (lane & pieces - 1)), vs = __shfl_sync(~0u, vs32, in32 + (lane & pieces - 1));
-          if (lane < pieces) {
-            stage[s].have[lane] = have;
-            stage[s].ks[lane] = ks;
-            stage[s].vs[lane] = vs;
+          const bool go = !*(volatile int*)&dead;
+          if constexpr (!S::EIGHT) {
+            if (lane < pieces) stage[s].have[lane] = have;
+            if (lane == 0) stage[s].full = whole;
+            __syncwarp();
           }
-          if (lane == 0) stage[s].full = whole;
+          if (lane == 0) mbar_arrive_expect_tx(su32(&full_bar[s]), go ? __popc(live) * 2 * BR * DP * S::E : 0);
           __syncwarp();
-          if (lane == 0) mbar_arrive(su32(&full_bar[s]));
-        }
-        __syncwarp();
-        if (++s == ST) {
-          s = 0;
-          ph ^= 1;
-        }
+          const uint32_t dst = su32(smem + s * 2 * S::TILE);
+          const int boxes = pieces * S::NCH * 2, j = lane & pieces - 1;  // box i: piece i % pieces, column and pool i / pieces
+          for (int i = lane; i < boxes; i += 32) {
+            const int c = (i >> log_pc) % S::NCH, v = (i >> log_pc) / S::NCH;
+            if (go && (live >> j & 1))
+              copy_box(dst + v * S::TILE + c * TK * S::COL + j * BR * S::COL, v ? &mv : &mk, c * S::CH, y, su32(&full_bar[s]));
+          }
+          if constexpr (S::EIGHT) {
+            const float ks = __shfl_sync(~0u, ks32, in32 + (lane & pieces - 1)), vs = __shfl_sync(~0u, vs32, in32 + (lane & pieces - 1));
+            bool taken = live >> j & 1;  // with the largest scale among its warp's keys that no stage has had
+            if (BR < S::KW) {
+              float top = taken ? fabsf(vs) : 0.f;
+              for (int d = 1; BR * d < S::KW; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+              taken = taken && (vs == 0.f || !(fabsf(vs) * kNear < top));  // the largest at the least, whatever the scales hold
+              live &= ~__ballot_sync(~0u, taken);
+              again = (live & ((1u << pieces) - 1)) != 0;
+            }
+            if (lane < pieces) {
+              stage[s].have[lane] = taken ? have : 0;
+              stage[s].ks[lane] = ks;
+              stage[s].vs[lane] = taken ? vs : 0.f;
+            }
+            if (lane == 0) stage[s].full = again ? kMore : whole;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(su32(&full_bar[s]));
+          }
+          __syncwarp();
+          if (++s == ST) {
+            s = 0;
+            ph ^= 1;
+          }
+          whole = false;
+        } while (S::EIGHT && again);
       }
       x = next;
     }
@@ -673,14 +691,15 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       l[r] = 0.f;
     }
 
-    for (int k = k0; k < k1; ++k) {
+    for (int k = k0; k < k1;) {
       if (!*(volatile int*)&dead && !wait(su32(&full_bar[s]), ph)) dead = 1;
       __syncwarp();
       timed_out = timed_out || *(volatile int*)&dead;
       const uint32_t kt = su32(smem + s * 2 * S::TILE), vt = kt + S::TILE;
       const Stage<S::PIECES>& sg = stage[s];
       const int from = (WIN && k >= w.st ? k + gap : k) * TK;  // the tile's first key
-      const bool clean = sg.full && (listed || (from + TK <= lim_min && (!WIN || from >= lim_max - p.window || from + TK <= p.sinks)));
+      k += S::EIGHT && !timed_out ? sg.full != kMore : 1;
+      const bool clean = sg.full == 1 && (listed || (from + TK <= lim_min && (!WIN || from >= lim_max - p.window || from + TK <= p.sinks)));
       // a key of the tile that row r of the lane's may not use; keys whose values have to be 0, as no row uses them
       auto hidden = [&](int j, int r) {
         return (j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && from + j >= lim[r]) ||

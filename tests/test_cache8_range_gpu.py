@@ -1,0 +1,115 @@
+"""Values, scales and page numbers at the ends of what the cache in 8 bits and attention with a window take, on the GPU
+against 64 bits.
+
+Tolerance of attention, from the arithmetic (u: half a unit in the last place of the outputs' type):
+  a logit errs by d as in cache8_ref; a weight by 2 d + 2^-19 relative and, of n terms, n 2^-24.
+  rows (few per key): a weight is two f16 halves, 2^-20 of it at the most and half a step of the second one, 2^-25, where the
+  row's largest is 2^12 at the least: 2^-37 of that, or all of it where it is less.  Up to 2^6 times that where pages that differ
+  no more than so share one product: 2^-31, and twice for two roundings.
+  tiles (many rows): a weight times its page's value scale has 11 bits, and half a step of f16, 2^-25, where the row's
+  largest such product is 2^8 at the least: 2^-33 of that, and twice; rows taken again have less.
+Times |v| of its own key, summed, plus one rounding to the type."""
+import math
+
+import pytest
+import torch
+
+import decoder_ref as ref
+from test_cache8_gpu import BF16, F16, F32, Held, ints, pp, tables  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(q, k, v, table, starts, lens, scale, window, sinks, rows, key_bits=33):
+    """(out, lse, tolerance of out, tolerance of lse) in float64; k, v [pages][H][page][D] in float64."""
+    T, Hq, D = q.shape
+    pages, H, page, _ = k.shape
+    G, dt = Hq // H, q.dtype
+    out, tol = torch.zeros((T, Hq, D), dtype=torch.float64), torch.full((T, Hq, D), ref.TINY[dt], dtype=torch.float64)
+    lse, tl = torch.full((T, Hq), -math.inf, dtype=torch.float64), torch.zeros((T, Hq), dtype=torch.float64)
+    for t, (b, n) in enumerate(ref.seen_keys(T, starts, lens, True)):
+        key = torch.arange(n)
+        key = key[(key >= n - window) | (key < sinks)]
+        ip, io = table[b, key // page].long(), key % page
+        good = (ip >= 0) & (ip < pages)
+        ip, io = ip[good], io[good]
+        if not len(ip):
+            continue
+        for h in range(H):
+            kk, vv, hs = k[ip, h, io], v[ip, h, io], slice(h * G, (h + 1) * G)
+            x = q[t, hs].double()
+            s = scale * (x @ kk.T)
+            d = scale * (x.abs() @ kk.abs().T).amax(-1, keepdim=True) * ((D + 12) * 2.0 ** -24 + 2.0 ** -key_bits)
+            d = d + scale * 2.0 ** -39 * (x.abs().amax(-1, keepdim=True) * kk.abs().sum(-1)).amax(-1, keepdim=True)
+            p = torch.softmax(s, -1)
+            rel = 2 * d + 2.0 ** -19 + len(ip) * 2.0 ** -24 + (2.0 ** -20 if rows else 2.0 ** -11)
+            out[t, hs], lse[t, hs] = p @ vv, torch.logsumexp(s, -1)
+            if rows:
+                lost = torch.minimum(p, 2.0 ** -30 * p.amax(-1, keepdim=True)) @ vv.abs()
+            else:
+                y = p * vv.abs().amax(-1)
+                lost = torch.minimum(y, 2.0 ** -32 * y.amax(-1, keepdim=True)).sum(-1, keepdim=True)
+            tol[t, hs] += rel * (p @ vv.abs()) + lost + ref.UNIT[dt] * out[t, hs].abs() * 1.01
+            tl[t, hs] = d[:, 0] + 2.0 ** -19 + len(ip) * 2.0 ** -24 + 2.0 ** -22 * lse[t, hs].abs()
+    return out, lse, tol, tl
+
+
+def close(got, want, tol):
+    """Within tolerances, row by row: what is finite there is finite here."""
+    got = got.double().cpu()
+    worst = float(((got - want).abs() / tol).max())
+    assert torch.isfinite(got).all() and worst <= 1, worst
+
+
+def over_codes(pp, dt, H, G, D, page, L, n, window, sinks, change, rows, seed=0, status=0, q=None):
+    """One call over a cache in 8 bits that `change(h, table)` has changed on the CPU."""
+    need = -(-L // page)
+    h = Held(pp, need + 2, H, page, D, dt, seed)
+    table = tables([L], page, need + 2, seed=seed)
+    change(h, table)
+    for i in range(2):
+        h.dc[i].copy_(h.c[i])
+        h.ds[i].copy_(h.s[i])
+    k, v = h.values()
+    starts = None if n == 1 else [0, n]
+    if q is None:
+        q = torch.randn((n, H * G, D), generator=torch.Generator().manual_seed(seed + 1)).to(dt)
+    out, lse = torch.full((n, H * G, D), math.nan, device="cuda", dtype=dt), torch.full((n, H * G), math.nan, device="cuda")
+    try:
+        pp.pp_attn_window(h.cache, q.cuda(), None if starts is None else ints(starts).cuda(), table.cuda(), ints([L]).cuda(), 0.125,
+                          pp.PP_ATTN_CAUSAL, window, sinks, out, lse)
+        assert h.status() == status
+        want, wl, tol, tl = attend(q, k, v, table, starts, [L], 0.125, window, sinks, rows)
+        close(out, want, tol)
+        seen = torch.isfinite(wl)
+        close(lse.cpu()[seen], wl[seen], tl[seen])
+    finally:
+        h.close()
+
+
+# ------------------------------------------------------------------ pages of 8 and 16: several value scales in one product
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("page", [8, 16, 32])
+@pytest.mark.parametrize("power", [3, 5, 20, 40, 90])
+@pytest.mark.parametrize("where", ["ahead", "left", "faint"])
+def test_a_page_of_large_values_beside_small_ones(pp, dt, page, power, where):
+    """Values 2^power times as large on a page that a draft's last token begins and those before it do not see; that windows have
+    left but the first token's; that all see, with weights of some 2^-73.  Other pages are their neighbours in one tile."""
+    D, L, n, window = 64, 13 * page + 1, 6, 1000
+    if where == "left":
+        n, window = 2, 8 * page  # the first token's window begins with the last key of page 4
+        L = 13 * page
+    if where == "faint":
+        n = 1
+    q = (1 + 0.1 * torch.randn((n, 4, D), generator=torch.Generator().manual_seed(2))).to(dt)
+
+    def change(h, table):
+        for i in range(2):  # (scores near 0, so that every key counts)
+            h.s[i] *= 0.02 if i == 0 else 1
+        id = int(table[0, {"ahead": 13, "left": 4, "faint": 5}[where]])
+        h.s[1][id] *= 2.0 ** power
+        if where == "faint":
+            h.c[0][id], h.s[0][id] = -127, 0.05
+
+    over_codes(pp, dt, 1, 4, D, page, L, n, window, 0, change, True, q=q)
