@@ -662,7 +662,8 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  * all their bits.  A weight is two f16 halves (few rows per key: down to 2^-14 of the row's largest, those below 2^-36 are
  * 0; in pages of 8 and 16 down to 2^-8, below 2^-30 0) or, times its page's value scale over the largest that the tokens near
  * by see, one of 11 bits (many tokens in 16 bits: down to 2^-22 of the row's largest such product, below 2^-33 0).  Scales
- * are finite and not negative.
+ * are finite and not negative, up to the largest that values have; beside value scales above 2^70 that a token or its
+ * neighbours see, products with those below 2^-71 have fewer bits (few rows per key).
  * A weight's product with v takes the weight in fp32 (fp32), as two 16-bit halves (16 bits, few rows
  * per key), or rounded to the type (16 bits, many tokens: 11 bits in f16, 8 in bf16).  f16 weights
  * below 2^-27 of the row's largest have fewer bits, and those below 2^-38 are 0 there.

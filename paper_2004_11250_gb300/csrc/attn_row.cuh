@@ -102,11 +102,15 @@ struct Shape {
   static_assert(!MM || NT * R * (DP + 8) * 2 <= ACC, "queries pass through the joining buffers");
 };
 
-constexpr int kMore = 2;
+constexpr int kMore = 2, kTurn = 4;
+// Sums over codes are of values as they are.  With scales up to this none of up to 2^31 weights of 2^15 leaves fp32; where a unit of rows
+// meets larger ones, its sums go on as multiples of 2^51 (the largest scales come to 2^70 then)
+constexpr float kHuge = 0x1p70f, kLess = 0x1p-51f;
 template <int PIECES>
 struct Stage {          // what the producer says of a tile
   int have[PIECES];     // keys of each piece that the call may use
-  int full;             // all of them (1); of codes also: the tile comes once more, with its other pieces (kMore)
+  int full;             // all of them (1); of codes also: the tile comes once more, with its other pieces (kMore); from here on the
+                        // scales, and the unit's sums, are multiples of 2^51 (kTurn)
   float ks[PIECES], vs[PIECES];  // their scales, of codes
 };
 
@@ -241,6 +245,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
   // keys with values that are not finite, a bit each: 16 from lim_min on, and 16 from the first row's window on
   __shared__ unsigned unfit;
   [[maybe_unused]] __shared__ float row_scale[kRows];
+  [[maybe_unused]] __shared__ int turned[kWarps];  // where the unit ends whose sums a warp has as multiples of 2^51
   __shared__ Walk found;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int NI = p.sel ? p.T : p.B;
@@ -249,6 +254,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
     dead = 0;
+    for (int i = 0; i < kWarps; ++i) turned[i] = -1;
     for (int i = 0; i < ST; ++i) {
       mbar_init(su32(&full_bar[i]), S::EIGHT ? 2 : 1);  // the copies, and the scales
       mbar_init(su32(&empty_bar[i]), kWarps);
@@ -441,6 +447,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
         low = limit_of(r0) - p.window;
       }
       int have32 = 0, y32 = 0;
+      [[maybe_unused]] bool huge = false;
       [[maybe_unused]] float ks32 = 0.f, vs32 = 0.f;
       for (int k = k0; k < k1; ++k) {
         const int in32 = (k - k0) << log_pc & 31;  // the tile's first piece among the 32
@@ -507,7 +514,10 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
               copy_box(dst + v * S::TILE + c * TK * S::COL + j * BR * S::COL, v ? &mv : &mk, c * S::CH, y, su32(&full_bar[s]));
           }
           if constexpr (S::EIGHT) {
-            const float ks = __shfl_sync(~0u, ks32, in32 + (lane & pieces - 1)), vs = __shfl_sync(~0u, vs32, in32 + (lane & pieces - 1));
+            const float ks = __shfl_sync(~0u, ks32, in32 + (lane & pieces - 1)), all = __shfl_sync(~0u, vs32, in32 + (lane & pieces - 1));
+            const bool turn = !huge && __any_sync(~0u, all > kHuge);
+            huge = huge || turn;
+            const float vs = huge ? all * kLess : all;
             bool taken = live >> j & 1;  // with the largest scale among its warp's keys that no stage has had
             if (BR < S::KW) {
               float top = taken ? fabsf(vs) : 0.f;
@@ -521,7 +531,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
               stage[s].ks[lane] = ks;
               stage[s].vs[lane] = taken ? vs : 0.f;
             }
-            if (lane == 0) stage[s].full = again ? kMore : whole;
+            if (lane == 0) stage[s].full = (again ? kMore : whole) | (turn ? kTurn : 0);
             __syncwarp();
             if (lane == 0) mbar_arrive(su32(&full_bar[s]));
           }
@@ -698,8 +708,8 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       const uint32_t kt = su32(smem + s * 2 * S::TILE), vt = kt + S::TILE;
       const Stage<S::PIECES>& sg = stage[s];
       const int from = (WIN && k >= w.st ? k + gap : k) * TK;  // the tile's first key
-      k += S::EIGHT && !timed_out ? sg.full != kMore : 1;
-      const bool clean = sg.full == 1 && (listed || (from + TK <= lim_min && (!WIN || from >= lim_max - p.window || from + TK <= p.sinks)));
+      k += S::EIGHT && !timed_out ? !(sg.full & kMore) : 1;
+      const bool clean = (S::EIGHT ? sg.full & 1 : sg.full) && (listed || (from + TK <= lim_min && (!WIN || from >= lim_max - p.window || from + TK <= p.sinks)));
       // a key of the tile that row r of the lane's may not use; keys whose values have to be 0, as no row uses them
       auto hidden = [&](int j, int r) {
         return (j & (BR - 1)) >= sg.have[j >> log_br] || (!listed && from + j >= lim[r]) ||
@@ -795,7 +805,9 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
               x[z][rb][e] = ex2(x[z][rb][e]);
               top = fmaxf(top, x[z][rb][e]);
             }
-        if (__builtin_expect(__any_sync(~0u, top > kMost8), 0)) {
+        const bool turn = sg.full & kTurn;
+        if (__builtin_expect(__any_sync(~0u, top > kMost8) || turn, 0)) {
+          if (turn && lane == 0) turned[warp] = next;
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
             float mx = -INFINITY;
@@ -819,8 +831,8 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
               for (int i = 0; i < 2; ++i) x[z][r >> 1][2 * i + (r & 1)] = ex2(__fadd_rn(sc[z][r >> 1][2 * i + (r & 1)], -to));
 #pragma unroll
             for (int i = 0; i < NO; ++i) {
-              o[r >> 1][i][r & 1] *= f;
-              o[r >> 1][i][2 + (r & 1)] *= f;
+              o[r >> 1][i][r & 1] *= turn ? f * kLess : f;
+              o[r >> 1][i][2 + (r & 1)] *= turn ? f * kLess : f;
             }
           }
         }
@@ -1044,6 +1056,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       }
     }
     group_sync<kWarps * 32>();
+    [[maybe_unused]] float grain = S::EIGHT && turned[warp] == next ? 1.f / kLess : 1.f;  // what 1 of the sums is (every warp met the turn)
     float f[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -1118,7 +1131,8 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
         const int r = i / (p.D / 4), d = i % (p.D / 4) * 4;
         const float4 v = *reinterpret_cast<const float4*>(acc + r * S::AS + d);
         const float n = rl[r] > 0.f || rl[r] != rl[r] ? 1.f / rl[r] : 0.f;
-        Vec<T, 4> y = {from_f32<T>(v.x * n), from_f32<T>(v.y * n), from_f32<T>(v.z * n), from_f32<T>(v.w * n)};
+        const float to = S::EIGHT ? grain : 1.f;
+        Vec<T, 4> y = {from_f32<T>(v.x * n * to), from_f32<T>(v.y * n * to), from_f32<T>(v.z * n * to), from_f32<T>(v.w * n * to)};
         T* dst = static_cast<T*>(p.out) +
                  ((int64_t)(w.t0 + p.G.div(r0 + r)) * p.H * p.G.d + h * p.G.d + p.G.mod(r0 + r)) * p.D + d;
         if (wide) {
@@ -1140,6 +1154,8 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       auto slot = [&](int part) {
         return p.partial + (int64_t)(part == 0 ? 2 * c0 + 1 : 2 * (c0 + part)) * S::PART;
       };
+      constexpr int kGrain = kRows * DP + kRows - 1;  // (over codes there are 8 rows, and the last maximum's place is free)
+      static_assert(!S::EIGHT || R < kRows, "the grain's place");
       auto store = [&](float* to) {
         for (int i = tid; i < nrows * (DP / 4); i += kWarps * 32) {
           const int r = i / (DP / 4), d = i % (DP / 4) * 4;
@@ -1149,6 +1165,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
           __stcg(to + kRows * DP + tid, rm[tid]);
           __stcg(to + kRows * DP + kRows + tid, rl[tid]);
         }
+        if (S::EIGHT && tid == 0) __stcg(to + kGrain, grain);
       };
       // the last of `of` to come here; what the others stored is then there to read
       // (one thread's release behind the barrier is every thread's)
@@ -1165,11 +1182,15 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
       };
       // n parts, step apart, into acc, rm and rl: in their order, whoever comes last
       auto join = [&](int part, int n, int step) {
+        // over codes in the parts' largest grain: what the sums of one count there
+        auto in_grain = [&](float c, float of) { return S::EIGHT && grain != of ? c * kLess : c; };
         if (EX > 0 && R <= 8 && n <= kGroup) {  // 16 lanes to a row, a part each
           const int r = tid / kGroup, i = tid % kGroup;
           const bool in = r < nrows && i < n;
           const float* from = slot(part + (in ? i : 0) * step) + kRows * DP + (in ? r : 0);
           const float pm = in ? __ldcg(from) : -INFINITY, pl = in ? __ldcg(from + kRows) : 0.f;
+          const float of = S::EIGHT && i < n ? __ldcg(slot(part + i * step) + kGrain) : 1.f;
+          if constexpr (S::EIGHT) grain = __any_sync(~0u, of != 1.f) ? 1.f / kLess : 1.f;  // (a warp has every part)
           float mx = pm;
 #pragma unroll
           for (int d = 1; d < kGroup; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, d));
@@ -1177,7 +1198,7 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
           float sum = c * pl;  // NaN stays NaN
 #pragma unroll
           for (int d = 1; d < kGroup; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-          if (in) wts[r][i] = c;
+          if (in) wts[r][i] = in_grain(c, of);
           if (i == 0 && r < nrows) {
             rm[r] = mx;
             rl[r] = sum;
@@ -1190,13 +1211,18 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
             sums[i % kRows][i / kRows] = __ldcg(from + kRows);
           }
         }
+        if constexpr (S::EIGHT) {
+          bool any = false;
+          for (int i = lane; i < n; i += 32) any = any || __ldcg(slot(part + i * step) + kGrain) != 1.f;
+          grain = __any_sync(~0u, any) ? 1.f / kLess : 1.f;
+        }
         group_sync<kWarps * 32>();
         if (tid < nrows) {
           float mx = -INFINITY, sum = 0.f;
           for (int i = 0; i < n; ++i) mx = fmaxf(mx, wts[tid][i]);
           for (int i = 0; i < n; ++i) {
             const float c = wts[tid][i] == -INFINITY ? 0.f : ex2(wts[tid][i] - mx);
-            wts[tid][i] = c;
+            wts[tid][i] = S::EIGHT ? in_grain(c, __ldcg(slot(part + i * step) + kGrain)) : c;
             sum += c * sums[tid][i];  // NaN stays NaN
           }
           rm[tid] = mx;

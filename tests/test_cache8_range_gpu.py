@@ -113,3 +113,34 @@ def test_a_page_of_large_values_beside_small_ones(pp, dt, page, power, where):
             h.c[0][id], h.s[0][id] = -127, 0.05
 
     over_codes(pp, dt, 1, 4, D, page, L, n, window, 0, change, True, q=q)
+
+
+# ------------------------------------------------------------------ values up to the largest of the type
+
+def of_scales(powers):
+    """Value scales of 2^(e - 1) to 2^e, with e from `powers` in turn along the pages, and codes from 0 on: sums of many large values."""
+    def change(h, table):
+        h.c[1].abs_()
+        for w in range(table.shape[1]):
+            id = int(table[0, w])
+            h.s[1][id] = (0.5 + h.s[1][id] / h.s[1].max() / 2) * 2.0 ** powers[w % len(powers)]
+    return change
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("page", [8, 64])
+@pytest.mark.parametrize("L,n", [(40, 1), (700, 1), (9000, 1), (90, 5), (400, 40)])
+@pytest.mark.parametrize("powers", [[100], [110], [120], [70, 71, 69], [120, 120, 120, 120, 120, 120, 120, 120, 0], [-60, -60, 120], [-106], [-140], [-60] * 100 + [120] * 41])
+def test_values_of_any_size_by_rows(pp, dt, page, L, n, powers):
+    """Outputs are averages of values up to 2^127, and sums of many such pass every type.  Short, split over CTAs, joined in two
+    levels, drafts, and a chunk on few rows' kernel (one head)."""
+    over_codes(pp, dt, 1, 2, 64, page, L, n, 10 ** 6, 0, of_scales(powers), True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_values_of_any_size_that_others_see(pp, dt):
+    """A draft's last token brings values near the type's largest: those before it are as if they were not there."""
+    for page in (8, 16, 64):
+        def change(h, table):
+            h.s[1][int(table[0, 3])] = 2.0 ** 120
+        over_codes(pp, dt, 1, 4, 64, page, 3 * page + 1, 5, 10 ** 6, 0, change, True)
