@@ -682,7 +682,8 @@ pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q
  * `window` (its own among them) and the first `sinks`.  Over either kind of cache.  Pages between the first keys and
  * the windows of a call's tokens are not read, and their entries of the table not looked at (they may be -1, and
  * the pages in use elsewhere); a window of width * page keys or more gives pp_attn_forward's bits.  f16 weights of many tokens
- * have 11 bits down to 2^-24 of the row's largest, and are 0 below 2^-35.
+ * have 11 bits down to 2^-24 of the row's largest, and are 0 below 2^-35. (bf16 over a cache in bf16: 8 bits
+ * down to 2^-85, and 0 below; values may be as large as the type's largest).
  * Errors: as pp_attn_forward; also window < 1, sinks < 0.
  */
 pp_status pp_attn_window(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,

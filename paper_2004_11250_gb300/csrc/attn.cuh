@@ -54,8 +54,9 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* m, int
 // Their sum is of the same weights, so m need not be the largest for it.
 template <class T, int UP>
 constexpr float kLift = std::is_same<T, __half>::value ? (float)UP : 0.f;
-// x - n, no less than that: beyond 2^24 fp32 holds no difference of n, and a weight must not pass its bound
-__device__ __forceinline__ float lower(float x, float n) { return __fadd_ru(x, -n); }
+// x - n, no less than that: beyond 2^24 fp32 holds no difference of n, and a weight must not pass its bound.  (No more than that
+// where n is below 0, or there no weight would be left)
+__device__ __forceinline__ float lower(float x, float n) { return n < 0.f ? __fadd_rd(x, -n) : __fadd_ru(x, -n); }
 // log of a row's sum `l` of weights taken from m
 template <class T, int UP>
 __device__ __forceinline__ float log_sum(float m, float l) {

@@ -59,9 +59,13 @@ constexpr int kMaskWords = 2048;       // token bits of the pages in one window
 constexpr int kAhead = 8;              // entries of the tokens' lists in flight per thread
 constexpr int kSplits = 8;             // shares of a tile's blocks at most
 constexpr int kUp = 13;                // f16 weights are up to 2^13 where m is not behind, and 2^2 times that
-constexpr int kUpWindow = 10;          // with a window, up to this when m is set, and while 8 of them
+// With a window, weights are up to 2^kUpWindow when m is set, and m stays while 8 of them sum up to kMostWindow: in f16 its largest
+// number; in bf16, which has fp32's exponents, so little that the weights of 2^31 keys sum up to less than 1 and their products
+// with the largest values stay within fp32 (there weights down to 2^-85 of the row's largest have their 8 bits, and those below are 0)
 template <class T>
-constexpr float kMostWindow = std::is_same<T, __half>::value ? 65504.f : 0x1p64f;  // sum up to this with it
+constexpr float kUpWindow = std::is_same<T, __half>::value ? 10.f : -41.f;
+template <class T>
+constexpr float kMostWindow = std::is_same<T, __half>::value ? 65504.f : 0x1p-30f;
 template <class T>
 constexpr float kGrow = std::is_same<T, __half>::value ? 2.f : 8.f;  // log2 of how far a row's weights may pass their bound
 
@@ -78,6 +82,13 @@ struct Block {          // what the copying warp says of a block
   int end;   // 1 + which of the last blocks, with keys that some tokens see and others do not (from 1 + kEnds on: of those where
              // the windows begin); 0: none of them
 };
+
+// log of a row's sum `l` of weights taken from m
+template <class T>
+__device__ __forceinline__ float log_of(bool window, float m, float l) {
+  constexpr float n = kUpWindow<T>;
+  return n < 0.f && window ? (m + n) * 0.693147181f + logf(l * 0x1p41f) : log_sum<T, kUp>(m, l);
+}
 
 // One row's attention over its selected pages, by one warp, 4 keys at a time: of a row whose product met a value that is not
 // finite, on a page of the tile's union that may not be its own.  A lane has 4 of the row's values.
@@ -171,7 +182,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
     attn_tile_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap mk,
                      const __grid_constant__ CUtensorMap mv) {
   using S = TileShape<DP>;
-  constexpr int UP = WIN ? kUpWindow : kUp, ARRIVALS = WIN ? 4 : kSoft;
+  constexpr int ARRIVALS = WIN ? 4 : kSoft;
   constexpr int CHUNK_Q = kRowsT * 128, CHUNK_KV = kKeys * 128;  // bytes of 64 values of every row
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -595,7 +606,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
 #pragma unroll
             for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
           }
-          const float mx = see ? lower(__fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl), kLift<T, UP>) : -INFINITY;
+          const float most = __fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl);
+          const float mx = !see ? -INFINITY : WIN ? lower(most, kUpWindow<T>) : lower(most, kLift<T, kUp>);
           const bool grow = mx > __fadd_rd(m, kGrow<T>);  // from -infinity, too
           if (__any_sync(~0u, grow)) {
             const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
@@ -733,7 +745,7 @@ __global__ void __launch_bounds__(kThreadsT, 2)
           }
         }
       }
-      if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : log_sum<T, kUp>(m, l);
+      if (p.lse && live_row) p.lse[cell] = l == 0.f ? -INFINITY : log_of<T>(WIN, m, l);
       unsigned again = __ballot_sync(~0u, odd && live_row && p.sel);
       __syncwarp();  // what the rows' own threads wrote lies before what the warp writes over it
       for (; again; again &= again - 1) {
@@ -823,7 +835,7 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
       for (int e = 0; e < 4; ++e) out[d + e] = y.v[e];
     }
   }
-  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : log_sum<T, kUp>(m, l);
+  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : log_of<T>(!p.ks && p.window < p.width * p.page, m, l);
 }
 
 template <class T, int DP>

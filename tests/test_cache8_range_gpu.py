@@ -54,6 +54,25 @@ def attend(q, k, v, table, starts, lens, scale, window, sinks, rows, key_bits=33
     return out, lse, tol, tl
 
 
+def in_bf16(q, k, v, table, starts, lens, scale, window, sinks):
+    """The same for one sequence over a cache in bf16, all keys at once on the GPU: weights of many rows have 8 bits."""
+    n, Hq, D = q.shape
+    _, H, page, _ = k.shape
+    L, ids = lens[0], table[0].long()
+    kk, vv = (x[ids].transpose(1, 2).reshape(-1, H, D)[:L].double().cuda() for x in (k, v))
+    x = q.double().cuda().view(n, H, Hq // H, D)
+    seen, at = torch.arange(L - n + 1, L + 1, device="cuda")[:, None], torch.arange(L, device="cuda")[None]
+    hide = ((at >= seen) | ((at < seen - window) & (at >= sinks)))[:, None, None]
+    s = (torch.einsum("nhgd,shd->nhgs", x, kk) * scale).masked_fill(hide, -math.inf)
+    d = torch.einsum("nhgd,shd->nhgs", x.abs(), kk.abs()).masked_fill(hide, 0).amax(-1, keepdim=True) * scale * (D + 12) * 2.0 ** -24
+    p = torch.softmax(s, -1)
+    out, mag = (torch.einsum("nhgs,shd->nhgd", p, y) for y in (vv, vv.abs()))
+    tol = (2 * d + 2.0 ** -19 + L * 2.0 ** -24 + 2.0 ** -8) * mag + ref.UNIT[q.dtype] * out.abs() * 1.01 + ref.TINY[q.dtype]
+    lse = torch.logsumexp(s, -1)
+    tl = d[..., 0] + 2.0 ** -19 + L * 2.0 ** -24 + 2.0 ** -22 * lse.abs()
+    return [y.reshape(n, Hq, *y.shape[3:]).cpu() for y in (out, lse, tol, tl)]
+
+
 def close(got, want, tol):
     """Within tolerances, row by row: what is finite there is finite here."""
     got = got.double().cpu()
@@ -144,3 +163,32 @@ def test_values_of_any_size_that_others_see(pp, dt):
         def change(h, table):
             h.s[1][int(table[0, 3])] = 2.0 ** 120
         over_codes(pp, dt, 1, 4, 64, page, 3 * page + 1, 5, 10 ** 6, 0, change, True)
+
+
+@pytest.mark.parametrize("H,G,n,L,window,sinks", [(8, 2, 64, 500, 300, 0), (8, 4, 40, 1500, 1000, 40), (16, 1, 256, 700, 690, 3), (2, 4, 128, 9000, 8000, 0)])
+@pytest.mark.parametrize("power", [0, 90, 110, 120, 127])
+@pytest.mark.parametrize("rise", [0, 7, 20, 58, -58])
+def test_windows_over_values_of_any_size_by_tiles(pp, H, G, n, L, window, sinks, power, rise):
+    """Chunks in bf16 whose scores rise (or fall) along the keys by so many powers of two, over values near the type's largest:
+    outputs are averages of them."""
+    D, page, dt = 64, 64, BF16
+    g = torch.Generator().manual_seed(5)
+    pages = -(-L // page)
+    table = tables([L], page, pages)
+    k, v = torch.zeros((pages, H, page, D)), torch.zeros((pages, H, page, D))
+    at = torch.arange(pages * page).view(pages, 1, page, 1) / L * rise / (D * 0.125 * 1.4427)  # logits in powers of two: rise times the place
+    k[table[0].long()] = at + 0.02 * torch.randn((pages, H, page, D), generator=g)
+    v[table[0].long()] = (0.5 + 0.49 * torch.rand((pages, H, page, D), generator=g)) * 2.0 ** power
+    k, v, q = k.to(dt), v.to(dt), (1 + 0.1 * torch.randn((n, H * G, D), generator=g)).to(dt)
+    cache = pp.pp_cache_create(k.cuda(), v.cuda())
+    out, lse = torch.full((n, H * G, D), math.nan, device="cuda", dtype=dt), torch.full((n, H * G), math.nan, device="cuda")
+    try:
+        pp.pp_attn_window(cache, q.cuda(), ints([0, n]).cuda(), table.cuda(), ints([L]).cuda(), 0.125, pp.PP_ATTN_CAUSAL, window,
+                          sinks, out, lse)
+        assert pp.pp_cache_device_status(cache) == 0
+    finally:
+        torch.cuda.synchronize()
+        pp.pp_cache_destroy(cache)
+    want, wl, tol, tl = in_bf16(q, k, v, table, [0, n], [L], 0.125, window, sinks)
+    close(out, want, tol)
+    close(lse, wl, tl)
