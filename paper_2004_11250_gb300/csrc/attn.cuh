@@ -112,7 +112,7 @@ bool tile_applicable(const AttnParams& p, int dtype, int sms);
 cudaError_t tile_prepare();
 size_t tile_space(int dtype, int D, int sms);  // device bytes of the shares' sums
 cudaError_t tile_launch(AttnParams p, const pp_cache& c, int sms, cudaStream_t stream);
-cudaError_t tile_join(const AttnParams& p, int dtype, cudaStream_t stream);  // the shares' sums into the outputs
+cudaError_t tile_join(const AttnParams& p, int dtype, bool over, cudaStream_t stream);  // the shares' sums (over: each over its total) into the outputs
 // attn8_tile.cu: the same over codes, two tiles at a time; its shares' sums take the same space.
 bool tile8_applicable(const AttnParams& p, int dtype, int sms);
 cudaError_t tile8_prepare();

@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         const int key = lane < 8 && k < n ? key_of(k) + (lane * 8 & ~(run - 1)) : INT32_MAX;
         return key < lim_max && (key < p.sinks || key + run > low) ? table[key >> p.log_page] : INT32_MIN;
       };
-      const float vinv = vtop > 0.f ? 1.f / vtop : 0.f;
+      // 1 over the largest scale, in two steps, as it may lie beyond fp32: a power of two, and what is left
+      const float vup = __int_as_float((254 - min(max(__float_as_int(vtop) >> 23, 1), 253)) << 23), vinv = vtop > 0.f ? 1.f / (vtop * vup) : 0.f;
       int64_t cell = -1;
       float ks = 0.f, vs = 0.f;
       auto resolve = [&](int id) {
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         };
         copy(0, p.k);
         if (lane < 8) {
-          const float lv = vs > 0.f ? fmaxf(__log2f(vs * vinv), kLeastScale) : kLeastScale;
+          const float lv = vs > 0.f ? fmaxf(__log2f(vs * vup * vinv), kLeastScale) : kLeastScale;
           note.ks[lane] = ks;
           note.lv[lane] = lv;
           note.inv[lane] = ex2(-lv);
@@ -547,9 +548,8 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       tm_fence_after();
       const int64_t cell = (int64_t)(base + p.G.div(live_row ? tr : 0)) * p.H * p.G.d + h * p.G.d + p.G.mod(live_row ? tr : 0);
       const bool parts = p.splits > 1;
-      // (the joining kernel takes bf16's sums as not lifted)
-      const float lift = std::is_same<T, __half>::value ? 1.f : 1.f / (float)(1 << kUp);
-      const float scale = parts ? vtop * lift : l == 0.f ? 0.f : vtop / l;
+      // first over the total, then times the scale: together they may lie below fp32's numbers, and a share's sums beyond them
+      const float over = l == 0.f ? 0.f : 1.f / l;
       const int64_t at = (int64_t)z * p.T * p.H * p.G.d + cell;
       T* dst = static_cast<T*>(p.out) + cell * p.D;
       const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 15) == 0;
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         }
         if (!live_row) continue;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] *= scale;
+        for (int i = 0; i < 32; ++i) o[i] = o[i] * over * vtop;
         if (parts) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
         }
       }
       if (live_row) {
-        if (parts) p.split_stats[at] = make_float2(lift == 1.f ? m : m + (float)kUp, l * lift);
+        if (parts) p.split_stats[at] = make_float2(m, l);
         else if (p.lse) p.lse[cell] = l == 0.f ? -INFINITY : log_sum<__half, kUp>(m, l);
       }
     }
@@ -617,7 +617,7 @@ cudaError_t prepare_one() {
 template <class T, int DP>
 cudaError_t launch(const AttnParams& p, int64_t grid, cudaStream_t stream) {
   const cudaError_t e = launch_after(attn8_tile_kernel<T, DP>, dim3((unsigned)grid), kThreads8, Shape8<DP>::SMEM, stream, 1, p);
-  return e != cudaSuccess || p.splits == 1 ? e : tile_join(p, std::is_same<T, __half>::value ? PP_F16 : PP_BF16, stream);
+  return e != cudaSuccess || p.splits == 1 ? e : tile_join(p, std::is_same<T, __half>::value ? PP_F16 : PP_BF16, true, stream);
 }
 
 // Pairs of tiles of a call at most: each sequence adds at most one that is not full.

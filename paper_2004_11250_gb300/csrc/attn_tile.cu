@@ -786,8 +786,8 @@ __global__ void __launch_bounds__(kThreadsT, 2)
   }
 }
 
-// The splits' sums of a row into its output: a warp per (token, query head).
-template <class T, int DP>
+// The splits' sums of a row into its output: a warp per (token, query head).  OVER: each is over its own total already.
+template <class T, int DP, bool OVER>
 __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_constant__ AttnParams p) {
   after_previous();
   const int Hq = p.H * p.G.d, lane = threadIdx.x % 32;
@@ -800,14 +800,19 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
     st[z] = z < p.splits ? p.split_stats[z * cells + cell] : make_float2(-INFINITY, 0.f);
     m = fmaxf(m, st[z].x);
   }
+  if constexpr (OVER) {
+#pragma unroll
+    for (int z = 0; z < kSplits; ++z) l += st[z].y == 0.f ? 0.f : ex2(st[z].x - m) * st[z].y;
+  }
+  const float r = OVER && l != 0.f ? 1.f / l : 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const int d = lane * 4 < DP ? lane * 4 : 0;
 #pragma unroll
   for (int z = 0; z < kSplits; ++z) {
     if (st[z].y == 0.f) continue;
-    const float w = ex2(st[z].x - m);
+    const float w = ex2(st[z].x - m) * (OVER ? st[z].y * r : 1.f);
     const float4 a = *reinterpret_cast<const float4*>(p.split_sums + (z * cells + cell) * DP + d);
-    l += w * st[z].y;
+    if (!OVER) l += w * st[z].y;
     o.x += w * a.x;
     o.y += w * a.y;
     o.z += w * a.z;
@@ -825,7 +830,7 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
                 p.sel + ((int64_t)t * p.H + h) * p.keep, h, s.keys, p.scale * 1.44269504f, out, lse);
     return;
   }
-  const float n = l == 0.f ? 0.f : 1.f / l;
+  const float n = OVER ? 1.f : l == 0.f ? 0.f : 1.f / l;
   if (in) {
     const Vec<T, 4> y = {from_f32<T>(o.x * n), from_f32<T>(o.y * n), from_f32<T>(o.z * n), from_f32<T>(o.w * n)};
     if ((reinterpret_cast<uintptr_t>(p.out) & 7) == 0) {
@@ -835,7 +840,7 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(const __grid_consta
       for (int e = 0; e < 4; ++e) out[d + e] = y.v[e];
     }
   }
-  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : log_of<T>(!p.ks && p.window < p.width * p.page, m, l);
+  if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : log_of<T>(!OVER && p.window < p.width * p.page, m, l);
 }
 
 template <class T, int DP>
@@ -849,7 +854,7 @@ template <class T, int DP>
 cudaError_t launch(const AttnParams& p, const pp_cache& c, int64_t grid, cudaStream_t stream) {
   const cudaError_t e = launch_after(p.window < p.width * p.page ? attn_tile_kernel<T, DP, true> : attn_tile_kernel<T, DP, false>,
                                      dim3((unsigned)grid), kThreadsT, TileShape<DP>::SMEM, stream, 1, p, c.mk, c.mv);
-  return e != cudaSuccess || p.splits == 1 ? e : tile_join(p, c.dtype, stream);
+  return e != cudaSuccess || p.splits == 1 ? e : tile_join(p, c.dtype, false, stream);
 }
 
 }  // namespace
@@ -875,11 +880,15 @@ bool tile_applicable(const AttnParams& p, int dtype, int sms) {
   return p.sel ? std::max(tiles, few) * 4 < units : few < units && tiles * 8 <= units * 9;
 }
 
-cudaError_t tile_join(const AttnParams& p, int dtype, cudaStream_t stream) {
+cudaError_t tile_join(const AttnParams& p, int dtype, bool over, cudaStream_t stream) {
   const dim3 grid((unsigned)(((int64_t)p.T * p.H * p.G.d + 7) / 8));
   auto run = [&](auto kernel) { return launch_after(kernel, grid, 256, 0, stream, 1, p); };
-  return dtype == PP_F16 ? (p.D <= 64 ? run(attn_tile_join_kernel<__half, 64>) : run(attn_tile_join_kernel<__half, 128>))
-                         : (p.D <= 64 ? run(attn_tile_join_kernel<__nv_bfloat16, 64>) : run(attn_tile_join_kernel<__nv_bfloat16, 128>));
+  auto wide = [&](auto* t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    return p.D <= 64 ? run(over ? attn_tile_join_kernel<T, 64, true> : attn_tile_join_kernel<T, 64, false>)
+                     : run(over ? attn_tile_join_kernel<T, 128, true> : attn_tile_join_kernel<T, 128, false>);
+  };
+  return dtype == PP_F16 ? wide((__half*)nullptr) : wide((__nv_bfloat16*)nullptr);
 }
 
 cudaError_t tile_prepare() {

@@ -192,3 +192,24 @@ def test_windows_over_values_of_any_size_by_tiles(pp, H, G, n, L, window, sinks,
     want, wl, tol, tl = in_bf16(q, k, v, table, [0, n], [L], 0.125, window, sinks)
     close(out, want, tol)
     close(lse, wl, tl)
+
+
+# ------------------------------------------------------------------ tiles of rows over codes
+
+TILED = [(16, 8, 64, 16, 170, 48), (16, 4, 128, 64, 700, 100), (8, 8, 128, 64, 2100, 40)]  # H, G, D, page, length, tokens; the last is split
+
+
+@pytest.mark.parametrize("case", TILED)
+@pytest.mark.parametrize("powers", [[-20], [-100], [-125], [-130], [-140], [100], [120], [120, -120], [-106, -106, -106, 0]])
+@pytest.mark.parametrize("window", [10 ** 6, 70])
+def test_values_of_any_size_by_tiles(pp, case, powers, window):
+    H, G, D, page, L, n = case
+    over_codes(pp, BF16, H, G, D, page, L, n, window, 0, of_scales(powers), False)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+def test_scales_below_normal_numbers_by_tiles(pp, dt):
+    """The largest value scale in sight has no reciprocal in fp32."""
+    for H, G, D, page, L, n in TILED:
+        over_codes(pp, dt, H, G, D, page, L, n, 10 ** 6, 0, of_scales([-130]), False)
+        over_codes(pp, dt, H, G, D, page, L, n, 10 ** 6, 0, of_scales([-148]), False)
