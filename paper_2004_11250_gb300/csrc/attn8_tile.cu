@@ -51,7 +51,10 @@ constexpr int kInfo = 8;                          // blocks whose notes are kept
 constexpr int kSplits = 8;                        // shares of a tile's blocks at most
 constexpr int kUp = 8;                            // weights are up to 2^8 when m is set
 constexpr float kMost = 65504.f;                  // 8 weights' sum at most: f16's largest number
-constexpr float kLeastScale = -90.f;              // log2 of vs at the least: a row that sees no other pages has sums of P / vs below 2^121
+constexpr float kLeastScale = -90.f;              // log2 of vs at the least: a row that sees no other pages has sums of P / vs below 2^121.
+// One that has nearly all its weight on pages of less is computed again by itself: its sum is above 2^98 then, and where it is not
+// above this, the largest weight lies on a page of more, beside which what those pages add is some 2^-31
+constexpr float kSmallPages = 0x1p60f;
 
 template <int DP>
 struct Shape8 {
@@ -62,7 +65,7 @@ struct Shape8 {
 
 struct alignas(16) Note {           // of a block
   float ks[8], lv[8], inv[8];       // of each 8 keys: the keys' scale; log2 of the values' over the largest, and 1 over that
-  uint32_t valid;                   // a bit for each 8 keys that are there
+  uint32_t valid, zero;             // a bit for each 8 keys that are there; whose values are 0 as their scale is
 };
 
 // 16 codes as 16 f16 (attn_row.cuh has the same by bytes' parity)
@@ -77,6 +80,68 @@ __device__ __forceinline__ uint4 f16_of8(uint32_t a, uint32_t b) {
   return make_uint4(f16_pair(a, 0x4140), f16_pair(a, 0x4342), f16_pair(b, 0x4140), f16_pair(b, 0x4342));
 }
 
+// A row's attention over blocks of keys of its own, by one warp in fp32, 8 keys (of one page) at a time: o is the average so far of
+// the lane's 4 values, so that it is as large as they are.  For rows whose pages' value scales are too small beside others'
+// for the tile's weights; 125 cycles a key.
+struct Average {
+  float o[4], m, l;
+};
+template <class T>
+__device__ __noinline__ void row_again(const AttnParams& p, const T* q, const int* table, int h, int lim, int first, int n, int sink_blocks,
+                                       int gap, Average& y) {
+  const int d = threadIdx.x % 32 * 4;
+  const bool in = d < p.D;
+  float x[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = in && p.scale != 0.f ? to_f32(q[d + e]) : 0.f;
+    y.o[e] = 0.f;
+  }
+  y.m = -INFINITY;
+  y.l = 0.f;
+  for (int i = 0; i < n * (kKeys / 8); ++i) {
+    const int k = first + i / (kKeys / 8), key = ((k < sink_blocks ? k : k + gap) << kLogKeys) + i % (kKeys / 8) * 8;
+    if (key >= lim || (key >= p.sinks && key + 8 <= lim - p.window)) continue;
+    const int id = table[key >> p.log_page];
+    if (id < 0 || id >= p.pages) continue;
+    const int64_t cell = (int64_t)id * p.H + h, at = (cell * p.page + (key & p.page - 1)) * p.D + d;
+    const float ks = p.ks[cell], vs = p.vs[cell];
+    uint32_t kc[8], vc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      kc[j] = in ? *reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(p.k) + at + j * p.D) : 0;
+      vc[j] = in ? *reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(p.v) + at + j * p.D) : 0;
+    }
+    auto code = [](uint32_t w, int e) { return (float)(int8_t)(w >> 8 * e); };
+    float s[8], mx = y.m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s[j] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j] = fmaf(x[e] * ks, code(kc[j], e), s[j]);
+#pragma unroll
+      for (int f = 16; f > 0; f >>= 1) s[j] += __shfl_xor_sync(~0u, s[j], f);
+      s[j] = key + j < lim && (key + j >= lim - p.window || key + j < p.sinks) ? s[j] * (p.scale * 1.44269504f) : -INFINITY;
+      mx = fmaxf(mx, s[j]);
+    }
+    const float base = mx == -INFINITY ? 0.f : mx, had = y.l * ex2(y.m - base);
+    float l = had;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) l += s[j] = ex2(s[j] - base);
+    if (l == 0.f) continue;
+    const float r = 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum = fmaf(s[j] * r, code(vc[j], e), sum);
+      y.o[e] = y.o[e] * (had * r) + sum * vs;
+    }
+    y.m = mx;
+    y.l = l;
+  }
+}
+
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_constant__ AttnParams p) {
   using S = Shape8<DP>;
@@ -89,7 +154,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
   __shared__ alignas(8) uint64_t q_full[2], k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], s_full[2][2],
       p_full[2][2], pv_done[2], o_full[2], note_full[kInfo], codes_full[2][kCopies], codes_empty[2][kCopies];
   __shared__ Note notes[kInfo];
-  __shared__ float most[kThreads8 / 32];
+  __shared__ float most[kThreads8 / 32], least[kThreads8 / 32];
   __shared__ uint8_t row_power[kSoft];
   __shared__ uint32_t tmem_s;
   __shared__ int scan[kThreads8 / 32], tile_of[4], dead;
@@ -194,24 +259,38 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
     for (int i = 0; i < kInfo; ++i) mbar_init(su32(&note_full[i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // the largest scale of values among the pages that some token sees
-  float vtop = 0.f;
+  // the largest scale of values among the pages that some token sees, the smallest above 0, and whether one is 0
+  float vtop = 0.f, vleast = INFINITY;
+  bool zeros = false;
   {
     const int sinks = min(p.sinks, lim_max), pages0 = (sinks + p.page - 1) >> p.log_page, from = max(pages0, low >> p.log_page);
     const int count = pages0 + max(0, ((lim_max + p.page - 1) >> p.log_page) - from);
     for (int i = tid; i < count; i += kThreads8) {
       const int id = table[i < pages0 ? i : i - pages0 + from];
-      if (id >= 0 && id < p.pages) vtop = fmaxf(vtop, p.vs[(int64_t)id * p.H + h]);
+      const bool there = id >= 0 && id < p.pages;
+      const float vs = there ? p.vs[(int64_t)id * p.H + h] : 0.f;
+      zeros = zeros || (there && vs == 0.f);
+      vtop = fmaxf(vtop, vs);
+      vleast = fminf(vleast, vs > 0.f ? vs : INFINITY);
     }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) vtop = fmaxf(vtop, __shfl_xor_sync(~0u, vtop, d));
-    if (lane == 0) most[warp] = vtop;
+    for (int d = 16; d > 0; d >>= 1) {
+      vtop = fmaxf(vtop, __shfl_xor_sync(~0u, vtop, d));
+      vleast = fminf(vleast, __shfl_xor_sync(~0u, vleast, d));
+    }
+    if (lane == 0) {
+      most[warp] = vtop;
+      least[warp] = vleast;
+    }
   }
   tm_fence_before();
-  __syncthreads();
+  zeros = __syncthreads_or(zeros);
   tm_fence_after();
 #pragma unroll
-  for (int i = 0; i < kThreads8 / 32; ++i) vtop = fmaxf(vtop, most[i]);
+  for (int i = 0; i < kThreads8 / 32; ++i) {
+    vtop = fmaxf(vtop, most[i]);
+    vleast = fminf(vleast, least[i]);
+  }
   const uint32_t tmem = tmem_s;
   // a bounded wait; after one gave up none waits any more
   auto hold = [&](uint64_t* bar, uint32_t parity) {
@@ -274,7 +353,11 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
           note.ks[lane] = ks;
           note.lv[lane] = lv;
           note.inv[lane] = ex2(-lv);
-          if (lane == 0) note.valid = there;
+        }
+        const unsigned zero = __ballot_sync(~0u, lane < 8 && cell >= 0 && vs == 0.f);
+        if (lane == 0) {
+          note.valid = there;
+          note.zero = zero;
         }
         warp_arrive(&note_full[g % kInfo]);
         copy(1, p.v);
@@ -329,7 +412,7 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
     // where the halves go: rows 4 on of 8 are swizzled by 4 more chunks
     const int to0 = c / 4 * CHUNK_KV + key0 * 128;
     const int at0 = to0 + ((c % 4 * 2 + e ^ key0 & 7) << 4), at1 = to0 + ((c % 4 * 2 + 1 - e ^ key0 & 7) << 4);
-    auto turn = [&](unsigned char* to, const unsigned char* codes) {
+    auto turn = [&](unsigned char* to, const unsigned char* codes, uint32_t zero) {
       uint2 x[NI], y[NI];
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
@@ -338,6 +421,11 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
           x[i] = *reinterpret_cast<const uint2*>(codes + from + i * RPL * p.D);
           y[i] = *reinterpret_cast<const uint2*>(codes + from + i * RPL * p.D + other);
         }
+      }
+      if (__builtin_expect(zero, 0)) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          if (zero >> (key0 + i * RPL) / 8 & 1) x[i] = y[i] = make_uint2(0, 0);
       }
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
@@ -353,7 +441,12 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       const int st = g % kStages, at = g % kCopies;
       hold(&codes_full[pool][at], g / kCopies & 1);
       hold(&empty[st], (g / kStages + 1) & 1);
-      turn(buf + st * S::KV, codes + (pool * kCopies + at) * S::CODES);
+      uint32_t zero = 0;
+      if (__builtin_expect(pool && zeros, 0)) {  // (the note is written before the values' copy)
+        hold(&note_full[g % kInfo], g / kInfo & 1);
+        zero = notes[g % kInfo].zero;
+      }
+      turn(buf + st * S::KV, codes + (pool * kCopies + at) * S::CODES, zero);
       warp_arrive(&full[st]);
       if (lane == 0) mbar_arrive(su32(&codes_empty[pool][at]));
     }
@@ -589,6 +682,26 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       if (live_row) {
         if (parts) p.split_stats[at] = make_float2(m, l);
         else if (p.lse) p.lse[cell] = l == 0.f ? -INFINITY : log_sum<__half, kUp>(m, l);
+      }
+      unsigned again = __ballot_sync(~0u, live_row && l > kSmallPages && vleast < vtop * 0x1p-90f);
+      __syncwarp();  // what the rows' own threads wrote lies before what the warp writes over it
+      for (; again; again &= again - 1) {
+        const int r = warp % 4 * 32 + __ffs(again) - 1, token = p.G.div(r), head = h * p.G.d + p.G.mod(r), d = lane * 4;
+        Average y;
+        row_again<T>(p, static_cast<const T*>(p.q) + (base + token) * p.q_ts + (int64_t)head * p.q_hs, table, h, limit(t * T1 + token), first, n,
+                     sink_blocks, gap, y);
+        const int64_t cell = (int64_t)(base + token) * p.H * p.G.d + head, at = (int64_t)z * p.T * p.H * p.G.d + cell;
+        if (d < p.D) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (parts) p.split_sums[at * DP + d + e] = y.o[e];
+            else static_cast<T*>(p.out)[cell * p.D + d + e] = from_f32<T>(y.o[e]);
+          }
+        }
+        if (lane == 0) {
+          if (parts) p.split_stats[at] = make_float2(y.m, y.l);
+          else if (p.lse) p.lse[cell] = y.l == 0.f ? -INFINITY : y.m * 0.693147181f + logf(y.l);
+        }
       }
     }
     tm_fence_before();

@@ -213,3 +213,32 @@ def test_scales_below_normal_numbers_by_tiles(pp, dt):
     for H, G, D, page, L, n in TILED:
         over_codes(pp, dt, H, G, D, page, L, n, 10 ** 6, 0, of_scales([-130]), False)
         over_codes(pp, dt, H, G, D, page, L, n, 10 ** 6, 0, of_scales([-148]), False)
+
+
+def last_pages_larger(power, pages, more=None):
+    """The last `pages` pages have values 2^power times those before them."""
+    def change(h, table):
+        for w in range(table.shape[1] - pages, table.shape[1]):
+            h.s[1][int(table[0, w])] *= 2.0 ** power
+        if more is not None:
+            more(h, table)
+    return change
+
+
+@pytest.mark.parametrize("H,G,D,page,L,n,window,last", [(16, 8, 64, 16, 170, 48, 20, 2), (16, 8, 128, 64, 700, 100, 60, 1), (8, 8, 128, 64, 2100, 40, 1500, 1),
+                                                        (16, 4, 80, 8, 333, 90, 10 ** 6, 3)])
+@pytest.mark.parametrize("power", [40, 80, 88, 95, 120, 124])
+def test_rows_that_see_small_pages_alone_by_tiles(pp, H, G, D, page, L, n, window, last, power):
+    """Whatever the values are that other tokens of their tile see, down to a ratio that log2 of the scales no longer holds in the weights."""
+    over_codes(pp, BF16, H, G, D, page, L, n, window, 0, last_pages_larger(power, last), False)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("H,G,D,page,L,n,window", [(16, 8, 64, 16, 170, 48, 16), (16, 8, 128, 64, 700, 100, 60), (1, 4, 64, 16, 170, 5, 16)])
+def test_scales_of_zero(pp, dt, H, G, D, page, L, n, window):
+    """Pages whose value scale is 0 hold zeros, whatever their codes are."""
+    def change(h, table):
+        for w in range(0, table.shape[1] - 1):
+            if w % 4 != 1:
+                h.s[1][int(table[0, w])] = 0
+    over_codes(pp, dt, H, G, D, page, L, n, window, 0, last_pages_larger(100 if dt is BF16 else 4, 1, change), n * G * H < 1000)
