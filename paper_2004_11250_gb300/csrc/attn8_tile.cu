@@ -308,9 +308,9 @@ __global__ void __launch_bounds__(kThreads8, 1) attn8_tile_kernel(const __grid_c
       // ---- copies, and what there is to say of a block.  Lane j < 8 has keys 8 j on; a run of keys on one page is one copy.
       // Pages are looked up two blocks ahead and scales one, so that neither is waited for
       const int run = min(p.page, kKeys), runs = run >> 3;
-      auto look = [&](int k) {  // the page's entry of the table; INT32_MIN: none of the run's keys is there
+      auto look = [&](int k) {  // the page's entry of the table (-1: no page); INT32_MIN: none of the run's keys is there
         const int key = lane < 8 && k < n ? key_of(k) + (lane * 8 & ~(run - 1)) : INT32_MAX;
-        return key < lim_max && (key < p.sinks || key + run > low) ? table[key >> p.log_page] : INT32_MIN;
+        return key < lim_max && (key < p.sinks || key + run > low) ? max(table[key >> p.log_page], -1) : INT32_MIN;
       };
       // 1 over the largest scale, in two steps, as it may lie beyond fp32: a power of two, and what is left
       const float vup = __int_as_float((254 - min(max(__float_as_int(vtop) >> 23, 1), 253)) << 23), vinv = vtop > 0.f ? 1.f / (vtop * vup) : 0.f;

@@ -242,3 +242,34 @@ def test_scales_of_zero(pp, dt, H, G, D, page, L, n, window):
             if w % 4 != 1:
                 h.s[1][int(table[0, w])] = 0
     over_codes(pp, dt, H, G, D, page, L, n, window, 0, last_pages_larger(100 if dt is BF16 else 4, 1, change), n * G * H < 1000)
+
+
+# ------------------------------------------------------------------ entries of the table
+
+@pytest.mark.parametrize("codes", [True, False])
+@pytest.mark.parametrize("H,G,n", [(16, 8, 48), (1, 4, 5)])
+@pytest.mark.parametrize("entry", [-2 ** 31, -2 ** 31 + 1, -1, 2 ** 31 - 1])
+def test_entries_that_are_no_pages(pp, codes, H, G, n, entry):
+    """Each is recorded and skipped by every kernel where tokens see it, and looked at by none where they do not."""
+    D, page, L, dt = 64, 16, 170, F16
+    h = Held(pp, 13, H, page, D, dt)
+    k, v = h.values()
+    pool = [x.to(dt) for x in (k, v)]
+    cache = h.cache if codes else pp.pp_cache_create(pool[0].cuda(), pool[1].cuda())
+    k, v = (k, v) if codes else [x.double() for x in pool]
+    q = torch.randn((n, H * G, D), generator=torch.Generator().manual_seed(1)).to(dt)
+    try:
+        for w, window, status in ((8, 10 ** 6, pp.PP_CACHE_BAD_PAGE), (0, 10 ** 6, pp.PP_CACHE_BAD_PAGE), (10, 10 ** 6, pp.PP_CACHE_BAD_PAGE), (3, 50, 0)):
+            table = tables([L], page, 13)
+            table[0, w] = entry
+            out, lse = torch.empty((n, H * G, D), device="cuda", dtype=dt), torch.empty((n, H * G), device="cuda")
+            pp.pp_attn_window(cache, q.cuda(), ints([0, n]).cuda(), table.cuda(), ints([L]).cuda(), 0.125, pp.PP_ATTN_CAUSAL, window, 0, out, lse)
+            assert pp.pp_cache_device_status(cache) == status
+            want, wl, tol, tl = attend(q, k, v, table, [0, n], [L], 0.125, window, 0, False, 20)
+            close(out, want, tol)
+            close(lse, wl, tl)
+    finally:
+        torch.cuda.synchronize()
+        if not codes:
+            pp.pp_cache_destroy(cache)
+        h.close()
