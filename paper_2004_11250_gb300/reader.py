@@ -47,6 +47,17 @@ class Layer:
         self.cache = pp.pp_cache_create(self.k, self.v, self.codes, self.scales)
 
 
+def pages_in_turn(tokens: int, page: int, window: Optional[int], sinks: int, most: int):
+    """(pages of the cache, which of them each entry of the table is, tokens that a step may bring; None: any number).
+
+    The pages of the first tokens stay.  With a window the others are used in turn: they hold the windows of a step of
+    `most` tokens, the step, and a page begun at either end, so that no page of a step is another that it writes or reads."""
+    width = -(-tokens // page)
+    first = -(-sinks // page)
+    pages = width if window is None else min(width, first + -(-(window + most) // page) + 2)
+    return pages, [w if w < first or pages == width else first + (w - first) % (pages - first) for w in range(width)], most if pages < width else None
+
+
 class FrameReader:
     """Reads frames and answers about them (one sequence).
 
@@ -72,11 +83,7 @@ class FrameReader:
         self.bits, self.window, self.sinks = bits, window, sinks
         gen = torch.Generator(device="cuda")
         gen.manual_seed(seed)
-        width = pages = -(-max_tokens // page)  # of the table; of the cache
-        first = -(-sinks // page)               # pages that stay
-        if window is not None:  # the others in turn: a frame's windows, the frame, and a page begun at either end
-            turn = -(-(window + self.rows * self.cols) // page) + 2
-            pages = min(pages, first + turn)
+        pages, entries, self.most = pages_in_turn(max_tokens, page, window, sinks, self.rows * self.cols)
         self.layers: List[Layer] = [Layer(self.C, Hq, H, D, pages, page, dtype, gen, bits) for _ in range(layers)]
         # a quarter of the pairs follows the frame's number, the rest its rows and columns
         P = D // 2
@@ -86,10 +93,7 @@ class FrameReader:
         self.axis = axis
         self.rope = pp.pp_rope_create(D, axis, self.freq, 3)
         order = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32)
-        at = torch.arange(width, device="cuda")
-        if pages < width:
-            at = torch.where(at < first, at, first + (at - first) % (pages - first))
-        self.table = order[at][None].contiguous()
+        self.table = order[torch.tensor(entries, device="cuda")][None].contiguous()
         self.map = torch.empty(self.net.out_shape, device="cuda")
         self.seen = 0    # tokens in the cache
         self.frames = 0
@@ -102,10 +106,18 @@ class FrameReader:
         return (x * torch.rsqrt((x * x).mean(-1, keepdim=True) + self.EPS)).to(self.dtype)
 
     def step(self, x: torch.Tensor, pos: torch.Tensor) -> torch.Tensor:
-        """The decoder over T new tokens x [T][C] at positions pos [3][T] (int32): its outputs [T][C]."""
-        T, n = x.shape[0], self.seen
-        if n + T > self.table.shape[1] * self.page:
+        """The decoder over T new tokens x [T][C] at positions pos [3][T] (int32): its outputs [T][C].  Where pages are used in
+        turn, a frame's number of tokens after the other: they have room for the windows of no more."""
+        T = x.shape[0]
+        if self.seen + T > self.table.shape[1] * self.page:
             raise ValueError("the cache is full")
+        if self.most is None or T <= self.most:
+            return self._step(x, pos)
+        parts = [slice(i, i + self.most) for i in range(0, T, self.most)]
+        return torch.cat([self._step(x[i], pos[:, i].contiguous()) for i in parts])
+
+    def _step(self, x: torch.Tensor, pos: torch.Tensor) -> torch.Tensor:
+        T, n = x.shape[0], self.seen
         s = torch.cuda.current_stream()
         at = torch.arange(n, n + T, device="cuda")
         slots = (self.table[0][at // self.page] * self.page + at % self.page).to(torch.int32)
