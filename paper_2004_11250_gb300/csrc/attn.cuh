@@ -69,6 +69,24 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Four codes as f16, in the bytes' order or the even ones and the odd ones: a byte u = code + 128 below the exponent of 1024
+// is 1024 + u.
+__device__ __forceinline__ uint32_t f16_of(uint32_t biased, uint32_t bytes) {
+  const uint32_t w = __byte_perm(biased, 0x64646464u, bytes);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1152.f));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void f16_in_order(uint32_t codes, uint32_t& a, uint32_t& b) {
+  const uint32_t u = codes ^ 0x80808080u;
+  a = f16_of(u, 0x4140);
+  b = f16_of(u, 0x4342);
+}
+__device__ __forceinline__ void f16_by_parity(uint32_t codes, uint32_t& even, uint32_t& odd) {
+  const uint32_t u = codes ^ 0x80808080u;
+  even = f16_of(u, 0x4240);
+  odd = f16_of(u, 0x4341);
+}
+
 // Whether some of 16 bytes of values are not finite.
 template <class T>
 __device__ __forceinline__ bool not_finite(uint4 v) {

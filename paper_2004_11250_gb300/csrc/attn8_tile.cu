@@ -68,16 +68,12 @@ struct alignas(16) Note {           // of a block
   uint32_t valid, zero;             // a bit for each 8 keys that are there; whose values are 0 as their scale is
 };
 
-// 16 codes as 16 f16 (attn_row.cuh has the same by bytes' parity)
-__device__ __forceinline__ uint32_t f16_pair(uint32_t biased, uint32_t bytes) {
-  const uint32_t w = __byte_perm(biased, 0x64646464u, bytes);  // 1024 + code + 128
-  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1152.f));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
+// 8 codes as f16, in order
 __device__ __forceinline__ uint4 f16_of8(uint32_t a, uint32_t b) {
-  a ^= 0x80808080u;
-  b ^= 0x80808080u;
-  return make_uint4(f16_pair(a, 0x4140), f16_pair(a, 0x4342), f16_pair(b, 0x4140), f16_pair(b, 0x4342));
+  uint4 y;
+  f16_in_order(a, y.x, y.y);
+  f16_in_order(b, y.z, y.w);
+  return y;
 }
 
 // A row's attention over blocks of keys of its own, by one warp in fp32, 8 keys (of one page) at a time: o is the average so far of

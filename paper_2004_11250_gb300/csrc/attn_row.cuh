@@ -154,24 +154,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// Four codes as f16, in the bytes' order or the even ones and the odd ones: a byte u = code + 128 below the exponent of 1024
-// is 1024 + u.
-__device__ __forceinline__ uint32_t f16_of(uint32_t biased, uint32_t bytes) {
-  const uint32_t w = __byte_perm(biased, 0x64646464u, bytes);
-  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1152.f));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ void f16_in_order(uint32_t codes, uint32_t& a, uint32_t& b) {
-  const uint32_t u = codes ^ 0x80808080u;
-  a = f16_of(u, 0x4140);
-  b = f16_of(u, 0x4342);
-}
-__device__ __forceinline__ void f16_by_parity(uint32_t codes, uint32_t& even, uint32_t& odd) {
-  const uint32_t u = codes ^ 0x80808080u;
-  even = f16_of(u, 0x4240);
-  odd = f16_of(u, 0x4341);
-}
-
 // Where chunk c of a key's codes lies in a tile.
 template <class S>
 __device__ __forceinline__ int place8(int key, int c) {
@@ -1204,30 +1186,30 @@ __global__ void __launch_bounds__(Shape<T, Cell, DP, RB>::THREADS, Shape<T, Cell
             rl[r] = sum;
           }
         } else {
-        for (int i = tid; i < n * kRows; i += kWarps * 32) {  // row i % 16 of part i / 16
-          const float* from = slot(part + i / kRows * step) + kRows * DP + i % kRows;
-          if (i % kRows < nrows) {
-            wts[i % kRows][i / kRows] = __ldcg(from);
-            sums[i % kRows][i / kRows] = __ldcg(from + kRows);
+          for (int i = tid; i < n * kRows; i += kWarps * 32) {  // row i % 16 of part i / 16
+            const float* from = slot(part + i / kRows * step) + kRows * DP + i % kRows;
+            if (i % kRows < nrows) {
+              wts[i % kRows][i / kRows] = __ldcg(from);
+              sums[i % kRows][i / kRows] = __ldcg(from + kRows);
+            }
           }
-        }
-        if constexpr (S::EIGHT) {
-          bool any = false;
-          for (int i = lane; i < n; i += 32) any = any || __ldcg(slot(part + i * step) + kGrain) != 1.f;
-          grain = __any_sync(~0u, any) ? 1.f / kLess : 1.f;
-        }
-        group_sync<kWarps * 32>();
-        if (tid < nrows) {
-          float mx = -INFINITY, sum = 0.f;
-          for (int i = 0; i < n; ++i) mx = fmaxf(mx, wts[tid][i]);
-          for (int i = 0; i < n; ++i) {
-            const float c = wts[tid][i] == -INFINITY ? 0.f : ex2(wts[tid][i] - mx);
-            wts[tid][i] = S::EIGHT ? in_grain(c, __ldcg(slot(part + i * step) + kGrain)) : c;
-            sum += c * sums[tid][i];  // NaN stays NaN
+          if constexpr (S::EIGHT) {
+            bool any = false;
+            for (int i = lane; i < n; i += 32) any = any || __ldcg(slot(part + i * step) + kGrain) != 1.f;
+            grain = __any_sync(~0u, any) ? 1.f / kLess : 1.f;
           }
-          rm[tid] = mx;
-          rl[tid] = sum;
-        }
+          group_sync<kWarps * 32>();
+          if (tid < nrows) {
+            float mx = -INFINITY, sum = 0.f;
+            for (int i = 0; i < n; ++i) mx = fmaxf(mx, wts[tid][i]);
+            for (int i = 0; i < n; ++i) {
+              const float c = wts[tid][i] == -INFINITY ? 0.f : ex2(wts[tid][i] - mx);
+              wts[tid][i] = S::EIGHT ? in_grain(c, __ldcg(slot(part + i * step) + kGrain)) : c;
+              sum += c * sums[tid][i];  // NaN stays NaN
+            }
+            rm[tid] = mx;
+            rl[tid] = sum;
+          }
         }
         group_sync<kWarps * 32>();
         for (int i = tid; i < nrows * (DP / 4); i += kWarps * 32) {

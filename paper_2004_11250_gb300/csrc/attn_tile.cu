@@ -599,56 +599,56 @@ __global__ void __launch_bounds__(kThreadsT, 2)
             }
           }
           if (WIN ? __builtin_expect(again, 0) : again) {
-          float top[4];
+            float top[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            top[c] = fmaxf(x[c], x[c + 4]);
+            for (int c = 0; c < 4; ++c) {
+              top[c] = fmaxf(x[c], x[c + 4]);
 #pragma unroll
-            for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
-          }
-          const float most = __fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl);
-          const float mx = !see ? -INFINITY : WIN ? lower(most, kUpWindow<T>) : lower(most, kLift<T, kUp>);
-          const bool grow = mx > __fadd_rd(m, kGrow<T>);  // from -infinity, too
-          if (__any_sync(~0u, grow)) {
-            const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
-            m = to;
-            l *= f;
-            if (g > 0) {  // the sums so far, in TMEM
-              hold(&pv_done, (g - 1) & 1);
-              waited = true;
-              __syncwarp();
-              tm_fence_after();
-#pragma unroll
-              for (int c = 0; c < DP; c += 32) {
-                float o[32];
-                tm_ld32(row_tm + c, o);
-                tm_wait_ld();
-                uint32_t r[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * f);
-                tm_st32(row_tm + c, r);
-              }
-              tm_wait_st();
+              for (int i = 8; i < 64; i += 8) top[c] = fmaxf(top[c], fmaxf(x[i + c], x[i + c + 4]));
             }
-          }
-          const float at = see ? (m == -INFINITY ? 0.f : m) : INFINITY;
-          const uint64_t sl2 = pack2(sl, sl), at2 = pack2(-at, -at);
-          uint64_t sum[4] = {};
+            const float most = __fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), sl);
+            const float mx = !see ? -INFINITY : WIN ? lower(most, kUpWindow<T>) : lower(most, kLift<T, kUp>);
+            const bool grow = mx > __fadd_rd(m, kGrow<T>);  // from -infinity, too
+            if (__any_sync(~0u, grow)) {
+              const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.f : ex2(m - to);
+              m = to;
+              l *= f;
+              if (g > 0) {  // the sums so far, in TMEM
+                hold(&pv_done, (g - 1) & 1);
+                waited = true;
+                __syncwarp();
+                tm_fence_after();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+                for (int c = 0; c < DP; c += 32) {
+                  float o[32];
+                  tm_ld32(row_tm + c, o);
+                  tm_wait_ld();
+                  uint32_t r[32];
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * f);
+                  tm_st32(row_tm + c, r);
+                }
+                tm_wait_st();
+              }
+            }
+            const float at = see ? (m == -INFINITY ? 0.f : m) : INFINITY;
+            const uint64_t sl2 = pack2(sl, sl), at2 = pack2(-at, -at);
+            uint64_t sum[4] = {};
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float a, c;
+              // scaled as the maximum is and then taken from it, not in one step (a product plus 0, so that the two are not merged):
+              // where scores are so large that fp32 numbers lie further than 1 apart, no weight passes its bound and the largest
+              // does not vanish
+              unpack2(add2(fma2(pack2(x[2 * i], x[2 * i + 1]), sl2, pack2(0.f, 0.f)), at2), a, c);
+              a = ex2(a);
+              c = ex2(c);
+              sum[i & 3] = add2(sum[i & 3], pack2(a, c));
+              w[i] = pack<T>(a, c);
+            }
             float a, c;
-            // scaled as the maximum is and then taken from it, not in one step (a product plus 0, so that the two are not merged):
-            // where scores are so large that fp32 numbers lie further than 1 apart, no weight passes its bound and the largest
-            // does not vanish
-            unpack2(add2(fma2(pack2(x[2 * i], x[2 * i + 1]), sl2, pack2(0.f, 0.f)), at2), a, c);
-            a = ex2(a);
-            c = ex2(c);
-            sum[i & 3] = add2(sum[i & 3], pack2(a, c));
-            w[i] = pack<T>(a, c);
-          }
-          float a, c;
-          unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, c);
-          l += a + c;
+            unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, c);
+            l += a + c;
           }
         }
         tm_st32(tm, w);
