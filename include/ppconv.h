@@ -658,8 +658,11 @@ pp_status pp_cache_select(const pp_cache* cache, int T, const void* q, int64_t q
  *           order, the ones that the token sees before others (of a token that sees P pages the first
  *           min(keep, P) entries count; those below 0 are skipped); NULL (keep 0): all pages
  * What the cache holds outside the visible keys is never used, NaN and infinities included.
- * A cache in 8 bits has its codes used as they are, exact, with the scales of their pages in fp32, and queries count with
- * all their bits.  A weight is two f16 halves (few rows per key: down to 2^-14 of the row's largest, those below 2^-36 are
+ * Sums of weights (up to 1, with many tokens in bf16 up to 2^8) times values are fp32's before they are divided: values may
+ * be as large as that leaves room for, over a cache in 8 bits as the type's largest.
+ * A cache in 8 bits has its codes used as they are, exact, with the scales of their pages in fp32.  Queries come as f16 times
+ * a power of two for each row: f16 as it is, bf16 exact down to 2^-31 of the row's largest (below in steps of 2^-38 of that),
+ * fp32 as three parts, to 2^-33 of a value and 2^-39 of the row's largest; rows below 2^-111 have fewer bits.  A weight is two f16 halves (few rows per key: down to 2^-14 of the row's largest, those below 2^-36 are
  * 0; in pages of 8 and 16 down to 2^-8, below 2^-30 0) or, times its page's value scale over the largest that the tokens near
  * by see, one of 11 bits (many tokens in 16 bits: down to 2^-22 of the row's largest such product, below 2^-33 0).  Scales
  * are finite and not negative, up to the largest that values have; beside value scales above 2^70 that a token or its
@@ -682,8 +685,8 @@ pp_status pp_attn_forward(const pp_cache* cache, int T, const void* q, int64_t q
  * `window` (its own among them) and the first `sinks`.  Over either kind of cache.  Pages between the first keys and
  * the windows of a call's tokens are not read, and their entries of the table not looked at (they may be -1, and
  * the pages in use elsewhere); a window of width * page keys or more gives pp_attn_forward's bits.  f16 weights of many tokens
- * have 11 bits down to 2^-24 of the row's largest, and are 0 below 2^-35. (bf16 over a cache in bf16: 8 bits
- * down to 2^-85, and 0 below; values may be as large as the type's largest).
+ * have 11 bits down to 2^-24 of the row's largest, and are 0 below 2^-35; those in bf16 have 8 down to 2^-85, are 0
+ * below, and leave room for values as large as the type's largest.
  * Errors: as pp_attn_forward; also window < 1, sinks < 0.
  */
 pp_status pp_attn_window(const pp_cache* cache, int T, const void* q, int64_t q_ts, int64_t q_hs, int Hq, int B,

@@ -23,8 +23,11 @@
 // smaller.  So most blocks read S once, and neither wait for nor look for a maximum.  That
 // path lies behind the loop: in line, the instruction cache cost a tenth of the time.
 //
-// Measured: 2048 tokens over 32768 keys, 32 heads of 128 over 8 (bf16): 1.01 ms, 1050 TFLOP/s
-// (keys of 16 bits: 1.01 ms).  Bound by shared memory and by whole rounds of CTAs: per 64 keys of
+// log2 vs reaches down to -90: a tile knows the smallest scale that its tokens see, and rows
+// with nearly all their weight on pages of less are computed again, each by a warp.
+//
+// Measured: 2048 tokens over 32768 keys, 32 heads of 128 over 8: 1.02 ms in bf16, 1040
+// TFLOP/s, 1.01 in f16 (keys of 16 bits: 1.01 ms).  Bound by shared memory and by whole rounds of CTAs: per 64 keys of
 // two tiles the products read 128 KB of it and the codes' way takes 64, 1540 cycles at its rate,
 // of some 1900; and 256 pairs of tiles come in two rounds of 152.  128 keys at a time, which read
 // the queries half as often, leave no room for a second S: 1.4 ms.
@@ -749,8 +752,8 @@ bool tile8_applicable(const AttnParams& p, int dtype, int sms) {
   if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
   // By what 64 keys of every sequence take.  The row kernel has three CTAs per SM, each of which meets them with 8 rows in about
   // 0.95 us; a CTA here meets them with a tile in as much, with two in 1.5 times that, and the CTAs come in rounds.  32 heads of
-  // 128 over 8, bf16, rows and tiles: 16 rows of each of 32 sequences of up to 8192 keys 168 and 197 us, 32 rows 324 and 197; 20
-  // rows of one of 30000 43 and 70, 64 rows of one of 32768 95 and 76, 1024 rows 1144 and 227.
+  // 128 over 8, bf16, rows and tiles: 16 rows of each of 32 sequences of 8192 keys 152 and 235 us (of up to 8192 96 and 175), 32
+  // rows 316 and 237 (172 and 176); 20 rows of one of 30000 41 and 66, 64 rows of one of 32768 84 and 72, 1024 rows 1042 and 207.
   const int64_t units = ((int64_t)p.T * p.G.d + 7) / 8 * p.H, pairs = most_pairs(p), s = splits_of(p, sms);
   const bool two = (int64_t)p.T * p.G.d > (int64_t)kRowsT * p.B;
   return units * s * 2 > 3 * (int64_t)sms * ((pairs * s + sms - 1) / sms) * (two ? 3 : 2);

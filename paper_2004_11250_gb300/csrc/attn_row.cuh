@@ -22,9 +22,9 @@
 // 16 rows (48 us against 22 in the fp32 case below).
 //
 // Measured, of a copy rate of 6.8 TB/s: 8 sequences of 65536 keys, 32 heads of 128
-// over 8 (f16) 308 us, 7.0 TB/s; 48 of up to 8192 (bf16) 151 us, 5.7 TB/s; 32 tokens
+// over 8 (f16) 303 us, 7.1 TB/s; 48 of up to 8192 (bf16) 143 us, 6.1 TB/s; 32 tokens
 // over 32 selected pages of 64 each (bf16) 45 us, 5.9 TB/s; fp32, 16 of up to 2500, 8
-// heads of 96 over 4: 22 us, 3.2 TB/s.  One sequence of 777 keys: 11 us, a chain of
+// heads of 96 over 4: 22 us, 3.2 TB/s.  One sequence of 777 keys: 10 us, a chain of
 // launch, lengths, page table, copy, tile and join.
 //
 // Over a cache in 8 bits a tile is 128 keys.  Codes are whole numbers, exact in f16, so
@@ -36,9 +36,9 @@
 // instructions for two: placed below the exponent of 1024, and 1152 taken
 // off.  At half the bytes a key the instructions count: weights are taken from the last
 // maximum while they fit, 8 rows to a unit leave registers for three CTAs per SM, and what is
-// rare lies behind the loop.  8 sequences of 65536 keys (f16) 169 us, 6.4 TB/s (260 at
-// first); 48 of up to 8192 (bf16) 80 us, 5.4 TB/s (114); the same in fp32 95 us; one of 777
-// keys 10.5 us.
+// rare lies behind the loop.  8 sequences of 65536 keys (f16) 168 us, 6.4 TB/s (260 at
+// first); 48 of up to 8192 (bf16) 79 us, 5.5 TB/s (114); the same in fp32 93 us, three
+// products where 16 bits have one; one of 777 keys 10.8 us.
 //
 // With a window, a unit's tiles are those of the first keys and of its rows' windows; what
 // lies between is not looked up.  32 tokens over 4096 of 32768 keys and 16 first ones (bf16):

@@ -34,8 +34,8 @@
 // With a window (a kernel of its own) the blocks between the first keys and the windows
 // are left out, and m is not looked for in each block: sums of 8 weights say when one
 // might not fit, and the block is computed again.  2048 tokens over windows of 4096
-// keys and 64 first ones (f16): 168 us, 830 TFLOP/s; each tile's start and end take a
-// sixth of it, and 512 tiles come in two rounds of 304.
+// keys and 64 first ones: 173 us, 805 TFLOP/s in f16, 168 in bf16; each tile's start and
+// end take a sixth of it, and 512 tiles come in two rounds of 304.
 #include <algorithm>
 #include <type_traits>
 
@@ -868,7 +868,7 @@ bool tile_applicable(const AttnParams& p, int dtype, int sms) {
   if (dtype == PP_F32 || p.D > 128 || p.G.d > 64 || !p.starts) return false;
   // a tile's list entries are counted in 32 bits
   if (p.sel && (int64_t)(kRowsT / p.G.d) * p.keep > INT32_MAX - 2 * kAhead * kThreadsT) return false;
-  // Units of rows (attn.cu) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where pages
+  // Units of rows (attn_row.cuh) share the keys' length among all CTAs, but meet each key with 16 rows (one token's, where pages
   // are selected) at about 1 us per 64 keys and CTA; a tile meets it with 128 in about the same, split 8 times at most.
   // Selected pages: neighbouring tokens' together are some four times one token's.
   // How tokens are spread over sequences is not known here.  Where sequences have less than a unit's 16 rows each (then

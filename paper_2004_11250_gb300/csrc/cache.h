@@ -37,7 +37,7 @@ struct pp_cache {
 
 namespace ppc {
 
-// The row kernel's keys per tile (attn.cu): 64 rows of 16-bit values, 32 of fp32.
+// The row kernel's keys per tile (attn_row.cuh): 64 rows of 16-bit values, 32 of fp32.
 inline int tile_keys(int dtype) { return dtype == PP_F32 ? 32 : 64; }
 constexpr int kTileKeys8 = 128;  // over codes of 8 bits
 // Device bytes that attention needs beside the status word: counters, partial results, shares of tiles.
