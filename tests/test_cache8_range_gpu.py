@@ -273,3 +273,39 @@ def test_entries_that_are_no_pages(pp, codes, H, G, n, entry):
         if not codes:
             pp.pp_cache_destroy(cache)
         h.close()
+
+
+@pytest.mark.parametrize("dt,H,G,D,page,L,n,window", [(F32, 2, 3, 256, 16, 500, 1, 300), (BF16, 1, 5, 256, 128, 3000, 1, 10 ** 6), (F32, 1, 16, 128, 256, 700, 3, 10 ** 6),
+                                                      (BF16, 2, 8, 16, 8, 90, 2, 33), (F32, 4, 1, 48, 16, 5000, 1, 4000), (BF16, 1, 64, 128, 16, 40, 1, 10 ** 6)])
+@pytest.mark.parametrize("powers", [[120], [0, 120], [90, -30, 5], [-100, 0, 60]])
+def test_values_of_any_size_in_other_layouts(pp, dt, H, G, D, page, L, n, window, powers):
+    over_codes(pp, dt, H, G, D, page, L, n, window, 7, of_scales(powers), True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B,most,page", [(700, 300, 16), (5, 4000, 64), (40, 900, 8)])
+def test_sequences_of_large_values_beside_others(pp, dt, B, most, page):
+    """Some sequences of a batch, and in some only the last pages, have values near the types' largest: CTAs go from one to the other."""
+    H, G, D = 1, 2, 64
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, most, (B,), generator=g).tolist()
+    need = sum(-(-v // page) for v in lens)
+    h = Held(pp, need, H, page, D, dt)
+    table = tables(lens, page, need)
+    for b, v in enumerate(lens):
+        w = -(-v // page)
+        for i in range({0: 0, 1: w // 2}.get(b % 4, w), w):
+            h.s[1][int(table[b, i])] *= 2.0 ** 124
+    h.ds[1].copy_(h.s[1])
+    k, v = h.values()
+    q = torch.randn((B, H * G, D), generator=g).to(dt)
+    out, lse = torch.full((B, H * G, D), math.nan, device="cuda", dtype=dt), torch.full((B, H * G), math.nan, device="cuda")
+    try:
+        pp.pp_attn_forward(h.cache, q.cuda(), None, table.cuda(), ints(lens).cuda(), 0.125, 0, None, out, lse)
+        assert h.status() == 0
+        want, wl, tol, tl = attend(q, k, v, table, None, lens, 0.125, 2 ** 31 - 1, 0, True)
+        close(out, want, tol)
+        seen = torch.isfinite(wl)
+        close(lse.cpu()[seen], wl[seen], tl[seen])
+    finally:
+        h.close()
